@@ -575,6 +575,80 @@ cat_status cat_debug_pca_patience(int64_t looks);
 enum { CAT_PCA_COLUMNS = 0, CAT_PCA_ALONE = 1, CAT_PCA_GRID = 2 };
 size_t cat_debug_pca_route_offset(int64_t N, int64_t D, int32_t p, cat_dtype dt, int32_t sweeps);
 
+/* ---- a transformer block's training step, with its activations kept in 8 bits ----
+ * Transformers are quantised block by block: the block's parameters are fitted on the calibration rows, and the rows that
+ * the fitted network gives are the LQ rows of cat_fit (App. H of the paper: ViT, DeiT, Swin).  These are the operators of
+ * such a step: layer norm, the product with bias, activation and residual, their gradients, and checkpoints in 8 bits
+ * of what the backward passes read again.
+ *
+ * Beside the conventions at the top: zero rows are allowed (sums over rows are then zero, arrays of rows may be NULL); a row may have any length,
+ * also an odd number of bfloat16 entries; every array that is given starts on a 16-byte boundary; parameters of the
+ * norm, biases and their gradients are float; outputs alias no input.  NaN and infinities go where the formulas take
+ * them.  Sums, means and products are held in fp32 and rounded once to `dt`.  Results are the same bits on every call:
+ * no order of additions depends on timing.
+ *
+ * cat_pack8     codes (N x D int8) and scales (N x ceil(D / 128) float) of x (N x D of dt).  128 consecutive channels of
+ *               a row (CAT_PACK_GROUP; the last group may be shorter) share a scale s = a / 127, a the group's
+ *               largest magnitude; a channel's code is the integer nearest to x * (127 / a), ties to even, and stands for
+ *               code * s.  Both quotients and the product are rounded to float.  A group with a < 2^-100 is held as zeros;
+ *               a NaN or an infinity makes all values of its group NaN.
+ * cat_unpack8   x = code * scale, rounded to dt.
+ * cat_layer_norm         mu and v the mean and the (biased) variance of a row, rstd = 1 / sqrt(v + eps),
+ *               y = (x - mu) * rstd * weight + bias.  weight, bias (D floats) nullable: 1 and 0.  mean, rstd (N floats)
+ *               nullable.  codes, scales: both or neither, the checkpoint of x as cat_pack8 gives it.
+ *               eps >= 0, finite (0 gives infinities on rows without variance).
+ * cat_layer_norm_packed  y from the checkpoint of x and its saved mean and rstd.
+ * cat_layer_norm_backward  with xhat = (x - mean) * rstd, g = dy * weight (x: the rows, or their checkpoint: one of the two):
+ *               dx = rstd * (g - mean_row(g) - xhat * mean_row(g * xhat)) + residual_grad (nullable, N x D of dt),
+ *               dweight = sum over rows of dy * xhat, dbias = sum over rows of dy (D floats, each nullable).
+ * cat_linear    z = x w^T + bias (x: M x K, w: N x K, bias: N floats, nullable), y = act(z) + residual (M x N, nullable).
+ *               codes, scales: both or neither, the checkpoint of z (of its fp32 values).
+ * cat_linear_backward_input   dx = (dy w) * act'(c): dy M x N, w N x K, dx M x K; c (M x K) the checkpoint of the rows whose
+ *               activation was the product's input; without codes act must be CAT_ACT_NONE.
+ * cat_linear_backward_weight  dw = dy^T u (N x K of dt), dbias = sum over rows of dy (N floats, nullable); u = x (M x K), or
+ *               act(c) of a checkpoint c.  With bfloat16 rows u is rounded to bfloat16 for the matrix cores.
+ * cat_activation_backward     dz = dy * act'(c), for an activation whose output goes elsewhere than into a product.
+ *
+ * Activations: CAT_ACT_GELU is z Phi(z) (erf), CAT_ACT_GELU_TANH its approximation 0.5 z (1 + tanh(sqrt(2 / pi) (z +
+ * 0.044715 z^3))), CAT_ACT_SILU z / (1 + exp(-z)).  The derivative of CAT_ACT_RELU at 0 is 0.
+ * One size of workspace covers both gradients of a product.  M, N (rows), K and D stay below 2^31; offsets are 64-bit.
+ * Errors: CAT_ERR_INVALID_ARG (shape, type, null or misaligned pointer, codes without scales, both or none of rows and
+ * checkpoint, unknown activation, eps), CAT_ERR_WORKSPACE, CAT_ERR_DEVICE. */
+#define CAT_PACK_GROUP 128
+typedef enum {
+    CAT_ACT_NONE = 0,
+    CAT_ACT_RELU = 1,
+    CAT_ACT_GELU = 2,
+    CAT_ACT_GELU_TANH = 3,
+    CAT_ACT_SILU = 4
+} cat_activation;
+cat_status cat_pack8(const void *x, int64_t N, int64_t D, cat_dtype dt, int8_t *codes, float *scales, void *hip_stream);
+cat_status cat_unpack8(const int8_t *codes, const float *scales, int64_t N, int64_t D, cat_dtype dt, void *x,
+                       void *hip_stream);
+cat_status cat_layer_norm(const void *x, int64_t N, int64_t D, cat_dtype dt, const float *weight, const float *bias,
+                          float eps, void *y, float *mean, float *rstd, int8_t *codes, float *scales, void *hip_stream);
+cat_status cat_layer_norm_packed(const int8_t *codes, const float *scales, const float *mean, const float *rstd,
+                                 int64_t N, int64_t D, cat_dtype dt, const float *weight, const float *bias, void *y,
+                                 void *hip_stream);
+size_t cat_layer_norm_backward_workspace_bytes(int64_t N, int64_t D, cat_dtype dt);
+cat_status cat_layer_norm_backward(const void *dy, const void *x, const int8_t *codes, const float *scales,
+                                   const float *mean, const float *rstd, int64_t N, int64_t D, cat_dtype dt,
+                                   const float *weight, const void *residual_grad, void *dx, float *dweight, float *dbias,
+                                   void *workspace, size_t workspace_bytes, void *hip_stream);
+size_t cat_linear_workspace_bytes(int64_t M, int64_t N, int64_t K, cat_dtype dt);
+cat_status cat_linear(const void *x, const void *w, const float *bias, const void *residual, int64_t M, int64_t N,
+                      int64_t K, cat_dtype dt, cat_activation act, void *y, int8_t *codes, float *scales,
+                      void *workspace, size_t workspace_bytes, void *hip_stream);
+size_t cat_linear_backward_workspace_bytes(int64_t M, int64_t N, int64_t K, cat_dtype dt);
+cat_status cat_linear_backward_input(const void *dy, const void *w, const int8_t *codes, const float *scales,
+                                     int64_t M, int64_t N, int64_t K, cat_dtype dt, cat_activation act, void *dx,
+                                     void *workspace, size_t workspace_bytes, void *hip_stream);
+cat_status cat_linear_backward_weight(const void *dy, const void *x, const int8_t *codes, const float *scales,
+                                      int64_t M, int64_t N, int64_t K, cat_dtype dt, cat_activation act, void *dw,
+                                      float *dbias, void *workspace, size_t workspace_bytes, void *hip_stream);
+cat_status cat_activation_backward(const void *dy, const int8_t *codes, const float *scales, int64_t N, int64_t D,
+                                   cat_dtype dt, cat_activation act, void *dz, void *hip_stream);
+
 /* Message of the last non-OK status on the calling thread ("" if none).  The
  * pointer stays valid until the next failing call on the same thread. */
 const char *cat_last_error(void);

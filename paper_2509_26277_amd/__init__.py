@@ -26,6 +26,15 @@ from .binding import (  # noqa: F401
     cat_fit_multi_k,
     cat_params_to_bf16,
     cat_apply_lp,
+    cat_pack8,
+    cat_unpack8,
+    cat_layer_norm,
+    cat_layer_norm_packed,
+    cat_layer_norm_backward,
+    cat_linear,
+    cat_linear_backward_input,
+    cat_linear_backward_weight,
+    cat_activation_backward,
     cat_fit_workspace_bytes,
     cat_apply_workspace_bytes,
     library_path,

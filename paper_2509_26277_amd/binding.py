@@ -31,7 +31,10 @@ EXPORTS = ("cat_select_path", "cat_fit_workspace_bytes", "cat_apply_workspace_by
            "cat_fit_multi_k_workspace_bytes", "cat_fit_multi_k", "cat_debug_multi_group_tiles",
            "cat_params_to_bf16", "cat_apply_lp_workspace_bytes", "cat_apply_lp",
            "cat_fit_bounds_workspace_bytes", "cat_fit_bounds", "cat_debug_padded_fit", "cat_debug_full_loop", "cat_debug_loop", "cat_debug_loop_route_offset", "cat_debug_pca_patience",
-           "cat_debug_pca_route_offset", "cat_stream_probe")
+           "cat_debug_pca_route_offset", "cat_stream_probe",
+           "cat_pack8", "cat_unpack8", "cat_layer_norm", "cat_layer_norm_packed", "cat_layer_norm_backward_workspace_bytes",
+           "cat_layer_norm_backward", "cat_linear_workspace_bytes", "cat_linear", "cat_linear_backward_workspace_bytes",
+           "cat_linear_backward_input", "cat_linear_backward_weight", "cat_activation_backward")
 
 
 class CatError(RuntimeError):
@@ -154,6 +157,31 @@ def load_library():
     lib.cat_debug_list_capacity.restype = c.c_int
     lib.cat_debug_rerank_queue.argtypes = [c.c_int]
     lib.cat_debug_rerank_queue.restype = c.c_int
+    dt, f32 = c.c_int, c.c_float
+    lib.cat_pack8.argtypes = [vp, i64, i64, dt, vp, vp, vp]
+    lib.cat_pack8.restype = c.c_int
+    lib.cat_unpack8.argtypes = [vp, vp, i64, i64, dt, vp, vp]
+    lib.cat_unpack8.restype = c.c_int
+    lib.cat_layer_norm.argtypes = [vp, i64, i64, dt, vp, vp, f32, vp, vp, vp, vp, vp, vp]
+    lib.cat_layer_norm.restype = c.c_int
+    lib.cat_layer_norm_packed.argtypes = [vp, vp, vp, vp, i64, i64, dt, vp, vp, vp, vp]
+    lib.cat_layer_norm_packed.restype = c.c_int
+    lib.cat_layer_norm_backward_workspace_bytes.argtypes = [i64, i64, dt]
+    lib.cat_layer_norm_backward_workspace_bytes.restype = sz
+    lib.cat_layer_norm_backward.argtypes = [vp, vp, vp, vp, vp, vp, i64, i64, dt, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.cat_layer_norm_backward.restype = c.c_int
+    lib.cat_linear_workspace_bytes.argtypes = [i64, i64, i64, dt]
+    lib.cat_linear_workspace_bytes.restype = sz
+    lib.cat_linear.argtypes = [vp, vp, vp, vp, i64, i64, i64, dt, c.c_int, vp, vp, vp, vp, sz, vp]
+    lib.cat_linear.restype = c.c_int
+    lib.cat_linear_backward_workspace_bytes.argtypes = [i64, i64, i64, dt]
+    lib.cat_linear_backward_workspace_bytes.restype = sz
+    lib.cat_linear_backward_input.argtypes = [vp, vp, vp, vp, i64, i64, i64, dt, c.c_int, vp, vp, sz, vp]
+    lib.cat_linear_backward_input.restype = c.c_int
+    lib.cat_linear_backward_weight.argtypes = [vp, vp, vp, vp, i64, i64, i64, dt, c.c_int, vp, vp, vp, sz, vp]
+    lib.cat_linear_backward_weight.restype = c.c_int
+    lib.cat_activation_backward.argtypes = [vp, vp, vp, i64, i64, dt, c.c_int, vp, vp]
+    lib.cat_activation_backward.restype = c.c_int
     lib.cat_last_error.argtypes = []
     lib.cat_last_error.restype = c.c_char_p
     _lib = lib
@@ -648,3 +676,177 @@ def cat_apply_pca(lq, mean, components, centroids_z, gamma, beta, alpha=1.0, wan
                              float(alpha), _dev(out, lq.dtype, (N, D), "out"), None if a is None else a.data_ptr(),
                              workspace.data_ptr(), workspace.numel(), _stream()))
     return out, a
+
+
+# ---------------------------------------------------------------------------
+# a transformer block's training step
+# ---------------------------------------------------------------------------
+CAT_PACK_GROUP = 128
+ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}
+
+
+def _rows(t, name):
+    """(N, D, type) of a matrix of rows."""
+    if t.dim() != 2:
+        raise ValueError(f"{name} must have two dimensions, got {tuple(t.shape)}")
+    return t.shape[0], t.shape[1], _dt(t)
+
+
+def _act(act):
+    if act not in ACTIVATIONS:
+        raise ValueError(f"unknown activation {act!r}: one of {', '.join(ACTIVATIONS)}")
+    return ACTIVATIONS[act]
+
+
+def _empty_packed(N, D, device):
+    return (torch.empty((N, D), dtype=torch.int8, device=device),
+            torch.empty((N, (D + CAT_PACK_GROUP - 1) // CAT_PACK_GROUP), dtype=torch.float32, device=device))
+
+
+def _packed(packed, N, D):
+    """Pointers of a checkpoint (codes, scales), or two None."""
+    if packed is None:
+        return None, None
+    codes, scales = packed
+    return (_dev(codes, torch.int8, (N, D), "codes"),
+            _dev(scales, torch.float32, (N, (D + CAT_PACK_GROUP - 1) // CAT_PACK_GROUP), "scales"))
+
+
+def cat_pack8(x):
+    """The checkpoint of a matrix in 8 bits (cat_pack8): (codes, scales), codes of x's shape, a scale for every 128 channels
+    of a row."""
+    N, D, dt = _rows(x, "x")
+    px = _dev(x, name="x")
+    codes, scales = _empty_packed(N, D, x.device)
+    _check(load_library().cat_pack8(px, N, D, dt, codes.data_ptr(), scales.data_ptr(), _stream()))
+    return codes, scales
+
+
+def cat_unpack8(codes, scales, dtype=torch.float32):
+    """The values that a checkpoint stands for (cat_unpack8), as float32 or bfloat16."""
+    if codes.dim() != 2:
+        raise ValueError(f"codes must have two dimensions, got {tuple(codes.shape)}")
+    N, D = codes.shape
+    pc, ps = _packed((codes, scales), N, D)
+    x = torch.empty((N, D), dtype=dtype, device=codes.device)
+    _check(load_library().cat_unpack8(pc, ps, N, D, _dt(x), x.data_ptr(), _stream()))
+    return x
+
+
+def cat_layer_norm(x, weight=None, bias=None, eps=1e-5, want_stats=False, pack=False, out=None):
+    """Layer norm of every row (cat_layer_norm), weight and bias float32 or None.  Returns y; with ``want_stats`` (y, mean,
+    rstd); with ``pack`` (y, mean, rstd, packed), ``packed`` the checkpoint of x that the backward pass takes."""
+    N, D, dt = _rows(x, "x")
+    px, pw, pb = _dev(x, name="x"), _dev(weight, torch.float32, (D,), "weight"), _dev(bias, torch.float32, (D,), "bias")
+    if out is None:
+        out = torch.empty_like(x)
+    mean = rstd = packed = None
+    if want_stats or pack:
+        mean, rstd = (torch.empty((N,), dtype=torch.float32, device=x.device) for _ in range(2))
+    if pack:
+        packed = _empty_packed(N, D, x.device)
+    pc, ps = (None, None) if packed is None else (packed[0].data_ptr(), packed[1].data_ptr())
+    _check(load_library().cat_layer_norm(px, N, D, dt, pw, pb, float(eps), _dev(out, x.dtype, (N, D), "out"),
+                                         None if mean is None else mean.data_ptr(), None if rstd is None else rstd.data_ptr(),
+                                         pc, ps, _stream()))
+    return (out, mean, rstd, packed) if pack else (out, mean, rstd) if want_stats else out
+
+
+def cat_layer_norm_packed(packed, mean, rstd, weight=None, bias=None, dtype=torch.float32):
+    """Layer norm's output again, from the checkpoint of its input and the row statistics (cat_layer_norm_packed)."""
+    N, D = packed[0].shape
+    pc, ps = _packed(packed, N, D)
+    y = torch.empty((N, D), dtype=dtype, device=packed[0].device)
+    _check(load_library().cat_layer_norm_packed(pc, ps, _dev(mean, torch.float32, (N,), "mean"), _dev(rstd, torch.float32, (N,), "rstd"),
+                                                N, D, _dt(y), _dev(weight, torch.float32, (D,), "weight"),
+                                                _dev(bias, torch.float32, (D,), "bias"), y.data_ptr(), _stream()))
+    return y
+
+
+def cat_layer_norm_backward(dy, mean, rstd, weight=None, x=None, packed=None, residual_grad=None, want_params=True, workspace=None):
+    """Gradients of layer norm (cat_layer_norm_backward) from its input ``x`` or the checkpoint ``packed`` of it.
+    ``residual_grad`` is added to the input's gradient.  Returns (dx, dweight, dbias), the last two None without
+    ``want_params``."""
+    lib = load_library()
+    N, D, dt = _rows(dy, "dy")
+    pc, ps = _packed(packed, N, D)
+    args = (_dev(dy, name="dy"), _dev(x, dy.dtype, (N, D), "x"), pc, ps, _dev(mean, torch.float32, (N,), "mean"),
+            _dev(rstd, torch.float32, (N,), "rstd"), N, D, dt, _dev(weight, torch.float32, (D,), "weight"),
+            _dev(residual_grad, dy.dtype, (N, D), "residual_grad"))
+    dx = torch.empty_like(dy)
+    dw, db = (torch.empty((D,), dtype=torch.float32, device=dy.device) if want_params else None for _ in range(2))
+    if workspace is None:
+        workspace = _workspace(lib.cat_layer_norm_backward_workspace_bytes(N, D, dt), dy.device)
+    _check(lib.cat_layer_norm_backward(*args, dx.data_ptr(), None if dw is None else dw.data_ptr(), None if db is None else db.data_ptr(),
+                                       workspace.data_ptr(), workspace.numel(), _stream()))
+    return dx, dw, db
+
+
+def cat_linear(x, w, bias=None, act="none", residual=None, pack=False, out=None, workspace=None):
+    """act(x w^T + bias) + residual (cat_linear): x (M x K), w (N x K) and residual (M x N) of one type, bias float32.
+    Returns y; with ``pack`` (y, packed), ``packed`` the checkpoint of x w^T + bias."""
+    lib = load_library()
+    M, K, dt = _rows(x, "x")
+    N = w.shape[0]
+    px, pw = _dev(x, name="x"), _dev(w, x.dtype, (N, K), "w")
+    pb, pr = _dev(bias, torch.float32, (N,), "bias"), _dev(residual, x.dtype, (M, N), "residual")
+    act = _act(act)
+    if out is None:
+        out = torch.empty((M, N), dtype=x.dtype, device=x.device)
+    packed = _empty_packed(M, N, x.device) if pack else None
+    pc, ps = (packed[0].data_ptr(), packed[1].data_ptr()) if pack else (None, None)
+    if workspace is None:
+        workspace = _workspace(lib.cat_linear_workspace_bytes(M, N, K, dt), x.device)
+    _check(lib.cat_linear(px, pw, pb, pr, M, N, K, dt, act, _dev(out, x.dtype, (M, N), "out"), pc, ps, workspace.data_ptr(),
+                          workspace.numel(), _stream()))
+    return (out, packed) if pack else out
+
+
+def cat_linear_backward_input(dy, w, act="none", packed=None, out=None, workspace=None):
+    """Gradient of a product's input (cat_linear_backward_input): dy w, times the derivative of ``act`` at the values of
+    the checkpoint ``packed`` (M x K) if the input was act of those."""
+    lib = load_library()
+    M, N, dt = _rows(dy, "dy")
+    K = w.shape[-1]
+    pd, pw = _dev(dy, name="dy"), _dev(w, dy.dtype, (N, K), "w")
+    pc, ps = _packed(packed, M, K)
+    act = _act(act)
+    if out is None:
+        out = torch.empty((M, K), dtype=dy.dtype, device=dy.device)
+    if workspace is None:
+        workspace = _workspace(lib.cat_linear_backward_workspace_bytes(M, N, K, dt), dy.device)
+    _check(lib.cat_linear_backward_input(pd, pw, pc, ps, M, N, K, dt, act, _dev(out, dy.dtype, (M, K), "out"), workspace.data_ptr(),
+                                         workspace.numel(), _stream()))
+    return out
+
+
+def cat_linear_backward_weight(dy, x=None, packed=None, act="none", want_bias=True, out=None, workspace=None):
+    """Gradients of a product's weight and bias (cat_linear_backward_weight) from its input ``x``, or from the checkpoint
+    ``packed`` of the rows whose ``act`` the input was.  Returns (dw, dbias), dbias float32, None without ``want_bias``."""
+    lib = load_library()
+    M, N, dt = _rows(dy, "dy")
+    given = x if x is not None else packed[0] if packed is not None else None
+    if given is None or given.dim() != 2:
+        raise ValueError("give x or packed, a matrix of rows")
+    K = given.shape[1]
+    pd, px = _dev(dy, name="dy"), _dev(x, dy.dtype, (M, K), "x")
+    pc, ps = _packed(packed, M, K)
+    act = _act(act)
+    if out is None:
+        out = torch.empty((N, K), dtype=dy.dtype, device=dy.device)
+    db = torch.empty((N,), dtype=torch.float32, device=dy.device) if want_bias else None
+    if workspace is None:
+        workspace = _workspace(lib.cat_linear_backward_workspace_bytes(M, N, K, dt), dy.device)
+    _check(lib.cat_linear_backward_weight(pd, px, pc, ps, M, N, K, dt, act, _dev(out, dy.dtype, (N, K), "out"),
+                                          None if db is None else db.data_ptr(), workspace.data_ptr(), workspace.numel(), _stream()))
+    return out, db
+
+
+def cat_activation_backward(dy, packed, act):
+    """dy times the derivative of ``act`` at the values of a checkpoint (cat_activation_backward)."""
+    N, D, dt = _rows(dy, "dy")
+    pd = _dev(dy, name="dy")
+    pc, ps = _packed(packed, N, D)
+    dz = torch.empty_like(dy)
+    _check(load_library().cat_activation_backward(pd, pc, ps, N, D, dt, _act(act), dz.data_ptr(), _stream()))
+    return dz

@@ -1,0 +1,229 @@
+// What the operators of a transformer block's training step share (layer norm, product with epilogue, checkpoints in
+// 8 bits): vector access to rows of any length, reductions over some lanes, the format of a checkpoint, activations.
+#pragma once
+#include <math.h>
+
+#include <type_traits>
+
+#include "cat_common.h"
+
+namespace cat {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef short i16x8 __attribute__((ext_vector_type(8)));
+
+// Two floats to two bfloat16 values, ties to even; NaN and infinities stay what they are (one v_cvt_pk_bf16_f32).
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
+    const f32x2 v = {a, b};
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2));
+}
+__device__ __forceinline__ void st_round(float* p, float v) { *p = v; }
+__device__ __forceinline__ void st_round(bf16_t* p, float v) { *p = (bf16_t)pack_bf16(v, 0.f); }
+
+// 16 bytes of a row: 8 bfloat16 or 4 float entries.  Rows whose length is no whole number of such groups start anywhere
+// on an element's boundary; the memory system takes 16-byte accesses there, only their address has to be declared so.
+template <typename T>
+constexpr int kVec = (int)(16 / sizeof(T));
+template <typename T>
+struct __attribute__((packed, aligned(sizeof(T)))) Group16 {
+    uint32_t w[4];
+};
+template <typename T>
+__device__ __forceinline__ void ld_group(const T* p, float (&v)[kVec<T>]) {
+    const Group16<T> g = *(const Group16<T>*)p;
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int e = 0; e < 4; e++) v[e] = __uint_as_float(g.w[e]);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; e++) {
+            v[2 * e] = __uint_as_float(g.w[e] << 16);
+            v[2 * e + 1] = __uint_as_float(g.w[e] & 0xFFFF0000u);
+        }
+    }
+}
+template <typename T>
+__device__ __forceinline__ void st_group(T* p, const float (&v)[kVec<T>]) {
+    Group16<T> g;
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int e = 0; e < 4; e++) g.w[e] = __float_as_uint(v[e]);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; e++) g.w[e] = pack_bf16(v[2 * e], v[2 * e + 1]);
+    }
+    *(Group16<T>*)p = g;
+}
+// the entries [j, j + kVec) of a row of D entries, zero behind its end
+template <typename T>
+__device__ __forceinline__ void ld_group_to(const T* row, int64_t j, int64_t D, float (&v)[kVec<T>]) {
+    constexpr int V = kVec<T>;
+    if (j + V <= D) {
+        ld_group(row + j, v);
+    } else {
+#pragma unroll
+        for (int e = 0; e < V; e++) v[e] = j + e < D ? ld_elem(row + j + e) : 0.f;
+    }
+}
+template <typename T>
+__device__ __forceinline__ void st_group_to(T* row, int64_t j, int64_t D, const float (&v)[kVec<T>]) {
+    constexpr int V = kVec<T>;
+    if (j + V <= D) {
+        st_group(row + j, v);
+    } else {
+#pragma unroll
+        for (int e = 0; e < V; e++)
+            if (j + e < D) st_round(row + j + e, v[e]);
+    }
+}
+// V parameters from index j on (nullptr: `other`); the array itself starts on a 16-byte boundary and j is a multiple of V
+template <int V>
+__device__ __forceinline__ void ld_params(const float* p, int64_t j, int64_t D, float other, float (&v)[V]) {
+    if (p == nullptr) {
+#pragma unroll
+        for (int e = 0; e < V; e++) v[e] = other;
+    } else if (j + V <= D) {
+#pragma unroll
+        for (int e = 0; e < V; e += 4) {
+            const float4 q = *(const float4*)(p + j + e);
+            v[e] = q.x, v[e + 1] = q.y, v[e + 2] = q.z, v[e + 3] = q.w;
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < V; e++) v[e] = j + e < D ? p[j + e] : other;
+    }
+}
+
+// ---- reductions over L = 8, 16, 32 or 64 neighbouring lanes, the result in each of them ----
+// Up to 16 lanes as permutations inside a row of 16 lanes, beyond that as exchanges between those rows.  All 64 lanes of
+// the wave must be active.
+template <int CTRL>
+__device__ __forceinline__ float dpp_f32(float v) {
+    return __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), CTRL, 0xF, 0xF, true));
+}
+template <int L>
+__device__ __forceinline__ float lanes_sum(float v) {
+    v += dpp_f32<0xB1>(v);                                    // quad_perm [1, 0, 3, 2]
+    v += dpp_f32<0x4E>(v);                                    // quad_perm [2, 3, 0, 1]
+    if constexpr (L >= 8) v += dpp_f32<0x141>(v);             // row_half_mirror
+    if constexpr (L >= 16) v += dpp_f32<0x140>(v);            // row_mirror
+    if constexpr (L >= 32) v += __shfl_xor(v, 16, kWave);
+    if constexpr (L >= 64) v += __shfl_xor(v, 32, kWave);
+    return v;
+}
+// the larger one; a NaN on either side stays (v_max drops it)
+__device__ __forceinline__ float max_nan(float a, float b) { return a >= b || a != a ? a : b; }
+template <int L>
+__device__ __forceinline__ float lanes_max(float v) {
+    v = max_nan(v, dpp_f32<0xB1>(v));
+    v = max_nan(v, dpp_f32<0x4E>(v));
+    if constexpr (L >= 8) v = max_nan(v, dpp_f32<0x141>(v));
+    if constexpr (L >= 16) v = max_nan(v, dpp_f32<0x140>(v));
+    if constexpr (L >= 32) v = max_nan(v, __shfl_xor(v, 16, kWave));
+    return v;
+}
+
+// ---- checkpoints in 8 bits ----
+// Groups of 128 consecutive channels of a row share a scale s = a / 127 with a the group's largest magnitude; a channel's
+// code is x * (127 / a), rounded to the nearest integer (ties to even), its value code * s.  Both quotients are correctly
+// rounded, so a group's codes do not depend on which kernel wrote them.  a < 2^-100 (where 127 / a comes near the largest
+// float): zeros.  A NaN or an infinity makes the group's scale one, and every value of the group NaN (0 * inf too).
+constexpr int kPackGroup = CAT_PACK_GROUP;
+struct PackScale {
+    float up, step;
+};
+__device__ __forceinline__ PackScale pack_scale(float amax) {
+    PackScale s;
+    const bool held = !(amax < 0x1p-100f);
+    s.up = held ? __fdiv_rn(127.f, amax) : 0.f;
+    s.step = held ? __fdiv_rn(amax, 127.f) : 0.f;
+    return s;
+}
+// (a NaN converts to 0; values beyond the range cannot occur: |x| * (127 / a) rounds to at most 127)
+__device__ __forceinline__ int pack_code(float x, float up) { return (int)__builtin_rintf(x * up); }
+__device__ __forceinline__ uint32_t pack_codes4(const float* v, float up) {
+    return ((uint32_t)pack_code(v[0], up) & 0xFFu) | (((uint32_t)pack_code(v[1], up) & 0xFFu) << 8) |
+           (((uint32_t)pack_code(v[2], up) & 0xFFu) << 16) | ((uint32_t)pack_code(v[3], up) << 24);
+}
+__device__ __forceinline__ float code_value(uint32_t w, int e) { return (float)(int8_t)(w >> (8 * e)); }
+struct __attribute__((packed, aligned(1))) Codes4 {
+    uint32_t w[1];
+};
+struct __attribute__((packed, aligned(1))) Codes8 {
+    uint32_t w[2];
+};
+// V codes from index j of a row on
+template <int V>
+__device__ __forceinline__ void st_codes(int8_t* row, int64_t j, int64_t D, const float (&v)[V], float up) {
+    std::conditional_t<V == 8, Codes8, Codes4> c;
+#pragma unroll
+    for (int e = 0; e < V / 4; e++) c.w[e] = pack_codes4(v + 4 * e, up);
+    if (j + V <= D) {
+        *(decltype(c)*)(row + j) = c;
+    } else {
+#pragma unroll
+        for (int e = 0; e < V; e++)
+            if (j + e < D) row[j + e] = (int8_t)(c.w[e / 4] >> (8 * (e % 4)));
+    }
+}
+// V values from index j of a row on, zero behind its end
+template <int V>
+__device__ __forceinline__ void ld_codes(const int8_t* row, int64_t j, int64_t D, float step, float (&v)[V]) {
+    if (j + V <= D) {
+        const std::conditional_t<V == 8, Codes8, Codes4> c = *(const std::conditional_t<V == 8, Codes8, Codes4>*)(row + j);
+#pragma unroll
+        for (int e = 0; e < V; e++) v[e] = code_value(c.w[e / 4], e % 4) * step;
+    } else {
+#pragma unroll
+        for (int e = 0; e < V; e++) v[e] = j + e < D ? (float)row[j + e] * step : 0.f;
+    }
+}
+
+// ---- activations ----
+// In fp32 throughout.  The saturated ends come out of exp and erf by themselves (exp -> inf gives 1 / inf = 0); a NaN stays.
+__device__ __forceinline__ float logistic(float z) { return __fdividef(1.f, 1.f + __expf(-z)); }
+constexpr float kInvSqrt2 = 0.70710678118654752f, kInvSqrt2Pi = 0.39894228040143268f;
+constexpr float kTanhIn = 0.79788456080286536f, kTanhCube = 0.044715f;
+// gelu with tanh: 0.5 z (1 + tanh u) = z * logistic(2 u), u = sqrt(2 / pi) (z + 0.044715 z^3)
+__device__ __forceinline__ float tanh_arg2(float z) { return 2.f * kTanhIn * z * fmaf(kTanhCube * z, z, 1.f); }
+__device__ __forceinline__ float act_value(float z, int act) {
+    switch (act) {
+        case CAT_ACT_RELU: return z > 0.f ? z : (z != z ? z : 0.f);
+        case CAT_ACT_GELU: return 0.5f * z * (1.f + erff(z * kInvSqrt2));
+        case CAT_ACT_GELU_TANH: return z * logistic(tanh_arg2(z));
+        case CAT_ACT_SILU: return z * logistic(z);
+        default: return z;
+    }
+}
+__device__ __forceinline__ float act_grad(float z, int act) {
+    switch (act) {
+        case CAT_ACT_RELU: return z > 0.f ? 1.f : (z != z ? z : 0.f);
+        case CAT_ACT_GELU: return fmaf(z * kInvSqrt2Pi, __expf(-0.5f * z * z), 0.5f * (1.f + erff(z * kInvSqrt2)));
+        case CAT_ACT_GELU_TANH: {
+            // (beyond |z| = 32 the factor p (1 - p) is zero in fp32, and z * z must not turn it into 0 * inf)
+            const float p = logistic(tanh_arg2(z)), c = fminf(fmaxf(z, -32.f), 32.f);
+            return fmaf(c * p * (1.f - p), 2.f * kTanhIn * fmaf(3.f * kTanhCube * c, c, 1.f), p);
+        }
+        case CAT_ACT_SILU: {
+            const float p = logistic(z);
+            return p * fmaf(z, 1.f - p, 1.f);
+        }
+        default: return 1.f;
+    }
+}
+
+// ---- checks of arguments (cat_pack.hip); `who` is the entry point's name ----
+cat_status check_rows(const char* who, int64_t N, int64_t D, cat_dtype dt);  // 0 <= N, 1 <= D, known type
+cat_status check_ptr(const char* who, const char* name, const void* p, bool needed);  // 16-byte aligned, and there if needed
+cat_status check_act(const char* who, int act);
+cat_status check_workspace(const char* who, const void* ws, size_t have, size_t need);
+
+}  // namespace cat
+
+#define CAT_TRY(expr)                       \
+    do {                                    \
+        const cat_status _s = (expr);       \
+        if (_s != CAT_OK) return _s;        \
+    } while (0)
