@@ -222,6 +222,11 @@ cat_status check_workspace(const char* who, const void* ws, size_t have, size_t 
 
 }  // namespace cat
 
+// out[c] = sum over P parts of parts[p][c], c < n: to `lo` below `split`, to `hi` from there on (each nullable); cat_pack.hip
+namespace cat {
+cat_status launch_sum_parts(const float* parts, int P, int64_t n, int64_t split, float* lo, float* hi, hipStream_t st);
+}
+
 #define CAT_TRY(expr)                       \
     do {                                    \
         const cat_status _s = (expr);       \

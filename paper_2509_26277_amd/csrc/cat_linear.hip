@@ -161,18 +161,6 @@ __global__ __launch_bounds__(256) void k_column_sums(const T* __restrict__ x, in
     for (int e = 0; e < V; e++)
         if (j + e < N) parts[(int64_t)blockIdx.y * N + j + e] = (s[0][e][lane] + s[1][e][lane]) + (s[2][e][lane] + s[3][e][lane]);
 }
-__global__ __launch_bounds__(256) void k_sum_parts(const float* __restrict__ parts, int P, int64_t N, float* __restrict__ out) {
-    __shared__ float s[4][kWave];
-    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
-    const int64_t c = (int64_t)blockIdx.x * kWave + lane;
-    float t = 0.f;
-    if (c < N)
-        for (int p = wave; p < P; p += 4) t += parts[(int64_t)p * N + c];
-    s[wave][lane] = t;
-    __syncthreads();
-    if (wave == 0 && c < N) out[c] = (s[0][lane] + s[1][lane]) + (s[2][lane] + s[3][lane]);
-}
-
 // ---- plans ----
 constexpr int64_t kMaxBlocks = 1 << 22;
 unsigned blocks_of(int64_t threads) {
@@ -426,8 +414,7 @@ cat_status cat_linear_backward_weight(const void* dy, const void* x, const int8_
         else
             hipLaunchKernelGGL(k_column_sums<bf16_t>, grid, dim3(256), 0, st, (const bf16_t*)dy, M, N, pl.sum_rows, parts);
         CAT_LAUNCH_CHECK("k_column_sums");
-        hipLaunchKernelGGL(k_sum_parts, dim3((unsigned)((N + 63) / 64)), dim3(256), 0, st, parts, pl.sum_parts, N, dbias);
-        CAT_LAUNCH_CHECK("k_sum_parts");
+        CAT_TRY(launch_sum_parts(parts, pl.sum_parts, N, N, dbias, nullptr, st));
     }
     if (pl.lay_q) CAT_TRY(lay_out(dt, dy, nullptr, nullptr, 0, M, N, pl.ldq, ws + pl.at_q, st));
     if (pl.lay_p) CAT_TRY(lay_out(dt, x, codes, scales, (int)act, M, K, pl.ldp, ws + pl.at_p, st));

@@ -15,58 +15,125 @@ namespace cat {
 namespace {
 
 constexpr int kNormThreads = 256;
-constexpr int64_t kNormMaxBlocks = 1 << 22;  // further rows by stride
+constexpr int64_t kNormMaxBlocks = 1 << 22;  // long rows: further ones by stride
 
-// the sum over the TPR threads of a row (TPR = 256: the workgroup; `slot` alternates, so that one barrier a sum is enough)
-template <int TPR>
-__device__ __forceinline__ float row_sum(float v, float (*slots)[4], int& slot) {
-    if constexpr (TPR <= kWave) {
-        return lanes_sum<TPR>(v);
-    } else {
-        v = lanes_sum<kWave>(v);
-        if ((threadIdx.x & (kWave - 1)) == 0) slots[slot][threadIdx.x / kWave] = v;
+// A lane's 16-byte group of a row as it lies in memory: the next row's are requested while the present one's are worked on,
+// so they have to be few registers.
+template <typename T, bool FROM8>
+struct Part {
+    uint32_t w[FROM8 ? kVec<T> / 4 : 4];
+    float step;
+    // entries [j, j + V) of a row of D entries, zero behind its end
+    __device__ __forceinline__ void load(const T* x, const int8_t* codes, const float* scales, int64_t row, int64_t j, int64_t D, int64_t G) {
+        constexpr int V = kVec<T>;
+        if constexpr (FROM8) {
+            const int8_t* c = codes + row * D + j;
+            step = j < D ? scales[row * G + j / kPackGroup] : 0.f;
+            if (j + V <= D) {
+                const std::conditional_t<V == 8, Codes8, Codes4> q = *(const std::conditional_t<V == 8, Codes8, Codes4>*)c;
+#pragma unroll
+                for (int e = 0; e < V / 4; e++) w[e] = q.w[e];
+            } else {
+#pragma unroll
+                for (int e = 0; e < V / 4; e++) w[e] = 0;
+#pragma unroll
+                for (int e = 0; e < V; e++)
+                    if (j + e < D) w[e / 4] |= (uint32_t)(uint8_t)c[e] << (8 * (e % 4));
+            }
+        } else {
+            const T* c = x + row * D + j;
+            if (j + V <= D) {
+                const Group16<T> q = *(const Group16<T>*)c;
+#pragma unroll
+                for (int e = 0; e < 4; e++) w[e] = q.w[e];
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; e++) w[e] = 0;
+#pragma unroll
+                for (int e = 0; e < V; e++)
+                    if (j + e < D) {
+                        if constexpr (sizeof(T) == 4)
+                            w[e] = __float_as_uint(c[e]);
+                        else
+                            w[e / 2] |= (uint32_t)c[e] << (16 * (e % 2));
+                    }
+            }
+        }
+    }
+    __device__ __forceinline__ float at(int e) const {
+        if constexpr (FROM8) return code_value(w[e / 4], e % 4) * step;
+        else if constexpr (sizeof(T) == 4) return __uint_as_float(w[e]);
+        else return __uint_as_float(e % 2 ? w[e / 2] & 0xFFFF0000u : w[e / 2] << 16);
+    }
+};
+
+// Sums over the TPR threads of a row, Q of them at a time.  TPR > 64: over the workgroup's waves by LDS; `slot` alternates, so
+// that one barrier a time is enough.
+template <int TPR, int Q>
+__device__ __forceinline__ void row_sums(float (&v)[Q], float (*slots)[2][8], int& slot) {
+#pragma unroll
+    for (int q = 0; q < Q; q++) v[q] = lanes_sum<(TPR < kWave ? TPR : kWave)>(v[q]);
+    if constexpr (TPR > kWave) {
+        if ((threadIdx.x & (kWave - 1)) == 0)
+#pragma unroll
+            for (int q = 0; q < Q; q++) slots[slot][q][threadIdx.x / kWave] = v[q];
         __syncthreads();
-        v = (slots[slot][0] + slots[slot][1]) + (slots[slot][2] + slots[slot][3]);
-        slot = slot == 2 ? 0 : slot + 1;
-        return v;
+#pragma unroll
+        for (int q = 0; q < Q; q++) {
+            const float* s = slots[slot][q];
+            v[q] = (s[0] + s[1]) + (s[2] + s[3]);
+            if constexpr (TPR > 256) v[q] += (s[4] + s[5]) + (s[6] + s[7]);
+        }
+        slot ^= 1;
     }
 }
+template <int TPR>
+constexpr int kThreads = TPR > kNormThreads ? TPR : kNormThreads;
 
 // ---- forward ----
-// PACK: also the checkpoint of x.  FROM8: x is a checkpoint, and mean and rstd are given.
+// PACK: also the checkpoint of x.  FROM8: x is a checkpoint, and mean and rstd are given.  Workgroups go through the rows
+// by stride: weight and bias stay in registers, and a row is requested while the one before it is worked on.
 template <typename T, int TPR, int VPL, bool PACK, bool FROM8>
-__global__ __launch_bounds__(kNormThreads) void k_norm(const T* __restrict__ x, int64_t N, int64_t D, const float* __restrict__ weight,
-                                                       const float* __restrict__ bias, float eps, T* __restrict__ y, float* __restrict__ mean,
-                                                       float* __restrict__ rstd, int8_t* __restrict__ codes, float* __restrict__ scales) {
-    constexpr int V = kVec<T>, RPB = kNormThreads / TPR, GL = kPackGroup / V;  // GL: neighbouring lanes that share a scale
-    __shared__ float slots[3][4];
+__global__ __launch_bounds__(kThreads<TPR>) void k_norm(const T* __restrict__ x, int64_t N, int64_t D, const float* __restrict__ weight,
+                                                        const float* __restrict__ bias, float eps, T* __restrict__ y, float* __restrict__ mean,
+                                                        float* __restrict__ rstd, int8_t* __restrict__ codes, float* __restrict__ scales) {
+    constexpr int V = kVec<T>, RPB = kThreads<TPR> / TPR, GL = kPackGroup / V;  // GL: neighbouring lanes that share a scale
+    __shared__ float slots[2][2][8];
     int slot = 0;
     const int sub = threadIdx.x % TPR;
-    const int64_t G = (D + kPackGroup - 1) / kPackGroup;
-    for (int64_t r0 = (int64_t)blockIdx.x * RPB; r0 < N; r0 += (int64_t)gridDim.x * RPB) {
-        const int64_t own_row = r0 + threadIdx.x / TPR;
+    const int64_t G = (D + kPackGroup - 1) / kPackGroup, stride = (int64_t)gridDim.x * RPB;
+    int64_t own_row = (int64_t)blockIdx.x * RPB + threadIdx.x / TPR;
+    Part<T, FROM8> next[VPL];
+#pragma unroll
+    for (int k = 0; k < VPL; k++) next[k].load(x, codes, scales, own_row < N ? own_row : N - 1, ((int64_t)k * TPR + sub) * V, D, G);
+    float w[VPL][V], b[VPL][V];
+#pragma unroll
+    for (int k = 0; k < VPL; k++) {
+        ld_params<V>(weight, ((int64_t)k * TPR + sub) * V, D, 1.f, w[k]);
+        ld_params<V>(bias, ((int64_t)k * TPR + sub) * V, D, 0.f, b[k]);
+    }
+    for (int64_t r0 = (int64_t)blockIdx.x * RPB; r0 < N; r0 += stride, own_row += stride) {
         const bool mine = own_row < N;
         const int64_t row = mine ? own_row : N - 1;
-        float v[VPL][V];
+        Part<T, FROM8> v[VPL];
 #pragma unroll
-        for (int k = 0; k < VPL; k++) {
-            const int64_t j = ((int64_t)k * TPR + sub) * V;
-            if constexpr (FROM8)
-                ld_codes<V>(codes + row * D, j, D, j < D ? scales[row * G + j / kPackGroup] : 0.f, v[k]);
-            else
-                ld_group_to(x + row * D, j, D, v[k]);
+        for (int k = 0; k < VPL; k++) v[k] = next[k];
+        if (r0 + stride < N) {
+            const int64_t r = own_row + stride < N ? own_row + stride : N - 1;
+#pragma unroll
+            for (int k = 0; k < VPL; k++) next[k].load(x, codes, scales, r, ((int64_t)k * TPR + sub) * V, D, G);
         }
         if constexpr (PACK) {
 #pragma unroll
             for (int k = 0; k < VPL; k++) {
                 const int64_t j = ((int64_t)k * TPR + sub) * V;
-                float a = 0.f;
+                float a = 0.f, f[V];
 #pragma unroll
-                for (int e = 0; e < V; e++) a = max_nan(a, fabsf(v[k][e]));
+                for (int e = 0; e < V; e++) f[e] = v[k].at(e), a = max_nan(a, fabsf(f[e]));
                 a = lanes_max<(TPR < GL ? TPR : GL)>(a);
                 const PackScale s = pack_scale(a);
                 if (mine && j < D) {
-                    st_codes<V>(codes + row * D, j, D, v[k], s.up);
+                    st_codes<V>(codes + row * D, j, D, f, s.up);
                     if (j % kPackGroup == 0) scales[row * G + j / kPackGroup] = s.step;
                 }
             }
@@ -75,23 +142,25 @@ __global__ __launch_bounds__(kNormThreads) void k_norm(const T* __restrict__ x, 
         if constexpr (FROM8) {
             mu = mean[row], rs = rstd[row];
         } else {
-            float s = 0.f;
+            float s[1] = {0.f};
 #pragma unroll
             for (int k = 0; k < VPL; k++)
 #pragma unroll
-                for (int e = 0; e < V; e++) s += v[k][e];
-            mu = row_sum<TPR>(s, slots, slot) / (float)D;
-            float q = 0.f;
+                for (int e = 0; e < V; e++) s[0] += v[k].at(e);
+            row_sums<TPR>(s, slots, slot);
+            mu = s[0] / (float)D;
+            float q[1] = {0.f};
 #pragma unroll
             for (int k = 0; k < VPL; k++) {
                 const int64_t j = ((int64_t)k * TPR + sub) * V;
 #pragma unroll
                 for (int e = 0; e < V; e++) {
-                    const float c = v[k][e] - mu;
-                    if (j + e < D) q = fmaf(c, c, q);
+                    const float c = v[k].at(e) - mu;
+                    if (j + e < D) q[0] = fmaf(c, c, q[0]);
                 }
             }
-            rs = 1.f / sqrtf(row_sum<TPR>(q, slots, slot) / (float)D + eps);
+            row_sums<TPR>(q, slots, slot);
+            rs = 1.f / sqrtf(q[0] / (float)D + eps);
             if (mine && sub == 0) {
                 if (mean) mean[row] = mu;
                 if (rstd) rstd[row] = rs;
@@ -102,11 +171,9 @@ __global__ __launch_bounds__(kNormThreads) void k_norm(const T* __restrict__ x, 
         for (int k = 0; k < VPL; k++) {
             const int64_t j = ((int64_t)k * TPR + sub) * V;
             if (j >= D) continue;
-            float w[V], b[V], o[V];
-            ld_params<V>(weight, j, D, 1.f, w);
-            ld_params<V>(bias, j, D, 0.f, b);
+            float o[V];
 #pragma unroll
-            for (int e = 0; e < V; e++) o[e] = fmaf((v[k][e] - mu) * rs, w[e], b[e]);
+            for (int e = 0; e < V; e++) o[e] = fmaf((v[k].at(e) - mu) * rs, w[k][e], b[k][e]);
             st_group_to(y + row * D, j, D, o);
         }
     }
@@ -119,7 +186,7 @@ __global__ __launch_bounds__(kNormThreads) void k_norm_long(const T* __restrict_
                                                             float* __restrict__ mean, float* __restrict__ rstd,
                                                             const int8_t* __restrict__ codes, const float* __restrict__ scales) {
     constexpr int V = kVec<T>;
-    __shared__ float slots[3][4];
+    __shared__ float slots[2][2][8];
     int slot = 0;
     const int64_t G = (D + kPackGroup - 1) / kPackGroup;
     for (int64_t row = blockIdx.x; row < N; row += gridDim.x) {
@@ -141,7 +208,9 @@ __global__ __launch_bounds__(kNormThreads) void k_norm_long(const T* __restrict_
 #pragma unroll
                 for (int e = 0; e < V; e++) s += v[e];
             }
-            mu = row_sum<kNormThreads>(s, slots, slot) / (float)D;
+            float t[1] = {s};
+            row_sums<kNormThreads>(t, slots, slot);
+            mu = t[0] / (float)D;
             for (int64_t j = (int64_t)threadIdx.x * V; j < D; j += kNormThreads * V) {
                 float v[V];
                 load(j, v);
@@ -149,7 +218,9 @@ __global__ __launch_bounds__(kNormThreads) void k_norm_long(const T* __restrict_
                 for (int e = 0; e < V; e++)
                     if (j + e < D) q = fmaf(v[e] - mu, v[e] - mu, q);
             }
-            rs = 1.f / sqrtf(row_sum<kNormThreads>(q, slots, slot) / (float)D + eps);
+            t[0] = q;
+            row_sums<kNormThreads>(t, slots, slot);
+            rs = 1.f / sqrtf(t[0] / (float)D + eps);
             if (threadIdx.x == 0) {
                 if (mean) mean[row] = mu;
                 if (rstd) rstd[row] = rs;
@@ -168,22 +239,37 @@ __global__ __launch_bounds__(kNormThreads) void k_norm_long(const T* __restrict_
 }
 
 // ---- backward ----
-// A workgroup goes through its rows by stride and keeps its threads' channels of dw and db in registers; at its end the
-// rows' slots (RPB of them share the channels) are added in LDS in a fixed order and written as the workgroup's part, which
-// k_norm_params adds up: no atomics, the same bits on every run.
+// A workgroup goes through its rows by stride, a row ahead as above, and keeps its threads' channels of dw and db in registers;
+// at its end the rows' slots (RPB of them share the channels) are added in LDS in a fixed order and written as the workgroup's
+// part, which launch_sum_parts adds up: no atomics, the same bits on every run.
 template <typename T, int TPR, int VPL, bool FROM8>
-__global__ __launch_bounds__(kNormThreads) void k_norm_backward(const T* __restrict__ dy, const T* __restrict__ x,
-                                                                const int8_t* __restrict__ codes, const float* __restrict__ scales,
-                                                                const float* __restrict__ mean, const float* __restrict__ rstd, int64_t N,
-                                                                int64_t D, const float* __restrict__ weight, const T* __restrict__ radd,
-                                                                T* __restrict__ dx, float* __restrict__ parts) {
-    constexpr int V = kVec<T>, RPB = kNormThreads / TPR;
-    __shared__ float slots[3][4];
-    __shared__ float sums[RPB > 1 ? kNormThreads * V : 1];
+__global__ __launch_bounds__(kThreads<TPR>) void k_norm_backward(const T* __restrict__ dy, const T* __restrict__ x,
+                                                                 const int8_t* __restrict__ codes, const float* __restrict__ scales,
+                                                                 const float* __restrict__ mean, const float* __restrict__ rstd, int64_t N,
+                                                                 int64_t D, const float* __restrict__ weight, const T* __restrict__ radd,
+                                                                 T* __restrict__ dx, float* __restrict__ parts) {
+    constexpr int V = kVec<T>, RPB = kThreads<TPR> / TPR;
+    __shared__ float slots[2][2][8];
+    __shared__ float sums[RPB > 1 ? kThreads<TPR> * V : 1];
     int slot = 0;
     const int sub = threadIdx.x % TPR;
-    const int64_t G = (D + kPackGroup - 1) / kPackGroup;
+    const int64_t G = (D + kPackGroup - 1) / kPackGroup, stride = (int64_t)gridDim.x * RPB;
     const float inv = 1.f / (float)D;
+    int64_t own_row = (int64_t)blockIdx.x * RPB + threadIdx.x / TPR;
+    Part<T, FROM8> next_x[VPL];
+    Part<T, false> next_g[VPL], next_a[VPL];
+    float next_mu, next_rs;
+    auto request = [&](int64_t r) {
+#pragma unroll
+        for (int k = 0; k < VPL; k++) {
+            const int64_t j = ((int64_t)k * TPR + sub) * V;
+            next_x[k].load(x, codes, scales, r, j, D, G);
+            next_g[k].load(dy, nullptr, nullptr, r, j, D, G);  // (zero behind the row's end, so that xhat there does not count)
+            if (radd) next_a[k].load(radd, nullptr, nullptr, r, j, D, G);
+        }
+        next_mu = mean[r], next_rs = rstd[r];
+    };
+    request(own_row < N ? own_row : N - 1);
     float aw[VPL][V], ab[VPL][V], w[VPL][V];
 #pragma unroll
     for (int k = 0; k < VPL; k++) {
@@ -191,50 +277,39 @@ __global__ __launch_bounds__(kNormThreads) void k_norm_backward(const T* __restr
 #pragma unroll
         for (int e = 0; e < V; e++) aw[k][e] = ab[k][e] = 0.f;
     }
-    for (int64_t r0 = (int64_t)blockIdx.x * RPB; r0 < N; r0 += (int64_t)gridDim.x * RPB) {
-        const int64_t own_row = r0 + threadIdx.x / TPR;
+    for (int64_t r0 = (int64_t)blockIdx.x * RPB; r0 < N; r0 += stride, own_row += stride) {
         const bool mine = own_row < N;
-        const int64_t row = mine ? own_row : N - 1;
-        const float mu = mean[row], rs = rstd[row];
-        float h[VPL][V], g[VPL][V];
-        float s1 = 0.f, s2 = 0.f;
+        Part<T, FROM8> px[VPL];
+        Part<T, false> pg[VPL], pa[VPL];
+        const float mu = next_mu, rs = next_rs;
 #pragma unroll
-        for (int k = 0; k < VPL; k++) {
-            const int64_t j = ((int64_t)k * TPR + sub) * V;
-            if constexpr (FROM8)
-                ld_codes<V>(codes + row * D, j, D, j < D ? scales[row * G + j / kPackGroup] : 0.f, h[k]);
-            else
-                ld_group_to(x + row * D, j, D, h[k]);
-            ld_group_to(dy + row * D, j, D, g[k]);  // (zero behind the row's end, so that xhat there does not count)
-        }
+        for (int k = 0; k < VPL; k++) px[k] = next_x[k], pg[k] = next_g[k], pa[k] = next_a[k];
+        if (r0 + stride < N) request(own_row + stride < N ? own_row + stride : N - 1);
+        float s[2] = {0.f, 0.f};
 #pragma unroll
         for (int k = 0; k < VPL; k++)
 #pragma unroll
             for (int e = 0; e < V; e++) {
-                h[k][e] = (h[k][e] - mu) * rs;
-                const float d = mine ? g[k][e] : 0.f;
+                const float h = (px[k].at(e) - mu) * rs, d = mine ? pg[k].at(e) : 0.f, g = d * w[k][e];
                 ab[k][e] += d;
-                aw[k][e] = fmaf(d, mine ? h[k][e] : 0.f, aw[k][e]);
-                g[k][e] *= w[k][e];
-                s1 += g[k][e];
-                s2 = fmaf(g[k][e], h[k][e], s2);
+                aw[k][e] = fmaf(d, mine ? h : 0.f, aw[k][e]);
+                s[0] += g;
+                s[1] = fmaf(g, h, s[1]);
             }
-        s1 = row_sum<TPR>(s1, slots, slot) * inv;
-        s2 = row_sum<TPR>(s2, slots, slot) * inv;
+        row_sums<TPR>(s, slots, slot);
+        const float s1 = s[0] * inv, s2 = s[1] * inv;
         if (!mine) continue;
 #pragma unroll
         for (int k = 0; k < VPL; k++) {
             const int64_t j = ((int64_t)k * TPR + sub) * V;
             if (j >= D) continue;
             float o[V];
-            if (radd)
-                ld_group_to(radd + row * D, j, D, o);
-            else
 #pragma unroll
-                for (int e = 0; e < V; e++) o[e] = 0.f;
-#pragma unroll
-            for (int e = 0; e < V; e++) o[e] = fmaf(rs, g[k][e] - s1 - h[k][e] * s2, o[e]);
-            st_group_to(dx + row * D, j, D, o);
+            for (int e = 0; e < V; e++) {
+                const float h = (px[k].at(e) - mu) * rs, g = pg[k].at(e) * w[k][e];
+                o[e] = fmaf(rs, g - s1 - h * s2, radd ? pa[k].at(e) : 0.f);
+            }
+            st_group_to(dx + own_row * D, j, D, o);
         }
     }
     if (!parts) return;
@@ -276,12 +351,12 @@ __global__ __launch_bounds__(kNormThreads) void k_norm_backward_long(const T* __
                                                                      int64_t D, const float* __restrict__ weight, const T* __restrict__ radd,
                                                                      T* __restrict__ dx) {
     constexpr int V = kVec<T>;
-    __shared__ float slots[3][4];
+    __shared__ float slots[2][2][8];
     int slot = 0;
     const int64_t G = (D + kPackGroup - 1) / kPackGroup;
     for (int64_t row = blockIdx.x; row < N; row += gridDim.x) {
         const float mu = mean[row], rs = rstd[row];
-        float s1 = 0.f, s2 = 0.f;
+        float s[2] = {0.f, 0.f};
         auto load = [&](int64_t j, float (&h)[V], float (&g)[V]) {
             float w[V];
             if constexpr (FROM8)
@@ -297,10 +372,10 @@ __global__ __launch_bounds__(kNormThreads) void k_norm_backward_long(const T* __
             float h[V], g[V];
             load(j, h, g);
 #pragma unroll
-            for (int e = 0; e < V; e++) s1 += g[e], s2 = fmaf(g[e], h[e], s2);
+            for (int e = 0; e < V; e++) s[0] += g[e], s[1] = fmaf(g[e], h[e], s[1]);
         }
-        s1 = row_sum<kNormThreads>(s1, slots, slot) / (float)D;
-        s2 = row_sum<kNormThreads>(s2, slots, slot) / (float)D;
+        row_sums<kNormThreads>(s, slots, slot);
+        const float s1 = s[0] / (float)D, s2 = s[1] / (float)D;
         for (int64_t j = (int64_t)threadIdx.x * V; j < D; j += kNormThreads * V) {
             float h[V], g[V], o[V];
             load(j, h, g);
@@ -339,112 +414,101 @@ __global__ __launch_bounds__(kNormThreads) void k_norm_columns(const T* __restri
     parts[(int64_t)blockIdx.y * 2 * D + D + j] = ab;
 }
 
-// dweight and dbias from the workgroups' parts (P x 2 x D): 64 channels a workgroup, four waves share the parts, a fixed order
-__global__ __launch_bounds__(256) void k_norm_params(const float* __restrict__ parts, int P, int64_t D, float* __restrict__ dweight,
-                                                     float* __restrict__ dbias) {
-    __shared__ float s[4][kWave];
-    const int lane = threadIdx.x & (kWave - 1), wv = threadIdx.x / kWave;
-    const int64_t c = (int64_t)blockIdx.x * kWave + lane;  // of 2 D
-    float t = 0.f;
-    if (c < 2 * D)
-        for (int p = wv; p < P; p += 4) t += parts[(int64_t)p * 2 * D + c];
-    s[wv][lane] = t;
-    __syncthreads();
-    if (wv || c >= 2 * D) return;
-    t = (s[0][lane] + s[1][lane]) + (s[2][lane] + s[3][lane]);
-    if (c < D) {
-        if (dweight) dweight[c] = t;
-    } else if (dbias) {
-        dbias[c - D] = t;
-    }
-}
-
 // ---- the instance for a row length ----
-// TPR threads with VPL groups each hold a row; 0 threads: the kernels for long rows.
+// TPR threads with VPL 16-byte groups each hold a row; 0 threads: the kernels for long rows.  A wave takes up to 32 entries
+// a lane in the forward pass and up to 16 in the backward pass, whose sums and rows ahead need more registers.
 struct NormShape {
     int tpr, vpl;
 };
-template <typename T>
+constexpr int64_t kNormLong = 8192;
+template <typename T, bool BACK>
 NormShape norm_shape(int64_t D) {
-    const int64_t n = (D + kVec<T> - 1) / kVec<T>;  // 16-byte groups of a row
+    constexpr int wide = kVec<T> == 8 ? 1 : 2;  // groups of 8 entries
+    const int64_t n = (D + kVec<T> - 1) / kVec<T>;
+    if (D > kNormLong) return {0, 0};
     if (n <= 8) return {8, 1};
     if (n <= 16) return {16, 1};
     if (n <= 32) return {32, 1};
     if (n <= 64) return {64, 1};
-    if (n <= 128) return {64, 2};
-    if (n <= 256) return {64, 4};
-    if (n <= 512) return {256, 2};
-    if (n <= 1024) return {256, 4};
-    if (n <= 2048 && sizeof(T) == 4) return {256, 8};
-    return {0, 0};
+    if (D <= 512) return {64, wide};
+    if (D <= 1024) return {64, 2 * wide};
+    if (!BACK) return D <= 2048 ? NormShape{64, 4 * wide} : D <= 4096 ? NormShape{256, 2 * wide} : NormShape{256, 4 * wide};
+    return D <= 2048 ? NormShape{256, wide} : D <= 4096 ? NormShape{256, 2 * wide} : NormShape{512, 2 * wide};
 }
-#define CAT_NORM_SHAPES(X) X(8, 1) X(16, 1) X(32, 1) X(64, 1) X(64, 2) X(64, 4) X(256, 2) X(256, 4) X(256, 8)
 
-// workgroups of the backward pass: their parts are written and read again, so no more than fill the card
-constexpr int kNormParts = 1024;
-int norm_parts(int64_t N, NormShape s) {
-    const int64_t rpb = s.tpr ? kNormThreads / s.tpr : 1, b = (N + rpb - 1) / rpb;
-    return (int)(b < kNormParts ? b : kNormParts);
+// workgroups: as many as the card holds at a time, and of the backward pass, whose parts are written and read again, no more
+constexpr int kNormGroups = 1024, kNormParts = 512;
+int norm_groups(int64_t N, NormShape s, int most) {
+    const int64_t rpb = s.tpr && s.tpr < kNormThreads ? kNormThreads / s.tpr : 1, b = (N + rpb - 1) / rpb;
+    return (int)(b < most ? b : most);
 }
 // long rows: shares of the rows that k_norm_columns takes
 constexpr int kColumnParts = 64;
 
-unsigned norm_blocks(int64_t N, int rpb) {
-    const int64_t b = (N + rpb - 1) / rpb;
-    return (unsigned)(b < kNormMaxBlocks ? b : kNormMaxBlocks);
-}
+unsigned norm_blocks(int64_t N) { return (unsigned)(N < kNormMaxBlocks ? N : kNormMaxBlocks); }
 
+template <typename T, int TPR, int VPL, bool PACK, bool FROM8>
+void norm_instance(const T* x, int64_t N, int64_t D, const float* weight, const float* bias, float eps, T* y, float* mean, float* rstd, int8_t* codes,
+                   float* scales, hipStream_t st) {
+    hipLaunchKernelGGL((k_norm<T, TPR, VPL, PACK, FROM8>), dim3((unsigned)norm_groups(N, {TPR, VPL}, kNormGroups)), dim3(kThreads<TPR>), 0, st, x, N, D,
+                       weight, bias, eps, y, mean, rstd, codes, scales);
+}
 template <typename T, bool PACK, bool FROM8>
 cat_status launch_norm(const T* x, int64_t N, int64_t D, const float* weight, const float* bias, float eps, T* y, float* mean, float* rstd,
                        int8_t* codes, float* scales, hipStream_t st) {
-    const NormShape s = norm_shape<T>(D);
-#define CAT_X(TPR, VPL)                                                                                                                  \
-    if (s.tpr == TPR && s.vpl == VPL)                                                                                                    \
-        hipLaunchKernelGGL((k_norm<T, TPR, VPL, PACK, FROM8>), dim3(norm_blocks(N, kNormThreads / TPR)), dim3(kNormThreads), 0, st, x, N, \
-                           D, weight, bias, eps, y, mean, rstd, codes, scales);
-    CAT_NORM_SHAPES(CAT_X)
+    const NormShape s = norm_shape<T, false>(D);
+#define CAT_X(TPR, VPL) \
+    if (s.tpr == TPR && s.vpl == VPL) norm_instance<T, TPR, VPL, PACK, FROM8>(x, N, D, weight, bias, eps, y, mean, rstd, codes, scales, st);
+    CAT_X(8, 1) CAT_X(16, 1) CAT_X(32, 1) CAT_X(64, 1) CAT_X(64, 2) CAT_X(64, 4) CAT_X(256, 4)
+    if constexpr (sizeof(T) == 4) {
+        CAT_X(64, 8) CAT_X(256, 8)
+    } else {
+        CAT_X(256, 2)
+    }
 #undef CAT_X
     if (!s.tpr) {
-        if (PACK) {
-            const cat_status r = cat_pack8(x, N, D, sizeof(T) == 4 ? CAT_F32 : CAT_BF16, codes, scales, (void*)st);
-            if (r != CAT_OK) return r;
-        }
-        hipLaunchKernelGGL((k_norm_long<T, FROM8>), dim3(norm_blocks(N, 1)), dim3(kNormThreads), 0, st, x, N, D, weight, bias, eps, y, mean,
-                           rstd, codes, scales);
+        if (PACK) CAT_TRY(cat_pack8(x, N, D, sizeof(T) == 4 ? CAT_F32 : CAT_BF16, codes, scales, (void*)st));
+        hipLaunchKernelGGL((k_norm_long<T, FROM8>), dim3(norm_blocks(N)), dim3(kNormThreads), 0, st, x, N, D, weight, bias, eps, y, mean, rstd, codes,
+                           scales);
     }
     CAT_LAUNCH_CHECK("k_norm");
     return CAT_OK;
 }
 
+template <typename T, int TPR, int VPL, bool FROM8>
+void norm_backward_instance(const T* dy, const T* x, const int8_t* codes, const float* scales, const float* mean, const float* rstd, int64_t N, int64_t D,
+                            const float* weight, const T* radd, T* dx, float* parts, int P, hipStream_t st) {
+    hipLaunchKernelGGL((k_norm_backward<T, TPR, VPL, FROM8>), dim3((unsigned)P), dim3(kThreads<TPR>), 0, st, dy, x, codes, scales, mean, rstd, N, D, weight,
+                       radd, dx, parts);
+}
 template <typename T, bool FROM8>
 cat_status launch_norm_backward(const T* dy, const T* x, const int8_t* codes, const float* scales, const float* mean, const float* rstd,
                                 int64_t N, int64_t D, const float* weight, const T* radd, T* dx, float* dweight, float* dbias, float* parts,
                                 hipStream_t st) {
-    const NormShape s = norm_shape<T>(D);
-    int P = norm_parts(N, s);
+    const NormShape s = norm_shape<T, true>(D);
+    int P = norm_groups(N, s, kNormParts);
     if (!dweight && !dbias) parts = nullptr;
-#define CAT_X(TPR, VPL)                                                                                                                \
-    if (s.tpr == TPR && s.vpl == VPL)                                                                                                  \
-        hipLaunchKernelGGL((k_norm_backward<T, TPR, VPL, FROM8>), dim3((unsigned)P), dim3(kNormThreads), 0, st, dy, x, codes, scales, mean, \
-                           rstd, N, D, weight, radd, dx, parts);
-    CAT_NORM_SHAPES(CAT_X)
+#define CAT_X(TPR, VPL) \
+    if (s.tpr == TPR && s.vpl == VPL) norm_backward_instance<T, TPR, VPL, FROM8>(dy, x, codes, scales, mean, rstd, N, D, weight, radd, dx, parts, P, st);
+    CAT_X(8, 1) CAT_X(16, 1) CAT_X(32, 1) CAT_X(64, 1) CAT_X(64, 2) CAT_X(256, 2)
+    if constexpr (sizeof(T) == 4) {
+        CAT_X(64, 4) CAT_X(256, 4) CAT_X(512, 4)
+    } else {
+        CAT_X(256, 1) CAT_X(512, 2)
+    }
 #undef CAT_X
     if (!s.tpr) {
-        hipLaunchKernelGGL((k_norm_backward_long<T, FROM8>), dim3(norm_blocks(N, 1)), dim3(kNormThreads), 0, st, dy, x, codes, scales, mean,
-                           rstd, N, D, weight, radd, dx);
+        hipLaunchKernelGGL((k_norm_backward_long<T, FROM8>), dim3(norm_blocks(N)), dim3(kNormThreads), 0, st, dy, x, codes, scales, mean, rstd, N, D,
+                           weight, radd, dx);
         CAT_LAUNCH_CHECK("k_norm_backward_long");
         if (parts) {
             P = (int)(N < kColumnParts ? N : kColumnParts);
-            hipLaunchKernelGGL((k_norm_columns<T, FROM8>), dim3((unsigned)((D + kNormThreads - 1) / kNormThreads), (unsigned)P),
-                               dim3(kNormThreads), 0, st, dy, x, codes, scales, mean, rstd, N, D, parts);
+            hipLaunchKernelGGL((k_norm_columns<T, FROM8>), dim3((unsigned)((D + kNormThreads - 1) / kNormThreads), (unsigned)P), dim3(kNormThreads), 0,
+                               st, dy, x, codes, scales, mean, rstd, N, D, parts);
         }
     }
     CAT_LAUNCH_CHECK("k_norm_backward");
-    if (parts) {
-        hipLaunchKernelGGL(k_norm_params, dim3((unsigned)((2 * D + kWave - 1) / kWave)), dim3(256), 0, st, parts, P, D, dweight, dbias);
-        CAT_LAUNCH_CHECK("k_norm_params");
-    }
-    return CAT_OK;
+    return parts ? launch_sum_parts(parts, P, 2 * D, D, dweight, dbias, st) : CAT_OK;
 }
 
 }  // namespace
@@ -499,8 +563,8 @@ cat_status cat_layer_norm_packed(const int8_t* codes, const float* scales, const
 
 size_t cat_layer_norm_backward_workspace_bytes(int64_t N, int64_t D, cat_dtype dt) {
     if (check_rows("cat_layer_norm_backward_workspace_bytes", N, D, dt) != CAT_OK) return 0;
-    const NormShape s = dt == CAT_F32 ? norm_shape<float>(D) : norm_shape<bf16_t>(D);
-    const int P = s.tpr ? norm_parts(N, s) : kColumnParts;
+    const NormShape s = dt == CAT_F32 ? norm_shape<float, true>(D) : norm_shape<bf16_t, true>(D);
+    const int P = s.tpr ? norm_groups(N, s, kNormParts) : kColumnParts;
     return ((size_t)(P > 0 ? P : 1) * 2 * (size_t)D * sizeof(float) + 255) & ~(size_t)255;
 }
 
