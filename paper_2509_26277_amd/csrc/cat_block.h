@@ -113,15 +113,27 @@ __device__ __forceinline__ float lanes_sum(float v) {
     if constexpr (L >= 64) v += __shfl_xor(v, 32, kWave);
     return v;
 }
-// the larger one; a NaN on either side stays (v_max drops it)
-__device__ __forceinline__ float max_nan(float a, float b) { return a >= b || a != a ? a : b; }
+// The largest magnitude, as bits: those of finite values are ordered as integers, infinity's above them and NaN's above that,
+// so a NaN stays (v_max_f32 drops it).
+__device__ __forceinline__ uint32_t mag_max(uint32_t a, float v) {
+    const uint32_t m = __float_as_uint(v) & 0x7FFFFFFFu;
+    return a > m ? a : m;
+}
+template <int CTRL>
+__device__ __forceinline__ uint32_t dpp_max(uint32_t v) {
+    const uint32_t o = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xF, 0xF, true);
+    return v > o ? v : o;
+}
 template <int L>
-__device__ __forceinline__ float lanes_max(float v) {
-    v = max_nan(v, dpp_f32<0xB1>(v));
-    v = max_nan(v, dpp_f32<0x4E>(v));
-    if constexpr (L >= 8) v = max_nan(v, dpp_f32<0x141>(v));
-    if constexpr (L >= 16) v = max_nan(v, dpp_f32<0x140>(v));
-    if constexpr (L >= 32) v = max_nan(v, __shfl_xor(v, 16, kWave));
+__device__ __forceinline__ uint32_t lanes_max(uint32_t v) {
+    v = dpp_max<0xB1>(v);
+    v = dpp_max<0x4E>(v);
+    if constexpr (L >= 8) v = dpp_max<0x141>(v);
+    if constexpr (L >= 16) v = dpp_max<0x140>(v);
+    if constexpr (L >= 32) {
+        const uint32_t o = (uint32_t)__shfl_xor((int)v, 16, kWave);
+        v = v > o ? v : o;
+    }
     return v;
 }
 
@@ -134,18 +146,25 @@ constexpr int kPackGroup = CAT_PACK_GROUP;
 struct PackScale {
     float up, step;
 };
-__device__ __forceinline__ PackScale pack_scale(float amax) {
+__device__ __forceinline__ PackScale pack_scale(uint32_t magnitude) {
+    const float amax = __uint_as_float(magnitude);
     PackScale s;
     const bool held = !(amax < 0x1p-100f);
     s.up = held ? __fdiv_rn(127.f, amax) : 0.f;
     s.step = held ? __fdiv_rn(amax, 127.f) : 0.f;
     return s;
 }
-// (a NaN converts to 0; values beyond the range cannot occur: |x| * (127 / a) rounds to at most 127)
-__device__ __forceinline__ int pack_code(float x, float up) { return (int)__builtin_rintf(x * up); }
+// Codes in the low bytes: |x| * (127 / a) rounds to at most 127, and the sum with 1.5 * 2^23, whose last place is 1, rounds it
+// to the nearest integer, ties to even, in two's complement.  (Not one fma: the product is rounded by itself.)
+__device__ __forceinline__ uint32_t pack_code(float x, float up) {
+#pragma clang fp contract(off)
+    const float p = x * up;
+    return __float_as_uint(p + 12582912.f);
+}
 __device__ __forceinline__ uint32_t pack_codes4(const float* v, float up) {
-    return ((uint32_t)pack_code(v[0], up) & 0xFFu) | (((uint32_t)pack_code(v[1], up) & 0xFFu) << 8) |
-           (((uint32_t)pack_code(v[2], up) & 0xFFu) << 16) | ((uint32_t)pack_code(v[3], up) << 24);
+    const uint32_t lo = __builtin_amdgcn_perm(pack_code(v[1], up), pack_code(v[0], up), 0x0C0C0400u);
+    const uint32_t hi = __builtin_amdgcn_perm(pack_code(v[3], up), pack_code(v[2], up), 0x04000C0Cu);
+    return lo | hi;
 }
 __device__ __forceinline__ float code_value(uint32_t w, int e) { return (float)(int8_t)(w >> (8 * e)); }
 struct __attribute__((packed, aligned(1))) Codes4 {
@@ -182,35 +201,74 @@ __device__ __forceinline__ void ld_codes(const int8_t* row, int64_t j, int64_t D
 }
 
 // ---- activations ----
-// In fp32 throughout.  The saturated ends come out of exp and erf by themselves (exp -> inf gives 1 / inf = 0); a NaN stays.
+// In fp32 throughout.  The saturated ends come out of the exponentials by themselves (exp -> inf gives 1 / inf = 0); a NaN
+// stays.  FAST, for bfloat16 results: the epilogue of a product is bound by these instructions (its matrix cores wait), and
+// the library's erf is some forty of them.
 __device__ __forceinline__ float logistic(float z) { return __fdividef(1.f, 1.f + __expf(-z)); }
 constexpr float kInvSqrt2 = 0.70710678118654752f, kInvSqrt2Pi = 0.39894228040143268f;
 constexpr float kTanhIn = 0.79788456080286536f, kTanhCube = 0.044715f;
 // gelu with tanh: 0.5 z (1 + tanh u) = z * logistic(2 u), u = sqrt(2 / pi) (z + 0.044715 z^3)
 __device__ __forceinline__ float tanh_arg2(float z) { return 2.f * kTanhIn * z * fmaf(kTanhCube * z, z, 1.f); }
-__device__ __forceinline__ float act_value(float z, int act) {
-    switch (act) {
-        case CAT_ACT_RELU: return z > 0.f ? z : (z != z ? z : 0.f);
-        case CAT_ACT_GELU: return 0.5f * z * (1.f + erff(z * kInvSqrt2));
-        case CAT_ACT_GELU_TANH: return z * logistic(tanh_arg2(z));
-        case CAT_ACT_SILU: return z * logistic(z);
-        default: return z;
+// The normal distribution's tail, Phi(-x) = exp(-x^2 / 2) G(x) for x >= 0: G as a polynomial of degree 7 in 1 / (1 + 0.36 x)
+// without a constant term, fitted for the smallest largest relative error over [0, 14] (8.8e-7; beyond 14 the exponential is
+// below the smallest float).
+__device__ __forceinline__ float tail_factor(float x) {
+    const float t = __builtin_amdgcn_rcpf(fmaf(0.36f, x, 1.f));
+    float g = fmaf(t, 0.04705369665f, -0.17975622158f);
+    g = fmaf(t, g, 0.18094301977f);
+    g = fmaf(t, g, 0.02655653377f);
+    g = fmaf(t, g, 0.13971675770f);
+    g = fmaf(t, g, 0.14177289019f);
+    g = fmaf(t, g, 0.14371301576f);
+    return t * g;
+}
+__device__ __forceinline__ float normal_exp(float z) { return __builtin_amdgcn_exp2f(z * z * -0.72134752044448170f); }
+template <int ACT, bool FAST>
+__device__ __forceinline__ float act_value(float z) {
+    if constexpr (ACT == CAT_ACT_RELU) {
+        return z > 0.f ? z : (z != z ? z : 0.f);
+    } else if constexpr (ACT == CAT_ACT_GELU && FAST) {  // z - z Phi(-z), or z Phi(z)
+        const float x = fminf(fabsf(z), 1e30f);           // (no inf * 0)
+        return fmaf(-x, normal_exp(z) * tail_factor(x), fmaxf(z, 0.f));
+    } else if constexpr (ACT == CAT_ACT_GELU) {
+        return 0.5f * z * (1.f + erff(z * kInvSqrt2));
+    } else if constexpr (ACT == CAT_ACT_GELU_TANH) {
+        return z * logistic(tanh_arg2(z));
+    } else if constexpr (ACT == CAT_ACT_SILU) {
+        return z * logistic(z);
+    } else {
+        return z;
     }
 }
-__device__ __forceinline__ float act_grad(float z, int act) {
+template <int ACT, bool FAST>
+__device__ __forceinline__ float act_grad(float z) {
+    if constexpr (ACT == CAT_ACT_RELU) {
+        return z > 0.f ? 1.f : (z != z ? z : 0.f);
+    } else if constexpr (ACT == CAT_ACT_GELU && FAST) {  // Phi + z phi: s below zero, 1 - s above
+        const float x = fminf(fabsf(z), 1e30f), s = normal_exp(z) * fmaf(-kInvSqrt2Pi, x, tail_factor(x));
+        return z > 0.f ? 1.f - s : s;
+    } else if constexpr (ACT == CAT_ACT_GELU) {
+        return fmaf(z * kInvSqrt2Pi, __expf(-0.5f * z * z), 0.5f * (1.f + erff(z * kInvSqrt2)));
+    } else if constexpr (ACT == CAT_ACT_GELU_TANH) {
+        // (beyond |z| = 32 the factor p (1 - p) is zero in fp32, and z * z must not turn it into 0 * inf)
+        const float p = logistic(tanh_arg2(z)), c = fminf(fmaxf(z, -32.f), 32.f);
+        return fmaf(c * p * (1.f - p), 2.f * kTanhIn * fmaf(3.f * kTanhCube * c, c, 1.f), p);
+    } else if constexpr (ACT == CAT_ACT_SILU) {
+        const float p = logistic(z);
+        return p * fmaf(z, 1.f - p, 1.f);
+    } else {
+        return 1.f;
+    }
+}
+// f(std::integral_constant<int, act>) for the activation: one branch, outside the loops over entries
+template <typename F>
+__device__ __forceinline__ void with_act(int act, F f) {
     switch (act) {
-        case CAT_ACT_RELU: return z > 0.f ? 1.f : (z != z ? z : 0.f);
-        case CAT_ACT_GELU: return fmaf(z * kInvSqrt2Pi, __expf(-0.5f * z * z), 0.5f * (1.f + erff(z * kInvSqrt2)));
-        case CAT_ACT_GELU_TANH: {
-            // (beyond |z| = 32 the factor p (1 - p) is zero in fp32, and z * z must not turn it into 0 * inf)
-            const float p = logistic(tanh_arg2(z)), c = fminf(fmaxf(z, -32.f), 32.f);
-            return fmaf(c * p * (1.f - p), 2.f * kTanhIn * fmaf(3.f * kTanhCube * c, c, 1.f), p);
-        }
-        case CAT_ACT_SILU: {
-            const float p = logistic(z);
-            return p * fmaf(z, 1.f - p, 1.f);
-        }
-        default: return 1.f;
+        case CAT_ACT_RELU: f(std::integral_constant<int, CAT_ACT_RELU>()); break;
+        case CAT_ACT_GELU: f(std::integral_constant<int, CAT_ACT_GELU>()); break;
+        case CAT_ACT_GELU_TANH: f(std::integral_constant<int, CAT_ACT_GELU_TANH>()); break;
+        case CAT_ACT_SILU: f(std::integral_constant<int, CAT_ACT_SILU>()); break;
+        default: f(std::integral_constant<int, CAT_ACT_NONE>()); break;
     }
 }
 

@@ -41,7 +41,7 @@ struct GemmArgs {
 
 constexpr int64_t kGemmMaxRowBytes = 1 << 23;  // offsets inside a tile of 256 rows stay below 2^31
 
-// E (4 or 8) neighbouring entries of a row of out, from column n on (a multiple of E), through the epilogue.  PACK: the 16
+// E (4 or 8) neighbouring entries of a row of out, from column n on (a multiple of E), through the epilogue (BIAS: theirs is not in the sums yet).  PACK: the 16
 // lanes of a DPP row hold 128 columns of one row of out, all of them active.
 template <typename T, int E>
 __device__ __forceinline__ void ld_entries(const T* row, int64_t n, int64_t N, float (&v)[E]) {
@@ -72,11 +72,11 @@ __device__ __forceinline__ void st_entries(T* row, int64_t n, int64_t N, const f
             if (n + e < N) st_round(row + n + e, v[e]);
     }
 }
-template <typename T, int KIND, int E, bool PACK>
+template <typename T, int KIND, int E, bool PACK, bool BIAS = true>
 __device__ __forceinline__ void finish(const Epilogue& e, int64_t m, int64_t n, int64_t N, bool valid, float (&v)[E]) {
     const int64_t at = m * N;
     if constexpr (KIND == kForward) {
-        if (e.bias) {
+        if (BIAS && e.bias) {
             float b[E];
             ld_params<E>(e.bias, valid ? n : 0, N, 0.f, b);
 #pragma unroll
@@ -84,9 +84,9 @@ __device__ __forceinline__ void finish(const Epilogue& e, int64_t m, int64_t n, 
         }
         if constexpr (PACK) {
             if (e.codes_out) {
-                float a = 0.f;
+                uint32_t a = 0;
 #pragma unroll
-                for (int i = 0; i < E; i++) a = max_nan(a, valid && n + i < N ? fabsf(v[i]) : 0.f);
+                for (int i = 0; i < E; i++) a = mag_max(a, valid && n + i < N ? v[i] : 0.f);
                 const PackScale s = pack_scale(lanes_max<kPackGroup / E>(a));
                 if (valid && n < N) {
                     st_codes<E>(e.codes_out + at, n, N, v, s.up);
@@ -95,25 +95,10 @@ __device__ __forceinline__ void finish(const Epilogue& e, int64_t m, int64_t n, 
             }
         }
         if (!valid || n >= N) return;
-        switch (e.act) {  // outside the loop over the entries: one branch
-            case CAT_ACT_RELU:
+        with_act(e.act, [&](auto which) {
 #pragma unroll
-                for (int i = 0; i < E; i++) v[i] = act_value(v[i], CAT_ACT_RELU);
-                break;
-            case CAT_ACT_GELU:
-#pragma unroll
-                for (int i = 0; i < E; i++) v[i] = act_value(v[i], CAT_ACT_GELU);
-                break;
-            case CAT_ACT_GELU_TANH:
-#pragma unroll
-                for (int i = 0; i < E; i++) v[i] = act_value(v[i], CAT_ACT_GELU_TANH);
-                break;
-            case CAT_ACT_SILU:
-#pragma unroll
-                for (int i = 0; i < E; i++) v[i] = act_value(v[i], CAT_ACT_SILU);
-                break;
-            default: break;
-        }
+            for (int i = 0; i < E; i++) v[i] = act_value<decltype(which)::value, sizeof(T) == 2>(v[i]);
+        });
         if (e.residual) {
             float r[E];
             ld_entries<T, E>((const T*)e.residual + at, n, N, r);
@@ -127,24 +112,10 @@ __device__ __forceinline__ void finish(const Epilogue& e, int64_t m, int64_t n, 
                 float c[E];
                 const float step = e.scales_in[m * ((N + kPackGroup - 1) / kPackGroup) + n / kPackGroup];
                 ld_codes<E>(e.codes_in + at, n, N, step, c);
-                switch (e.act) {
-                    case CAT_ACT_RELU:
+                with_act(e.act, [&](auto which) {
 #pragma unroll
-                        for (int i = 0; i < E; i++) v[i] *= act_grad(c[i], CAT_ACT_RELU);
-                        break;
-                    case CAT_ACT_GELU:
-#pragma unroll
-                        for (int i = 0; i < E; i++) v[i] *= act_grad(c[i], CAT_ACT_GELU);
-                        break;
-                    case CAT_ACT_GELU_TANH:
-#pragma unroll
-                        for (int i = 0; i < E; i++) v[i] *= act_grad(c[i], CAT_ACT_GELU_TANH);
-                        break;
-                    default:
-#pragma unroll
-                        for (int i = 0; i < E; i++) v[i] *= act_grad(c[i], CAT_ACT_SILU);
-                        break;
-                }
+                    for (int i = 0; i < E; i++) v[i] *= act_grad<decltype(which)::value, sizeof(T) == 2>(c[i]);
+                });
             }
         }
     }

@@ -4,13 +4,15 @@
 // A workgroup computes TM x TN entries of out, each of its waves WM x 128.  A step takes 128 bytes of k (64 bfloat16 or 32
 // float entries) of both operands into LDS by loads that go there directly (no registers, no stores; what lies outside an
 // operand arrives as zeros by the bounds of its buffer), two steps' worth of LDS in turn.
-//   k contiguous: 128 bytes of a row, its eight 16-byte chunks c at position c ^ (row & 7), so that the 16 rows of a
+//   k contiguous: 128 bytes of a row, its eight 16-byte chunks c at position c ^ key(row), so that the 16 rows of a
 //                 fragment are read without bank conflicts; the load's lane order does the exchange.
 //   turned:       the rows of k as they lie, chunk c at c ^ f(k).  bfloat16 fragments are read by ds_read_b64_tr_b16,
 //                 which hands a lane four k of its column; float ones entry by entry.
-// The n side is the matrix instruction's first operand: a lane then holds four neighbouring columns of one row of out, and
-// a wave whole scale groups of 128 columns.  At the end each wave passes its rows, 16 at a time, through a patch of LDS of
-// its own, from which a lane takes 8 neighbouring columns: loads and stores of the epilogue are whole lines.
+// The n side is the matrix instruction's first operand: a lane then holds four columns of one row of out a tile, and a wave
+// whole scale groups of 128 columns.  Its tiles are paired, tile 2 t taking columns 0..3, 8..11, 16..19, 24..27 of 32 and
+// tile 2 t + 1 the others, so that a lane's eight columns of a pair are neighbours: the epilogue works on them where they are,
+// with 16-byte loads and stores.  (Through LDS, 16 rows at a time, a tile's epilogue took 11 to 27 us, as long as 8 to 16
+// steps of k.)  Only tiles that end inside, and rows that are no whole 16-byte groups, still go through LDS, row by row.
 #pragma once
 #include "cat_gemm.h"
 
@@ -32,10 +34,11 @@ struct Stage {
     static constexpr int kStep = kStepBytes / (int)sizeof(T);
     static constexpr int kRowBytes = TURNED ? ROWS * (int)sizeof(T) : kStepBytes;  // in LDS
     uint32_t off[kLoads];
-    int kc;  // k contiguous: this lane's first k of a step
+    int kc[2];  // k contiguous: this lane's first k of a step, even and odd loads
     const char* base;
     int64_t left, step_bytes;
 
+    static __device__ __forceinline__ int key(int row) { return (row & 3) | ((row >> 1) & 4); }
     static __device__ __forceinline__ int swizzle(int k) { return sizeof(T) == 2 ? 2 * ((k + (k >> 3)) & 3) : 4 * ((k >> 2) & 3); }
 
     __device__ __forceinline__ void init(const void* ptr, int64_t ld, int64_t bytes, int64_t r0, int64_t rows, int64_t k0, int wave, int lane) {
@@ -44,7 +47,7 @@ struct Stage {
         base = (const char*)ptr + at;
         left = bytes - at;
         step_bytes = TURNED ? kStep * pitch : kStepBytes;
-        kc = 0;
+        kc[0] = kc[1] = 0;
 #pragma unroll
         for (int i = 0; i < kLoads; i++) {
             const int byte = (wave * kLoads + i) * 1024 + lane * 16;
@@ -53,8 +56,8 @@ struct Stage {
                 const int c = pos ^ swizzle(line);
                 off[i] = r0 + c * kVec<T> < rows ? (uint32_t)(line * pitch + c * 16) : kOutside;
             } else {
-                const int c = pos ^ (line & 7);
-                kc = c * kVec<T>;  // (line & 7 is the same for all loads of a lane)
+                const int c = pos ^ key(line);
+                kc[i & 1] = c * kVec<T>;  // (the key depends on a row's place among 16, two loads' worth)
                 off[i] = r0 + line < rows ? (uint32_t)(line * pitch + c * 16) : kOutside;
             }
         }
@@ -63,44 +66,57 @@ struct Stage {
     __device__ __forceinline__ void load(lds_char lds, int wave, int64_t k_left) {
         const uint32_t n = left <= 0 ? 0u : left < (int64_t)kOutside ? (uint32_t)left : kOutside;
         auto rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, n, 0x00027000);
-        const bool cut = !TURNED && k_left < kStep && kc >= k_left;  // (turned: rows behind the last lie behind the buffer's end)
+        // (turned: rows behind the last lie behind the buffer's end)
+        const bool cut[2] = {!TURNED && k_left < kStep && kc[0] >= k_left, !TURNED && k_left < kStep && kc[1] >= k_left};
 #pragma unroll
         for (int i = 0; i < kLoads; i++)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_void)(lds + (wave * kLoads + i) * 1024), 16, cut ? kOutside : off[i], 0, 0, 0);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_void)(lds + (wave * kLoads + i) * 1024), 16, cut[i & 1] ? kOutside : off[i], 0, 0, 0);
         base += step_bytes;
         left -= step_bytes;
     }
 };
 
 // Fragments of one operand: 16 rows x half a step.  Lane (r = lane % 16, g = lane / 16) holds bfloat16 k = 32 h + 8 g .. + 7
-// or float k = 16 h + 4 g .. + 3 of row r.
-template <typename T, bool TURNED, int ROWS>
+// or float k = 16 h + 4 g .. + 3 of row r.  PAIRED: row r of tiles 2 t and 2 t + 1 is row 32 t + 8 (r / 4) + r % 4 (+ 4).
+template <typename T, bool TURNED, bool PAIRED, int ROWS>
 struct Fragments {
-    uint32_t at[TURNED ? 4 : 2];
-    // tile16: the wave's first tile of 16 rows
+    static constexpr int kAt = TURNED || PAIRED ? 4 : 2;
+    uint32_t at[kAt];
+    // tile16: the wave's first tile of 16 rows (PAIRED: an even one)
     __device__ __forceinline__ void init(int tile16, int lane) {
         const int r = lane & 15, g = lane >> 4;
-        if constexpr (!TURNED) {
+        using S = Stage<T, TURNED, ROWS, 4>;
+        if constexpr (!TURNED && !PAIRED) {
 #pragma unroll
-            for (int h = 0; h < 2; h++) at[h] = (tile16 * 16 + r) * kStepBytes + ((h * 4 + g) ^ (r & 7)) * 16;
-        } else if constexpr (sizeof(T) == 2) {
-            const int f = 2 * (((r >> 2) + g) & 3);  // swizzle(k) for k = 8 g + r / 4 (+ 4, + 32)
+            for (int h = 0; h < 2; h++) at[h] = (tile16 * 16 + r) * kStepBytes + ((h * 4 + g) ^ S::key(r)) * 16;
+        } else if constexpr (!TURNED) {  // [odd tile][h]; the key of rows 8 (r / 4) + r % 4 (+ 4) is that of r / 4's parity and r % 4
 #pragma unroll
-            for (int t = 0; t < 4; t++) {
-                const int tile = tile16 + t;
-                at[t] = (8 * g + (r >> 2)) * (ROWS * 2) + (((2 * (tile & 3) + ((r & 3) >> 1)) ^ f) + 8 * (tile >> 2)) * 16 + (r & 1) * 8;
+            for (int i = 0; i < 4; i++) {
+                const int row = 8 * (r >> 2) + (r & 3) + 4 * (i >> 1);
+                at[i] = (tile16 * 16 + row) * kStepBytes + (((i & 1) * 4 + g) ^ S::key(row)) * 16;
             }
         } else {
+            // turned: columns are addressed in pieces of 4 (bfloat16, 8 bytes, supplied by one lane) or by themselves (float);
+            // bits 5 and 6 of a column's place change with f(k), so tiles 0..3 of every 64 columns have an address each
 #pragma unroll
             for (int t = 0; t < 4; t++) {
                 const int tile = tile16 + t;
-                at[t] = 4 * g * (ROWS * 4) + (4 * ((tile & 3) ^ g) + 16 * (tile >> 2)) * 16 + r * 4;
+                if constexpr (sizeof(T) == 2) {
+                    const int k = 8 * g + (r >> 2), q = r & 3;  // this lane supplies columns 4 q .. 4 q + 3 of the tile at k (+ 4, + 32)
+                    const int col = PAIRED ? 32 * (tile >> 1) + 8 * q + 4 * (tile & 1) : 16 * tile + 4 * q;
+                    at[t] = k * (ROWS * 2) + ((col >> 3) ^ S::swizzle(k)) * 16 + (col & 7) * 2;
+                } else {
+                    const int k = 4 * g;
+                    const int col = PAIRED ? 32 * (tile >> 1) + 8 * (r >> 2) + (r & 3) + 4 * (tile & 1) : 16 * tile + r;
+                    at[t] = k * (ROWS * 4) + ((col >> 2) ^ S::swizzle(k)) * 16 + (col & 3) * 4;
+                }
             }
         }
     }
     __device__ __forceinline__ f32x4 read(lds_char lds, int t, int h) const {
         if constexpr (!TURNED) {
-            return *(__attribute__((address_space(3))) f32x4*)(lds + at[h] + t * 16 * kStepBytes);
+            const uint32_t a = PAIRED ? at[(t & 1) * 2 + h] + (t >> 1) * 32 * kStepBytes : at[h] + t * 16 * kStepBytes;
+            return *(__attribute__((address_space(3))) f32x4*)(lds + a);
         } else if constexpr (sizeof(T) == 2) {
             const lds_char p = lds + at[t & 3] + (t >> 2) * 128 + h * 32 * (ROWS * 2);
             union {
@@ -131,6 +147,104 @@ __device__ __forceinline__ f32x4 multiply(f32x4 a, f32x4 b, f32x4 c) {
     }
 }
 
+// The epilogue of a wave's MT x 16 rows by 128 columns, all of them inside out, whose rows are whole 16-byte groups.  Lane
+// (r, g): rows m + 16 mt, columns n + 32 t .. + 7, t = 0..3, in acc[mt][2 t] and acc[mt][2 t + 1].
+template <typename T>
+__device__ __forceinline__ void ld8(const T* p, float (&v)[8]) {
+    if constexpr (sizeof(T) == 2) {
+        const uint4 q = *(const uint4*)p;
+        const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+        for (int e = 0; e < 4; e++) v[2 * e] = __uint_as_float(w[e] << 16), v[2 * e + 1] = __uint_as_float(w[e] & 0xFFFF0000u);
+    } else {
+        const f32x4 lo = *(const f32x4*)p, hi = *(const f32x4*)(p + 4);
+#pragma unroll
+        for (int e = 0; e < 4; e++) v[e] = lo[e], v[4 + e] = hi[e];
+    }
+}
+template <typename T>
+__device__ __forceinline__ void st8(T* p, const float (&v)[8]) {
+    if constexpr (sizeof(T) == 2) {
+        *(uint4*)p = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
+    } else {
+        *(f32x4*)p = f32x4{v[0], v[1], v[2], v[3]};
+        *(f32x4*)(p + 4) = f32x4{v[4], v[5], v[6], v[7]};
+    }
+}
+template <typename T, int KIND, int MT>
+__device__ __forceinline__ void finish_whole(const Epilogue& e, f32x4 (&acc)[MT][8], int64_t m, int64_t M, int64_t n, int64_t N, int g) {
+    const int64_t G = (N + kPackGroup - 1) / kPackGroup, group = n / kPackGroup;
+    if constexpr (KIND == kForward) {
+        if (e.codes_out) {
+#pragma unroll
+            for (int mt = 0; mt < MT; mt++) {
+                uint32_t a = 0;
+#pragma unroll
+                for (int nt = 0; nt < 8; nt++)
+#pragma unroll
+                    for (int i = 0; i < 4; i++) a = mag_max(a, acc[mt][nt][i]);
+                // (the four lanes of a row of out, 16 apart)
+                uint32_t o = (uint32_t)__shfl_xor((int)a, 16, kWave);
+                a = a > o ? a : o;
+                o = (uint32_t)__shfl_xor((int)a, 32, kWave);
+                const PackScale s = pack_scale(a > o ? a : o);
+                const int64_t row = m + 16 * mt;
+                if (row < M) {
+#pragma unroll
+                    for (int t = 0; t < 4; t++) {
+                        const float lo[4] = {acc[mt][2 * t][0], acc[mt][2 * t][1], acc[mt][2 * t][2], acc[mt][2 * t][3]};
+                        const float hi[4] = {acc[mt][2 * t + 1][0], acc[mt][2 * t + 1][1], acc[mt][2 * t + 1][2], acc[mt][2 * t + 1][3]};
+                        *(uint2*)(e.codes_out + row * N + n + 32 * t) = make_uint2(pack_codes4(lo, s.up), pack_codes4(hi, s.up));
+                    }
+                    if (g == 0) e.scales_out[row * G + group] = s.step;
+                }
+                __builtin_amdgcn_sched_barrier(0);  // (a row at a time: all of them together do not fit the registers)
+            }
+        }
+    }
+    const auto rows = [&](auto which) {
+        constexpr int ACT = decltype(which)::value;
+        constexpr bool fast = sizeof(T) == 2;
+#pragma unroll
+        for (int mt = 0; mt < MT; mt++) {
+            const int64_t row = m + 16 * mt;
+            if (row >= M) continue;
+            float more[4][8];  // the residual, or the argument of the derivative
+            const bool res = KIND == kForward && e.residual;
+            if (res) {
+#pragma unroll
+                for (int t = 0; t < 4; t++) ld8((const T*)e.residual + row * N + n + 32 * t, more[t]);
+            }
+            if constexpr (KIND == kInputGrad && ACT != CAT_ACT_NONE) {
+                const float step = e.scales_in[row * G + group];
+#pragma unroll
+                for (int t = 0; t < 4; t++) {
+                    const uint2 c = *(const uint2*)(e.codes_in + row * N + n + 32 * t);
+#pragma unroll
+                    for (int i = 0; i < 4; i++) more[t][i] = code_value(c.x, i) * step, more[t][4 + i] = code_value(c.y, i) * step;
+                }
+            }
+#pragma unroll
+            for (int t = 0; t < 4; t++) {
+                float v[8];
+#pragma unroll
+                for (int i = 0; i < 8; i++) {
+                    v[i] = acc[mt][2 * t + (i >> 2)][i & 3];
+                    if constexpr (KIND == kForward) v[i] = act_value<ACT, fast>(v[i]);
+                    if constexpr (KIND == kInputGrad) v[i] *= act_grad<ACT, fast>(more[t][i]);
+                    if (res) v[i] += more[t][i];
+                }
+                st8((T*)e.out + row * N + n + 32 * t, v);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    if constexpr (KIND == kWeightGrad)
+        rows(std::integral_constant<int, CAT_ACT_NONE>());
+    else
+        with_act(e.act, rows);
+}
+
 template <typename T, int KIND, int TM, int TN, int WM>
 __global__ __launch_bounds__((TM / WM) * (TN / 128) * 64) void k_gemm(const GemmArgs a) {
 #ifdef __HIP_DEVICE_COMPILE__  // (the host's pass does not know all of the builtins, and would leave out the kernel's stub)
@@ -159,21 +273,26 @@ __global__ __launch_bounds__((TM / WM) * (TN / 128) * 64) void k_gemm(const Gemm
     Stage<T, QT, TM, W> sq;
     sp.init(a.p, a.ldp, a.p_bytes, n0, a.n, k0, wave, lane);
     sq.init(a.q, a.ldq, a.q_bytes, m0, a.m, k0, wave, lane);
-    Fragments<T, PT, TN> fp;
-    Fragments<T, QT, TM> fq;
+    Fragments<T, PT, true, TN> fp;
+    Fragments<T, QT, false, TM> fq;
     fp.init(wn * NT, lane);
     fq.init(wm * MT, lane);
-
-    f32x4 acc[MT][NT];
-#pragma unroll
-    for (int mt = 0; mt < MT; mt++)
-#pragma unroll
-        for (int nt = 0; nt < NT; nt++) acc[mt][nt] = f32x4{0.f, 0.f, 0.f, 0.f};
 
     int cur = 0;
     if (k_left > 0) {
         sp.load(lds, wave, k_left);
         sq.load(lds + TN * kStepBytes, wave, k_left);
+    }
+    // the sums begin with the bias (with shares of k the kernel that joins them adds it)
+    const int r = lane & 15, g = lane >> 4;
+    const int64_t nw = n0 + wn * WN, nl = nw + 8 * g;  // the wave's first column; this lane's of pair t: nl + 32 t
+    f32x4 acc[MT][NT];
+#pragma unroll
+    for (int nt = 0; nt < NT; nt++) {
+        float b[4] = {0.f, 0.f, 0.f, 0.f};
+        if (KIND == kForward && a.e.bias && a.splits == 1) ld_params<4>(a.e.bias, nl + (nt >> 1) * 32 + 4 * (nt & 1), a.n, 0.f, b);
+#pragma unroll
+        for (int mt = 0; mt < MT; mt++) acc[mt][nt] = f32x4{b[0], b[1], b[2], b[3]};
     }
     __syncthreads();
     for (; k_left > 0; k_left -= kStep, cur ^= kBuf) {
@@ -196,7 +315,7 @@ __global__ __launch_bounds__((TM / WM) * (TN / 128) * 64) void k_gemm(const Gemm
         __syncthreads();
     }
 
-    const int r = lane & 15, g = lane >> 4;
+    const bool whole = nw + WN <= a.n && a.n % 8 == 0;
     if (a.splits > 1) {  // the sum of a share of k: fp32, joined by a kernel of its own
         float* part = a.parts + (int64_t)blockIdx.y * a.m * a.n;
 #pragma unroll
@@ -205,33 +324,38 @@ __global__ __launch_bounds__((TM / WM) * (TN / 128) * 64) void k_gemm(const Gemm
             if (m >= a.m) continue;
 #pragma unroll
             for (int nt = 0; nt < NT; nt++) {
-                const int64_t n = n0 + wn * WN + nt * 16 + 4 * g;
+                const int64_t n = nl + (nt >> 1) * 32 + 4 * (nt & 1);
                 const float v[4] = {acc[mt][nt][0], acc[mt][nt][1], acc[mt][nt][2], acc[mt][nt][3]};
                 if (n < a.n) st_group_to(part + m * a.n, n, a.n, v);
             }
         }
         return;
     }
+    if (whole) {
+        finish_whole<T, KIND, MT>(a.e, acc, m0 + wm * WM + r, a.m, nl, a.n, g);
+        return;
+    }
     const lds_char patch = lds + wave * kPatch;
 #pragma unroll 1
     for (int mt = 0; mt < MT; mt++) {
 #pragma unroll
-        for (int nt = 0; nt < NT; nt++) *(__attribute__((address_space(3))) f32x4*)(patch + r * kPatchPitch + nt * 64 + g * 16) = acc[0][nt];
+        for (int nt = 0; nt < NT; nt++)
+            *(__attribute__((address_space(3))) f32x4*)(patch + r * kPatchPitch + ((nt >> 1) * 32 + 8 * g + 4 * (nt & 1)) * 4) = acc[0][nt];
 #pragma unroll
-        for (int j = 0; j + 1 < MT; j++)  // (so that the loop need not be unrolled: the epilogue is long)
+        for (int j = 0; j + 1 < MT; j++)  // (so that the loop need not be unrolled)
 #pragma unroll
             for (int nt = 0; nt < NT; nt++) acc[j][nt] = acc[j + 1][nt];
         // the patch is the wave's own, and a wave's LDS accesses are done in order
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
-        const int64_t n = n0 + wn * WN + r * 8;
+        const int64_t n = nw + r * 8;
 #pragma unroll 1
         for (int s = 0; s < 4; s++) {
             const int64_t m = m0 + wm * WM + mt * 16 + s * 4 + g;
             const lds_char from = patch + (s * 4 + g) * kPatchPitch + r * 32;
             const f32x4 lo = *(__attribute__((address_space(3))) f32x4*)from, hi = *(__attribute__((address_space(3))) f32x4*)(from + 16);
             float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-            finish<T, KIND, 8, true>(a.e, m, n, a.n, m < a.m, v);
+            finish<T, KIND, 8, true, false>(a.e, m, n, a.n, m < a.m, v);
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();

@@ -125,9 +125,10 @@ __global__ __launch_bounds__(256) void k_lay_out(const T* __restrict__ src, cons
         float v[V];
         if constexpr (FROM8) {
             ld_codes<V>(codes + row * cols, j, cols, scales[row * G + j / kPackGroup], v);
-            if (act != CAT_ACT_NONE)
+            with_act(act, [&](auto which) {  // act(0) = 0 behind the row's end
 #pragma unroll
-                for (int e = 0; e < V; e++) v[e] = act_value(v[e], act);  // act(0) = 0 behind the row's end
+                for (int e = 0; e < V; e++) v[e] = act_value<decltype(which)::value, sizeof(T) == 2>(v[e]);
+            });
         } else {
             ld_group_to(src + row * cols, j, cols, v);
         }

@@ -127,9 +127,10 @@ __global__ __launch_bounds__(kThreads<TPR>) void k_norm(const T* __restrict__ x,
 #pragma unroll
             for (int k = 0; k < VPL; k++) {
                 const int64_t j = ((int64_t)k * TPR + sub) * V;
-                float a = 0.f, f[V];
+                uint32_t a = 0;
+                float f[V];
 #pragma unroll
-                for (int e = 0; e < V; e++) f[e] = v[k].at(e), a = max_nan(a, fabsf(f[e]));
+                for (int e = 0; e < V; e++) f[e] = v[k].at(e), a = mag_max(a, f[e]);
                 a = lanes_max<(TPR < GL ? TPR : GL)>(a);
                 const PackScale s = pack_scale(a);
                 if (mine && j < D) {

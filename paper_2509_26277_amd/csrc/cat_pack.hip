@@ -96,9 +96,9 @@ __global__ __launch_bounds__(256) void k_pack8(const T* __restrict__ x, int64_t 
         const Place<T> p = place_of<T>(mine ? t : n - 1, G);
         float v[V];
         ld_group_to(x + p.row * D, p.j, D, v);
-        float a = 0.f;
+        uint32_t a = 0;
 #pragma unroll
-        for (int e = 0; e < V; e++) a = max_nan(a, fabsf(v[e]));
+        for (int e = 0; e < V; e++) a = mag_max(a, v[e]);
         a = lanes_max<parts>(a);
         const PackScale s = pack_scale(a);
         if (!mine) continue;
@@ -131,8 +131,10 @@ __global__ __launch_bounds__(256) void k_activation_backward(const T* __restrict
         float d[V], z[V];
         ld_group_to(dy + p.row * D, p.j, D, d);
         ld_codes<V>(codes + p.row * D, p.j, D, scales[p.group], z);
+        with_act(act, [&](auto which) {
 #pragma unroll
-        for (int e = 0; e < V; e++) d[e] *= act_grad(z[e], act);
+            for (int e = 0; e < V; e++) d[e] *= act_grad<decltype(which)::value, sizeof(T) == 2>(z[e]);
+        });
         st_group_to(dz + p.row * D, p.j, D, d);
     }
 }
