@@ -18,8 +18,6 @@
 
 namespace cat {
 
-typedef short i16x4 __attribute__((ext_vector_type(4)));
-typedef __attribute__((address_space(3))) i16x4* lds_i16x4;
 typedef __attribute__((address_space(3))) void* lds_void;
 typedef __attribute__((address_space(3))) char* lds_char;
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
@@ -62,17 +60,21 @@ struct Stage {
             }
         }
     }
-    // k_left: entries of k from this step on; the last step may be short
-    __device__ __forceinline__ void load(lds_char lds, int wave, int64_t k_left) {
+    // One step's loads: begin(), then one() for each of them.  k_left: entries of k from this step on; the last step may be
+    // short, and behind it nothing is left (zeros, not used).
+    __amdgpu_buffer_rsrc_t rsrc;
+    bool cut[2];
+    __device__ __forceinline__ void begin(int64_t k_left) {
         const uint32_t n = left <= 0 ? 0u : left < (int64_t)kOutside ? (uint32_t)left : kOutside;
-        auto rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, n, 0x00027000);
+        rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, n, 0x00027000);
+        const int kl = k_left < kStep ? (int)(k_left < 0 ? 0 : k_left) : kStep;
         // (turned: rows behind the last lie behind the buffer's end)
-        const bool cut[2] = {!TURNED && k_left < kStep && kc[0] >= k_left, !TURNED && k_left < kStep && kc[1] >= k_left};
-#pragma unroll
-        for (int i = 0; i < kLoads; i++)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_void)(lds + (wave * kLoads + i) * 1024), 16, cut[i & 1] ? kOutside : off[i], 0, 0, 0);
+        cut[0] = !TURNED && kc[0] >= kl, cut[1] = !TURNED && kc[1] >= kl;
         base += step_bytes;
         left -= step_bytes;
+    }
+    __device__ __forceinline__ void one(lds_char lds, int wave, int i) const {
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_void)(lds + (wave * kLoads + i) * 1024), 16, cut[i & 1] ? kOutside : off[i], 0, 0, 0);
     }
 };
 
@@ -113,26 +115,71 @@ struct Fragments {
             }
         }
     }
-    __device__ __forceinline__ f32x4 read(lds_char lds, int t, int h) const {
-        if constexpr (!TURNED) {
-            const uint32_t a = PAIRED ? at[(t & 1) * 2 + h] + (t >> 1) * 32 * kStepBytes : at[h] + t * 16 * kStepBytes;
-            return *(__attribute__((address_space(3))) f32x4*)(lds + a);
-        } else if constexpr (sizeof(T) == 2) {
-            const lds_char p = lds + at[t & 3] + (t >> 2) * 128 + h * 32 * (ROWS * 2);
-            union {
-                i16x4 s[2];
-                f32x4 f;
-            } u;
-            u.s[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4)p);
-            u.s[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4)(p + 4 * (ROWS * 2)));
-            return u.f;
+    // tiles FROM, FROM + 1 of half step H
+    template <int H, int FROM, int NF>
+    __device__ __forceinline__ void read2(lds_char lds, f32x4 (&f)[NF]) const {
+        if constexpr (TURNED && sizeof(T) == 2) {
+            turned2<H * 32 * ROWS * 2 + (FROM >> 2) * 128, 4 * ROWS * 2>((uint32_t)(uintptr_t)lds, at[FROM & 3], at[(FROM & 3) + 1], f[FROM], f[FROM + 1]);
         } else {
-            const lds_char p = lds + at[t & 3] + (t >> 2) * 256 + h * 16 * (ROWS * 4);
-            f32x4 f;
 #pragma unroll
-            for (int j = 0; j < 4; j++) f[j] = *(__attribute__((address_space(3))) float*)(p + j * (ROWS * 4));
-            return f;
+            for (int t = FROM; t < FROM + 2; t++) {
+                if constexpr (!TURNED) {
+                    const uint32_t a = PAIRED ? at[(t & 1) * 2 + H] + (t >> 1) * 32 * kStepBytes : at[H] + t * 16 * kStepBytes;
+                    f[t] = *(__attribute__((address_space(3))) f32x4*)(lds + a);
+                } else {
+                    const lds_char p = lds + at[t & 3] + (t >> 2) * 256 + H * 16 * (ROWS * 4);
+#pragma unroll
+                    for (int j = 0; j < 4; j++) f[t][j] = *(__attribute__((address_space(3))) float*)(p + j * (ROWS * 4));
+                }
+            }
         }
+    }
+    template <int H, int NF>
+    __device__ __forceinline__ void read(lds_char lds, f32x4 (&f)[NF]) const {
+        if constexpr (TURNED && sizeof(T) == 2 && NF % 4 == 0) {
+            const uint32_t base = (uint32_t)(uintptr_t)lds;
+            turned4<H * 32 * ROWS * 2, 4 * ROWS * 2>(base, f[0], f[1], f[2], f[3]);
+            if constexpr (NF == 8) turned4<H * 32 * ROWS * 2 + 128, 4 * ROWS * 2>(base, f[4], f[5], f[6], f[7]);
+        } else {
+            read2<H, 0>(lds, f);
+            if constexpr (NF > 2) read2<H, 2>(lds, f);
+            if constexpr (NF > 4) read2<H, 4>(lds, f), read2<H, 6>(lds, f);
+        }
+    }
+    // The turning reads as blocks that end with their own wait: behind the builtin the compiler puts a wait for all loads into
+    // LDS under way, the next step's among them, which was a third of the time of a gradient's step.
+    template <int OFF, int NEXT>
+    __device__ __forceinline__ void turned2(uint32_t base, uint32_t at0, uint32_t at1, f32x4& f0, f32x4& f1) const {
+        f32x2 a0, a1, b0, b1;
+        asm volatile(
+            "ds_read_b64_tr_b16 %0, %4 offset:%6\n\t"
+            "ds_read_b64_tr_b16 %1, %4 offset:%7\n\t"
+            "ds_read_b64_tr_b16 %2, %5 offset:%6\n\t"
+            "ds_read_b64_tr_b16 %3, %5 offset:%7\n\t"
+            "s_waitcnt lgkmcnt(0)"
+            : "=&v"(a0), "=&v"(a1), "=&v"(b0), "=&v"(b1)
+            : "v"(base + at0), "v"(base + at1), "n"(OFF), "n"(OFF + NEXT)
+            : "memory");
+        f0 = f32x4{a0[0], a0[1], a1[0], a1[1]}, f1 = f32x4{b0[0], b0[1], b1[0], b1[1]};
+    }
+    template <int OFF, int NEXT>
+    __device__ __forceinline__ void turned4(uint32_t base, f32x4& f0, f32x4& f1, f32x4& f2, f32x4& f3) const {
+        f32x2 a0, a1, b0, b1, c0, c1, d0, d1;
+        asm volatile(
+            "ds_read_b64_tr_b16 %0, %8 offset:%12\n\t"
+            "ds_read_b64_tr_b16 %1, %8 offset:%13\n\t"
+            "ds_read_b64_tr_b16 %2, %9 offset:%12\n\t"
+            "ds_read_b64_tr_b16 %3, %9 offset:%13\n\t"
+            "ds_read_b64_tr_b16 %4, %10 offset:%12\n\t"
+            "ds_read_b64_tr_b16 %5, %10 offset:%13\n\t"
+            "ds_read_b64_tr_b16 %6, %11 offset:%12\n\t"
+            "ds_read_b64_tr_b16 %7, %11 offset:%13\n\t"
+            "s_waitcnt lgkmcnt(0)"
+            : "=&v"(a0), "=&v"(a1), "=&v"(b0), "=&v"(b1), "=&v"(c0), "=&v"(c1), "=&v"(d0), "=&v"(d1)
+            : "v"(base + at[0]), "v"(base + at[1]), "v"(base + at[2]), "v"(base + at[3]), "n"(OFF), "n"(OFF + NEXT)
+            : "memory");
+        f0 = f32x4{a0[0], a0[1], a1[0], a1[1]}, f1 = f32x4{b0[0], b0[1], b1[0], b1[1]};
+        f2 = f32x4{c0[0], c0[1], c1[0], c1[1]}, f3 = f32x4{d0[0], d0[1], d1[0], d1[1]};
     }
 };
 
@@ -279,10 +326,9 @@ __global__ __launch_bounds__((TM / WM) * (TN / 128) * 64) void k_gemm(const Gemm
     fq.init(wm * MT, lane);
 
     int cur = 0;
-    if (k_left > 0) {
-        sp.load(lds, wave, k_left);
-        sq.load(lds + TN * kStepBytes, wave, k_left);
-    }
+    sp.begin(k_left), sq.begin(k_left);
+#pragma unroll
+    for (int i = 0; i < 4; i++) sp.one(lds, wave, i), sq.one(lds + TN * kStepBytes, wave, i);
     // the sums begin with the bias (with shares of k the kernel that joins them adds it)
     const int r = lane & 15, g = lane >> 4;
     const int64_t nw = n0 + wn * WN, nl = nw + 8 * g;  // the wave's first column; this lane's of pair t: nl + 32 t
@@ -294,26 +340,57 @@ __global__ __launch_bounds__((TM / WM) * (TN / 128) * 64) void k_gemm(const Gemm
 #pragma unroll
         for (int mt = 0; mt < MT; mt++) acc[mt][nt] = f32x4{b[0], b[1], b[2], b[3]};
     }
+    // A step's second half is read while the first is multiplied, and the next step's first half while the second half's last
+    // rows are: the wait for the next step's loads, and for the waves that still read this one's, stands before those rows, and
+    // the loads of the step after it follow, one by one between the products.
+    const auto multiply_rows = [&](const f32x4(&p)[NT], const f32x4(&q)[MT], int from, int to) {  // products from .. to - 1
+#pragma unroll
+        for (int i = from; i < to; i++) acc[i / NT][i % NT] = multiply<T>(p[i % NT], q[i / NT], acc[i / NT][i % NT]);
+    };
+    f32x4 p0[NT], q0[MT], p1[NT], q1[MT];
+    constexpr int kAll = MT * NT, kLoads = Stage<T, PT, TN, W>::kLoads;
+    static_assert(kLoads == 4 && Stage<T, QT, TM, W>::kLoads == 4, "");
     __syncthreads();
+    sp.begin(k_left - kStep), sq.begin(k_left - kStep);
+#pragma unroll
+    for (int i = 0; i < kLoads; i++) sp.one(lds + kBuf, wave, i), sq.one(lds + kBuf + TN * kStepBytes, wave, i);
+    fp.template read<0>(lds, p0);
+    fq.template read<0>(lds + TN * kStepBytes, q0);
     for (; k_left > 0; k_left -= kStep, cur ^= kBuf) {
-        if (k_left > kStep) {
-            sp.load(lds + (cur ^ kBuf), wave, k_left - kStep);
-            sq.load(lds + (cur ^ kBuf) + TN * kStepBytes, wave, k_left - kStep);
+        fp.template read<1>(lds + cur, p1);
+        fq.template read<1>(lds + cur + TN * kStepBytes, q1);
+        multiply_rows(p0, q0, 0, kAll);
+        multiply_rows(p1, q1, 0, kAll / 2);
+#pragma unroll
+        for (int i = 0; i < NT + MT; i++) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);  // a product
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);  // a DS read
         }
-#pragma unroll
-        for (int h = 0; h < 2; h++) {
-            f32x4 p[NT], q[MT];
-#pragma unroll
-            for (int nt = 0; nt < NT; nt++) p[nt] = fp.read(lds + cur, nt, h);
-#pragma unroll
-            for (int mt = 0; mt < MT; mt++) q[mt] = fq.read(lds + cur + TN * kStepBytes, mt, h);
-#pragma unroll
-            for (int mt = 0; mt < MT; mt++)
-#pragma unroll
-                for (int nt = 0; nt < NT; nt++) acc[mt][nt] = multiply<T>(p[nt], q[mt], acc[mt][nt]);
-        }
+        __builtin_amdgcn_sched_barrier(0);
         __syncthreads();
+        sp.begin(k_left - 2 * kStep), sq.begin(k_left - 2 * kStep);
+        // (after the last step: of a buffer that is not used)
+        const lds_char next_p = lds + (cur ^ kBuf), next_q = next_p + TN * kStepBytes;
+        const auto part = [&](auto which) {
+            constexpr int i = decltype(which)::value;
+            multiply_rows(p1, q1, kAll / 2 + kAll / 16 * i, kAll / 2 + kAll / 16 * (i + 1));
+            if constexpr (i < NT / 2) fp.template read2<0, 2 * i>(next_p, p0);
+            if constexpr (i >= 4 && i < 4 + MT / 2) fq.template read2<0, 2 * (i - 4)>(next_q, q0);
+            if constexpr (i < kLoads) sp.one(lds + cur, wave, i);
+            if constexpr (i >= kLoads) sq.one(lds + cur + TN * kStepBytes, wave, i - kLoads);
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        part(std::integral_constant<int, 0>()), part(std::integral_constant<int, 1>());
+        part(std::integral_constant<int, 2>()), part(std::integral_constant<int, 3>());
+        part(std::integral_constant<int, 4>()), part(std::integral_constant<int, 5>());
+        part(std::integral_constant<int, 6>()), part(std::integral_constant<int, 7>());
+        // (keeps the compiler from moving these reads behind the products, to where the loop uses them)
+#pragma unroll
+        for (int i = 0; i < NT; i++) asm volatile("" : "+v"(p0[i]));
+#pragma unroll
+        for (int i = 0; i < MT; i++) asm volatile("" : "+v"(q0[i]));
     }
+    __syncthreads();
 
     const bool whole = nw + WN <= a.n && a.n % 8 == 0;
     if (a.splits > 1) {  // the sum of a share of k: fp32, joined by a kernel of its own
