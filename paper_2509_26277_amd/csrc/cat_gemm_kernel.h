@@ -33,45 +33,44 @@ struct Stage {
     static constexpr int kRowBytes = TURNED ? ROWS * (int)sizeof(T) : kStepBytes;  // in LDS
     uint32_t off[kLoads];
     int kc[2];  // k contiguous: this lane's first k of a step, even and odd loads
+    int64_t pitch;
     const char* base;
-    int64_t left, step_bytes;
+    int64_t left;
 
     static __device__ __forceinline__ int key(int row) { return (row & 3) | ((row >> 1) & 4); }
     static __device__ __forceinline__ int swizzle(int k) { return sizeof(T) == 2 ? 2 * ((k + (k >> 3)) & 3) : 4 * ((k >> 2) & 3); }
 
-    __device__ __forceinline__ void init(const void* ptr, int64_t ld, int64_t bytes, int64_t r0, int64_t rows, int64_t k0, int wave, int lane) {
-        const int64_t pitch = ld * (int64_t)sizeof(T);
-        const int64_t at = TURNED ? k0 * pitch + r0 * (int64_t)sizeof(T) : r0 * pitch + k0 * (int64_t)sizeof(T);
-        base = (const char*)ptr + at;
-        left = bytes - at;
-        step_bytes = TURNED ? kStep * pitch : kStepBytes;
+    // Offsets inside a tile.  Rows behind the operand's last and rows of k behind its last lie behind the buffer's end.  Columns
+    // of a turned operand behind its last do not; like those rows, they only reach entries of out that are not stored.
+    __device__ __forceinline__ void init(int64_t ld, int wave, int lane) {
+        pitch = ld * (int64_t)sizeof(T);
         kc[0] = kc[1] = 0;
 #pragma unroll
         for (int i = 0; i < kLoads; i++) {
             const int byte = (wave * kLoads + i) * 1024 + lane * 16;
             const int line = byte / kRowBytes, pos = byte % kRowBytes / 16;
-            if constexpr (TURNED) {
-                const int c = pos ^ swizzle(line);
-                off[i] = r0 + c * kVec<T> < rows ? (uint32_t)(line * pitch + c * 16) : kOutside;
-            } else {
-                const int c = pos ^ key(line);
-                kc[i & 1] = c * kVec<T>;  // (the key depends on a row's place among 16, two loads' worth)
-                off[i] = r0 + line < rows ? (uint32_t)(line * pitch + c * 16) : kOutside;
-            }
+            const int c = pos ^ (TURNED ? swizzle(line) : key(line));
+            if (!TURNED) kc[i & 1] = c * kVec<T>;  // (the key depends on a row's place among 16, two loads' worth)
+            off[i] = (uint32_t)(line * pitch + c * 16);
         }
     }
-    // One step's loads: begin(), then one() for each of them.  k_left: entries of k from this step on; the last step may be
-    // short, and behind it nothing is left (zeros, not used).
+    // where a tile's first step begins, and what may be read from there on (never nothing: a tile begins inside)
+    __device__ __forceinline__ void tile(const void* ptr, int64_t bytes, int64_t r0, int64_t k0, const char*& from, int64_t& much) const {
+        const int64_t at = TURNED ? k0 * pitch + r0 * (int64_t)sizeof(T) : r0 * pitch + k0 * (int64_t)sizeof(T);
+        from = (const char*)ptr + at;
+        much = bytes - at;
+    }
+    // One step's loads: begin(), then one() for each of them.  kl: entries of k in this step (the last may be short).
     __amdgpu_buffer_rsrc_t rsrc;
     bool cut[2];
-    __device__ __forceinline__ void begin(int64_t k_left) {
-        const uint32_t n = left <= 0 ? 0u : left < (int64_t)kOutside ? (uint32_t)left : kOutside;
+    __device__ __forceinline__ void begin(int kl) {
+        const uint32_t n = (uint64_t)left >> 31 ? kOutside : (uint32_t)left;
         rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, n, 0x00027000);
-        const int kl = k_left < kStep ? (int)(k_left < 0 ? 0 : k_left) : kStep;
         // (turned: rows behind the last lie behind the buffer's end)
         cut[0] = !TURNED && kc[0] >= kl, cut[1] = !TURNED && kc[1] >= kl;
-        base += step_bytes;
-        left -= step_bytes;
+        const int64_t step = TURNED ? kStep * pitch : kStepBytes;
+        base += step;
+        left -= step;
     }
     __device__ __forceinline__ void one(lds_char lds, int wave, int i) const {
         __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_void)(lds + (wave * kLoads + i) * 1024), 16, cut[i & 1] ? kOutside : off[i], 0, 0, 0);
@@ -231,10 +230,10 @@ __device__ __forceinline__ void finish_whole(const Epilogue& e, f32x4 (&acc)[MT]
 #pragma unroll
                     for (int i = 0; i < 4; i++) a = mag_max(a, acc[mt][nt][i]);
                 // (the four lanes of a row of out, 16 apart)
-                uint32_t o = (uint32_t)__shfl_xor((int)a, 16, kWave);
-                a = a > o ? a : o;
-                o = (uint32_t)__shfl_xor((int)a, 32, kWave);
-                const PackScale s = pack_scale(a > o ? a : o);
+                const auto by16 = __builtin_amdgcn_permlane16_swap(a, a, false, false);
+                a = by16[0] > by16[1] ? by16[0] : by16[1];
+                const auto by32 = __builtin_amdgcn_permlane32_swap(a, a, false, false);
+                const PackScale s = pack_scale(by32[0] > by32[1] ? by32[0] : by32[1]);
                 const int64_t row = m + 16 * mt;
                 if (row < M) {
 #pragma unroll
@@ -292,151 +291,206 @@ __device__ __forceinline__ void finish_whole(const Epilogue& e, f32x4 (&acc)[MT]
         with_act(e.act, rows);
 }
 
+// Workgroups stay for all of their tiles: a tile's first loads are under way while the one before it is finished and stored.
 template <typename T, int KIND, int TM, int TN, int WM>
-__global__ __launch_bounds__((TM / WM) * (TN / 128) * 64) void k_gemm(const GemmArgs a) {
+__global__ __launch_bounds__((TM / WM) * (TN / 128) * 64, 2) void k_gemm(const GemmArgs a) {
 #ifdef __HIP_DEVICE_COMPILE__  // (the host's pass does not know all of the builtins, and would leave out the kernel's stub)
     constexpr bool PT = KIND != kForward, QT = KIND == kWeightGrad;
     constexpr int WN = 128, W = (TM / WM) * (TN / WN), MT = WM / 16, NT = WN / 16;
     constexpr int kStep = kStepBytes / (int)sizeof(T);
     constexpr int kBuf = (TM + TN) * kStepBytes;
-    constexpr int kPatchPitch = WN * 4 + 16, kPatch = 16 * kPatchPitch;
-    static_assert(W * kPatch <= 2 * kBuf, "the waves' patches fit the stages");
-    __shared__ __attribute__((aligned(1024))) char lds_mem[2 * kBuf];
-    const lds_char lds = (lds_char)lds_mem;
+    constexpr int kPatchPitch = WN * 4 + 16, kPatch = 4 * kPatchPitch;
+    __shared__ __attribute__((aligned(1024))) char lds_mem[2 * kBuf + 2 * 1024 + W * kPatch];
+    const lds_char lds = (lds_char)lds_mem, lds_bias = lds + 2 * kBuf;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave / (TN / WN), wn = wave % (TN / WN);
 
     // Workgroups go to the eight XCDs in turn; each XCD takes a run of neighbouring tiles, eight columns of them at a time, so
     // that what its L2 holds of either operand serves many of them.
-    const int64_t tm = (a.m + TM - 1) / TM, tn = (a.n + TN - 1) / TN, tiles = tm * tn;
-    const int64_t b = blockIdx.x, share = tiles / 8, more = tiles % 8, x = b % 8, i = b / 8;
-    const int64_t t = x * share + (x < more ? x : more) + i;
-    const int64_t band = t / (8 * tm), in = t - band * 8 * tm, width = tn - band * 8 < 8 ? tn - band * 8 : 8;
-    const int64_t m0 = in / width * TM, n0 = (band * 8 + in % width) * TN;
+    const uint32_t tm = (uint32_t)((a.m + TM - 1) / TM), tn = (uint32_t)((a.n + TN - 1) / TN), tiles = tm * tn;
+    const uint32_t xcd = blockIdx.x & 7, share = tiles / 8, more = tiles % 8;
+    const uint32_t stride = (gridDim.x - xcd + 7) / 8, end = (xcd + 1) * share + (xcd + 1 < more ? xcd + 1 : more);
+    uint32_t t = xcd * share + (xcd < more ? xcd : more) + blockIdx.x / 8;
+    if (t >= end) return;
+    const auto place = [&](uint32_t tile, uint32_t& m0, uint32_t& n0) {
+        const uint32_t band = tile / (8 * tm), in = tile - band * 8 * tm, width = tn - band * 8 < 8 ? tn - band * 8 : 8;
+        m0 = in / width, n0 = band * 8 + in % width;
+    };
 
-    const int64_t k0 = (int64_t)blockIdx.y * a.k_split;
-    int64_t k_left = a.k - k0 < a.k_split ? a.k - k0 : a.k_split;
+    const int64_t k0 = (int64_t)blockIdx.y * a.k_split, k_all = a.k - k0 < a.k_split ? a.k - k0 : a.k_split;
     Stage<T, PT, TN, W> sp;
     Stage<T, QT, TM, W> sq;
-    sp.init(a.p, a.ldp, a.p_bytes, n0, a.n, k0, wave, lane);
-    sq.init(a.q, a.ldq, a.q_bytes, m0, a.m, k0, wave, lane);
     Fragments<T, PT, true, TN> fp;
     Fragments<T, QT, false, TM> fq;
-    fp.init(wn * NT, lane);
-    fq.init(wm * MT, lane);
-
-    int cur = 0;
-    sp.begin(k_left), sq.begin(k_left);
-#pragma unroll
-    for (int i = 0; i < 4; i++) sp.one(lds, wave, i), sq.one(lds + TN * kStepBytes, wave, i);
-    // the sums begin with the bias (with shares of k the kernel that joins them adds it)
-    const int r = lane & 15, g = lane >> 4;
-    const int64_t nw = n0 + wn * WN, nl = nw + 8 * g;  // the wave's first column; this lane's of pair t: nl + 32 t
-    f32x4 acc[MT][NT];
-#pragma unroll
-    for (int nt = 0; nt < NT; nt++) {
-        float b[4] = {0.f, 0.f, 0.f, 0.f};
-        if (KIND == kForward && a.e.bias && a.splits == 1) ld_params<4>(a.e.bias, nl + (nt >> 1) * 32 + 4 * (nt & 1), a.n, 0.f, b);
-#pragma unroll
-        for (int mt = 0; mt < MT; mt++) acc[mt][nt] = f32x4{b[0], b[1], b[2], b[3]};
-    }
-    // A step's second half is read while the first is multiplied, and the next step's first half while the second half's last
-    // rows are: the wait for the next step's loads, and for the waves that still read this one's, stands before those rows, and
-    // the loads of the step after it follow, one by one between the products.
-    const auto multiply_rows = [&](const f32x4(&p)[NT], const f32x4(&q)[MT], int from, int to) {  // products from .. to - 1
-#pragma unroll
-        for (int i = from; i < to; i++) acc[i / NT][i % NT] = multiply<T>(p[i % NT], q[i / NT], acc[i / NT][i % NT]);
+    const auto addresses = [&](int of_lane) {
+        sp.init(a.ldp, wave, of_lane);
+        sq.init(a.ldq, wave, of_lane);
+        fp.init(wn * NT, of_lane);
+        fq.init(wm * MT, of_lane);
     };
-    f32x4 p0[NT], q0[MT], p1[NT], q1[MT];
+    addresses(lane);
     constexpr int kAll = MT * NT, kLoads = Stage<T, PT, TN, W>::kLoads;
     static_assert(kLoads == 4 && Stage<T, QT, TM, W>::kLoads == 4, "");
-    __syncthreads();
-    sp.begin(k_left - kStep), sq.begin(k_left - kStep);
-#pragma unroll
-    for (int i = 0; i < kLoads; i++) sp.one(lds + kBuf, wave, i), sq.one(lds + kBuf + TN * kStepBytes, wave, i);
-    fp.template read<0>(lds, p0);
-    fq.template read<0>(lds + TN * kStepBytes, q0);
-    for (; k_left > 0; k_left -= kStep, cur ^= kBuf) {
-        fp.template read<1>(lds + cur, p1);
-        fq.template read<1>(lds + cur + TN * kStepBytes, q1);
-        multiply_rows(p0, q0, 0, kAll);
-        multiply_rows(p1, q1, 0, kAll / 2);
-#pragma unroll
-        for (int i = 0; i < NT + MT; i++) {
-            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);  // a product
-            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);  // a DS read
-        }
-        __builtin_amdgcn_sched_barrier(0);
-        __syncthreads();
-        sp.begin(k_left - 2 * kStep), sq.begin(k_left - 2 * kStep);
-        // (after the last step: of a buffer that is not used)
-        const lds_char next_p = lds + (cur ^ kBuf), next_q = next_p + TN * kStepBytes;
-        const auto part = [&](auto which) {
-            constexpr int i = decltype(which)::value;
-            multiply_rows(p1, q1, kAll / 2 + kAll / 16 * i, kAll / 2 + kAll / 16 * (i + 1));
-            if constexpr (i < NT / 2) fp.template read2<0, 2 * i>(next_p, p0);
-            if constexpr (i >= 4 && i < 4 + MT / 2) fq.template read2<0, 2 * (i - 4)>(next_q, q0);
-            if constexpr (i < kLoads) sp.one(lds + cur, wave, i);
-            if constexpr (i >= kLoads) sq.one(lds + cur + TN * kStepBytes, wave, i - kLoads);
-            __builtin_amdgcn_sched_barrier(0);
-        };
-        part(std::integral_constant<int, 0>()), part(std::integral_constant<int, 1>());
-        part(std::integral_constant<int, 2>()), part(std::integral_constant<int, 3>());
-        part(std::integral_constant<int, 4>()), part(std::integral_constant<int, 5>());
-        part(std::integral_constant<int, 6>()), part(std::integral_constant<int, 7>());
-        // (keeps the compiler from moving these reads behind the products, to where the loop uses them)
-#pragma unroll
-        for (int i = 0; i < NT; i++) asm volatile("" : "+v"(p0[i]));
-#pragma unroll
-        for (int i = 0; i < MT; i++) asm volatile("" : "+v"(q0[i]));
-    }
-    __syncthreads();
 
-    const bool whole = nw + WN <= a.n && a.n % 8 == 0;
-    if (a.splits > 1) {  // the sum of a share of k: fp32, joined by a kernel of its own
-        float* part = a.parts + (int64_t)blockIdx.y * a.m * a.n;
+    // The next step to be requested, of this tile or of the next one (behind the last tile: of that one again, not used).
+    const int steps = (int)((k_all + kStep - 1) / kStep), tail = (int)(k_all - (int64_t)(steps - 1) * kStep);
+    uint32_t tile_m, tile_n;
+    place(t, tile_m, tile_n);
+    int ahead = steps;
+    sp.tile(a.p, a.p_bytes, (int64_t)tile_n * TN, k0, sp.base, sp.left);
+    sq.tile(a.q, a.q_bytes, (int64_t)tile_m * TM, k0, sq.base, sq.left);
+    uint32_t next_m, next_n;
+    const char *next_p, *next_q;
+    int64_t next_p_left, next_q_left;
+    const auto look_ahead = [&] {
+        place(t + stride < end ? t + stride : t, next_m, next_n);
+        sp.tile(a.p, a.p_bytes, (int64_t)next_n * TN, k0, next_p, next_p_left);
+        sq.tile(a.q, a.q_bytes, (int64_t)next_m * TM, k0, next_q, next_q_left);
+    };
+    const auto begin = [&] {
+        const bool turn = ahead == 0;
+        ahead = turn ? steps : ahead;
+        sp.base = turn ? next_p : sp.base, sp.left = turn ? next_p_left : sp.left;
+        sq.base = turn ? next_q : sq.base, sq.left = turn ? next_q_left : sq.left;
+        const int kl = ahead == 1 ? tail : kStep;
+        sp.begin(kl), sq.begin(kl);
+        ahead--;
+    };
+    look_ahead();
+    begin();
 #pragma unroll
-        for (int mt = 0; mt < MT; mt++) {
-            const int64_t m = m0 + wm * WM + mt * 16 + r;
-            if (m >= a.m) continue;
+    for (int i = 0; i < 4; i++) sp.one(lds, wave, i), sq.one(lds + TN * kStepBytes, wave, i);
+    __syncthreads();
+    begin();
+#pragma unroll
+    for (int i = 0; i < 4; i++) sp.one(lds + kBuf, wave, i), sq.one(lds + kBuf + TN * kStepBytes, wave, i);
+
+    int cur = 0, odd = 0;
+    for (;; t += stride, odd ^= 1024) {
+        const int64_t m0 = (int64_t)tile_m * TM, n0 = (int64_t)tile_n * TN;
+        // The addresses are made anew for every tile, from a lane number that the compiler takes for another one: kept over a
+        // tile's end they would not fit the registers, and their way back from memory would wait for that tile's stores.
+        int lane_again = lane;
+        asm volatile("" : "+v"(lane_again));
+        addresses(lane_again);
+        look_ahead();
+        // the tile's bias into LDS, for its end (without one, and with shares of k, which the joining kernel finishes: zeros)
+        if (KIND == kForward && wave == 0) {
+            const int64_t there = a.e.bias && a.splits == 1 ? (a.n - n0) * 4 : 0;
+            auto rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)(a.e.bias + n0), 0, there < TN * 4 ? (uint32_t)there : TN * 4, 0x00027000);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_void)(lds_bias + odd), 16, lane_again * 16, 0, 0, 0);
+        }
+        f32x4 acc[MT][NT];
+#pragma unroll
+        for (int mt = 0; mt < MT; mt++)
+#pragma unroll
+            for (int nt = 0; nt < NT; nt++) acc[mt][nt] = f32x4{0.f, 0.f, 0.f, 0.f};
+        // A step's second half is read while the first is multiplied, and the next step's first half while the second half's last
+        // rows are: the wait for the next step's loads, and for the waves that still read this one's, stands before those rows, and
+        // the loads of the step after it follow, one by one between the products.
+        const auto multiply_rows = [&](const f32x4(&p)[NT], const f32x4(&q)[MT], int from, int to) {  // products from .. to - 1
+#pragma unroll
+            for (int i = from; i < to; i++) acc[i / NT][i % NT] = multiply<T>(p[i % NT], q[i / NT], acc[i / NT][i % NT]);
+        };
+        f32x4 p0[NT], q0[MT], p1[NT], q1[MT];
+        fp.template read<0>(lds + cur, p0);
+        fq.template read<0>(lds + cur + TN * kStepBytes, q0);
+        for (int step = 0; step < steps; step++, cur ^= kBuf) {
+            begin();
+            fp.template read<1>(lds + cur, p1);
+            fq.template read<1>(lds + cur + TN * kStepBytes, q1);
+            multiply_rows(p0, q0, 0, kAll);
+            multiply_rows(p1, q1, 0, kAll / 2);
+#pragma unroll
+            for (int i = 0; i < NT + MT; i++) {
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);  // a product
+                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);  // a DS read
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            __syncthreads();
+            // (after the last step: of the next tile, and read again there)
+            const lds_char then_p = lds + (cur ^ kBuf), then_q = then_p + TN * kStepBytes;
+            const auto part = [&](auto which) {
+                constexpr int i = decltype(which)::value;
+                multiply_rows(p1, q1, kAll / 2 + kAll / 16 * i, kAll / 2 + kAll / 16 * (i + 1));
+                if constexpr (i < NT / 2) fp.template read2<0, 2 * i>(then_p, p0);
+                if constexpr (i >= 4 && i < 4 + MT / 2) fq.template read2<0, 2 * (i - 4)>(then_q, q0);
+                if constexpr (i < kLoads) sp.one(lds + cur, wave, i);
+                if constexpr (i >= kLoads) sq.one(lds + cur + TN * kStepBytes, wave, i - kLoads);
+                __builtin_amdgcn_sched_barrier(0);
+            };
+            part(std::integral_constant<int, 0>()), part(std::integral_constant<int, 1>());
+            part(std::integral_constant<int, 2>()), part(std::integral_constant<int, 3>());
+            part(std::integral_constant<int, 4>()), part(std::integral_constant<int, 5>());
+            part(std::integral_constant<int, 6>()), part(std::integral_constant<int, 7>());
+            // (keeps the compiler from moving these reads behind the products, to where the loop uses them)
+#pragma unroll
+            for (int i = 0; i < NT; i++) asm volatile("" : "+v"(p0[i]));
+#pragma unroll
+            for (int i = 0; i < MT; i++) asm volatile("" : "+v"(q0[i]));
+        }
+
+        int lane_end = lane;
+        asm volatile("" : "+v"(lane_end));
+        const int r = lane_end & 15, g = lane_end >> 4;
+        const int64_t nw = n0 + wn * WN, nl = nw + 8 * g;  // the wave's first column; this lane's of pair t: nl + 32 t
+        if (KIND == kForward) {
 #pragma unroll
             for (int nt = 0; nt < NT; nt++) {
-                const int64_t n = nl + (nt >> 1) * 32 + 4 * (nt & 1);
-                const float v[4] = {acc[mt][nt][0], acc[mt][nt][1], acc[mt][nt][2], acc[mt][nt][3]};
-                if (n < a.n) st_group_to(part + m * a.n, n, a.n, v);
+                const f32x4 b = *(__attribute__((address_space(3))) f32x4*)(lds_bias + odd + (wn * WN + 8 * g + (nt >> 1) * 32 + 4 * (nt & 1)) * 4);
+#pragma unroll
+                for (int mt = 0; mt < MT; mt++) acc[mt][nt] += b;
             }
         }
-        return;
-    }
-    if (whole) {
-        finish_whole<T, KIND, MT>(a.e, acc, m0 + wm * WM + r, a.m, nl, a.n, g);
-        return;
-    }
-    const lds_char patch = lds + wave * kPatch;
+        if (a.splits > 1) {  // the sum of a share of k: fp32, joined by a kernel of its own
+            float* part = a.parts + (int64_t)blockIdx.y * a.m * a.n;
+#pragma unroll
+            for (int mt = 0; mt < MT; mt++) {
+                const int64_t m = m0 + wm * WM + mt * 16 + r;
+                if (m >= a.m) continue;
+#pragma unroll
+                for (int nt = 0; nt < NT; nt++) {
+                    const int64_t n = nl + (nt >> 1) * 32 + 4 * (nt & 1);
+                    const float v[4] = {acc[mt][nt][0], acc[mt][nt][1], acc[mt][nt][2], acc[mt][nt][3]};
+                    if (n < a.n) st_group_to(part + m * a.n, n, a.n, v);
+                }
+            }
+        } else if (nw + WN <= a.n && a.n % 8 == 0) {
+            finish_whole<T, KIND, MT>(a.e, acc, m0 + wm * WM + r, a.m, nl, a.n, g);
+        } else if (nw < a.n) {
+            const lds_char patch = lds_bias + 2 * 1024 + wave * kPatch;
 #pragma unroll 1
-    for (int mt = 0; mt < MT; mt++) {
-#pragma unroll
-        for (int nt = 0; nt < NT; nt++)
-            *(__attribute__((address_space(3))) f32x4*)(patch + r * kPatchPitch + ((nt >> 1) * 32 + 8 * g + 4 * (nt & 1)) * 4) = acc[0][nt];
-#pragma unroll
-        for (int j = 0; j + 1 < MT; j++)  // (so that the loop need not be unrolled)
-#pragma unroll
-            for (int nt = 0; nt < NT; nt++) acc[j][nt] = acc[j + 1][nt];
-        // the patch is the wave's own, and a wave's LDS accesses are done in order
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-        const int64_t n = nw + r * 8;
+            for (int mt = 0; mt < MT; mt++) {
+                const int64_t n = nw + r * 8;
 #pragma unroll 1
-        for (int s = 0; s < 4; s++) {
-            const int64_t m = m0 + wm * WM + mt * 16 + s * 4 + g;
-            const lds_char from = patch + (s * 4 + g) * kPatchPitch + r * 32;
-            const f32x4 lo = *(__attribute__((address_space(3))) f32x4*)from, hi = *(__attribute__((address_space(3))) f32x4*)(from + 16);
-            float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-            finish<T, KIND, 8, true, false>(a.e, m, n, a.n, m < a.m, v);
+                for (int s = 0; s < 4; s++) {  // four rows at a time
+                    if ((r >> 2) == s) {
+#pragma unroll
+                        for (int j = 0; j < MT; j++)  // (a uniform branch: moving the sums down instead costs as many registers again)
+                            if (j == mt) {
+#pragma unroll
+                                for (int nt = 0; nt < NT; nt++)
+                                    *(__attribute__((address_space(3))) f32x4*)(patch + (r & 3) * kPatchPitch +
+                                                                                ((nt >> 1) * 32 + 8 * g + 4 * (nt & 1)) * 4) = acc[j][nt];
+                            }
+                    }
+                    // the patch is the wave's own, and a wave's LDS accesses are done in order
+                    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                    __builtin_amdgcn_wave_barrier();
+                    const int64_t m = m0 + wm * WM + mt * 16 + s * 4 + g;
+                    const lds_char from = patch + g * kPatchPitch + r * 32;
+                    const f32x4 lo = *(__attribute__((address_space(3))) f32x4*)from, hi = *(__attribute__((address_space(3))) f32x4*)(from + 16);
+                    float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+                    finish<T, KIND, 8, true, false>(a.e, m, n, a.n, m < a.m, v);
+                    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                    __builtin_amdgcn_wave_barrier();
+                }
+            }
         }
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
+        if (t + stride >= end) break;
+        tile_m = next_m, tile_n = next_n;
     }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the loads ahead: no wave ends while LDS is still written for it
 #endif
 }
 
@@ -444,7 +498,9 @@ template <typename T, int KIND, int TM, int TN, int WM>
 cat_status launch_gemm_tiles(const GemmArgs& a, hipStream_t st) {
     const int64_t tiles = ((a.m + TM - 1) / TM) * ((a.n + TN - 1) / TN);
     if (tiles >= (1ll << 31)) return set_error(CAT_ERR_UNSUPPORTED, "product of %lld x %lld entries has too many tiles", (long long)a.m, (long long)a.n);
-    hipLaunchKernelGGL((k_gemm<T, KIND, TM, TN, WM>), dim3((unsigned)tiles, (unsigned)a.splits), dim3((TM / WM) * (TN / 128) * 64), 0, st, a);
+    // as many workgroups as the card holds at a time (256 CUs, by LDS one large tile's or two small ones' each)
+    const int64_t most = 256 * (TM == 256 ? 1 : 2);
+    hipLaunchKernelGGL((k_gemm<T, KIND, TM, TN, WM>), dim3((unsigned)(a.splits > 1 || tiles < most ? tiles : most), (unsigned)a.splits), dim3((TM / WM) * (TN / 128) * 64), 0, st, a);
     CAT_LAUNCH_CHECK("k_gemm");
     return CAT_OK;
 }
