@@ -208,13 +208,14 @@ def _dev(t, dtype=None, shape=None, name="tensor"):
         raise ValueError(f"{name} must be a contiguous device tensor")
     if dtype is not None and t.dtype != dtype:
         raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
-    if shape is not None and tuple(t.shape) != tuple(shape):
+    if shape is not None and t.shape != shape:
         raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
     return t.data_ptr()
 
 
 def _stream():
-    return torch.cuda.current_stream().cuda_stream
+    """The current stream's handle, without the Stream object around it (2.5 us of a small call's 13)."""
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
 
 
 def select_path(path):
