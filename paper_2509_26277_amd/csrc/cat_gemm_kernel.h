@@ -12,7 +12,7 @@
 // whole scale groups of 128 columns.  Its tiles are paired, tile 2 t taking columns 0..3, 8..11, 16..19, 24..27 of 32 and
 // tile 2 t + 1 the others, so that a lane's eight columns of a pair are neighbours: the epilogue works on them where they are,
 // with 16-byte loads and stores.  (Through LDS, 16 rows at a time, a tile's epilogue took 11 to 27 us, as long as 8 to 16
-// steps of k.)  Only tiles that end inside, and rows that are no whole 16-byte groups, still go through LDS, row by row.
+// steps of k.)
 #pragma once
 #include "cat_gemm.h"
 
@@ -193,32 +193,38 @@ __device__ __forceinline__ f32x4 multiply(f32x4 a, f32x4 b, f32x4 c) {
     }
 }
 
-// The epilogue of a wave's MT x 16 rows by 128 columns, all of them inside out, whose rows are whole 16-byte groups.  Lane
-// (r, g): rows m + 16 mt, columns n + 32 t .. + 7, t = 0..3, in acc[mt][2 t] and acc[mt][2 t + 1].
-template <typename T>
-__device__ __forceinline__ void ld8(const T* p, float (&v)[8]) {
-    if constexpr (sizeof(T) == 2) {
-        const uint4 q = *(const uint4*)p;
+// The epilogue of a wave's MT x 16 rows by 128 columns.  Lane (r, g): rows m + 16 mt, columns n + 32 t .. + 7, t = 0..3, in
+// acc[mt][2 t] and acc[mt][2 t + 1].  WHOLE: all columns lie inside out, whose rows are whole 16-byte groups.  Otherwise the
+// eight columns are read and written where they lie (16-byte accesses on an element's boundary), entry by entry where they
+// cross the row's end.
+template <typename T, bool WHOLE>
+__device__ __forceinline__ void ld8(const T* row, int64_t n, int64_t N, float (&v)[8]) {
+    if constexpr (!WHOLE) {
+        ld_entries<T, 8>(row, n, N, v);
+    } else if constexpr (sizeof(T) == 2) {
+        const uint4 q = *(const uint4*)(row + n);
         const uint32_t w[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
         for (int e = 0; e < 4; e++) v[2 * e] = __uint_as_float(w[e] << 16), v[2 * e + 1] = __uint_as_float(w[e] & 0xFFFF0000u);
     } else {
-        const f32x4 lo = *(const f32x4*)p, hi = *(const f32x4*)(p + 4);
+        const f32x4 lo = *(const f32x4*)(row + n), hi = *(const f32x4*)(row + n + 4);
 #pragma unroll
         for (int e = 0; e < 4; e++) v[e] = lo[e], v[4 + e] = hi[e];
     }
 }
-template <typename T>
-__device__ __forceinline__ void st8(T* p, const float (&v)[8]) {
-    if constexpr (sizeof(T) == 2) {
-        *(uint4*)p = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
+template <typename T, bool WHOLE>
+__device__ __forceinline__ void st8(T* row, int64_t n, int64_t N, const float (&v)[8]) {
+    if constexpr (!WHOLE) {
+        st_entries<T, 8>(row, n, N, v);
+    } else if constexpr (sizeof(T) == 2) {
+        *(uint4*)(row + n) = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
     } else {
-        *(f32x4*)p = f32x4{v[0], v[1], v[2], v[3]};
-        *(f32x4*)(p + 4) = f32x4{v[4], v[5], v[6], v[7]};
+        *(f32x4*)(row + n) = f32x4{v[0], v[1], v[2], v[3]};
+        *(f32x4*)(row + n + 4) = f32x4{v[4], v[5], v[6], v[7]};
     }
 }
-template <typename T, int KIND, int MT>
-__device__ __forceinline__ void finish_whole(const Epilogue& e, f32x4 (&acc)[MT][8], int64_t m, int64_t M, int64_t n, int64_t N, int g) {
+template <typename T, int KIND, int MT, bool WHOLE>
+__device__ __forceinline__ void finish_rows(const Epilogue& e, f32x4 (&acc)[MT][8], int64_t m, int64_t M, int64_t n, int64_t N, int g) {
     const int64_t G = (N + kPackGroup - 1) / kPackGroup, group = n / kPackGroup;
     if constexpr (KIND == kForward) {
         if (e.codes_out) {
@@ -228,7 +234,8 @@ __device__ __forceinline__ void finish_whole(const Epilogue& e, f32x4 (&acc)[MT]
 #pragma unroll
                 for (int nt = 0; nt < 8; nt++)
 #pragma unroll
-                    for (int i = 0; i < 4; i++) a = mag_max(a, acc[mt][nt][i]);
+                    for (int i = 0; i < 4; i++)
+                        if (WHOLE || n + 32 * (nt >> 1) + 4 * (nt & 1) + i < N) a = mag_max(a, acc[mt][nt][i]);
                 // (the four lanes of a row of out, 16 apart)
                 const auto by16 = __builtin_amdgcn_permlane16_swap(a, a, false, false);
                 a = by16[0] > by16[1] ? by16[0] : by16[1];
@@ -238,9 +245,13 @@ __device__ __forceinline__ void finish_whole(const Epilogue& e, f32x4 (&acc)[MT]
                 if (row < M) {
 #pragma unroll
                     for (int t = 0; t < 4; t++) {
-                        const float lo[4] = {acc[mt][2 * t][0], acc[mt][2 * t][1], acc[mt][2 * t][2], acc[mt][2 * t][3]};
-                        const float hi[4] = {acc[mt][2 * t + 1][0], acc[mt][2 * t + 1][1], acc[mt][2 * t + 1][2], acc[mt][2 * t + 1][3]};
-                        *(uint2*)(e.codes_out + row * N + n + 32 * t) = make_uint2(pack_codes4(lo, s.up), pack_codes4(hi, s.up));
+                        float v[8];
+#pragma unroll
+                        for (int i = 0; i < 8; i++) v[i] = acc[mt][2 * t + (i >> 2)][i & 3];
+                        if constexpr (WHOLE)
+                            *(uint2*)(e.codes_out + row * N + n + 32 * t) = make_uint2(pack_codes4(v, s.up), pack_codes4(v + 4, s.up));
+                        else
+                            st_codes<8>(e.codes_out + row * N, n + 32 * t, N, v, s.up);
                     }
                     if (g == 0) e.scales_out[row * G + group] = s.step;
                 }
@@ -259,15 +270,19 @@ __device__ __forceinline__ void finish_whole(const Epilogue& e, f32x4 (&acc)[MT]
             const bool res = KIND == kForward && e.residual;
             if (res) {
 #pragma unroll
-                for (int t = 0; t < 4; t++) ld8((const T*)e.residual + row * N + n + 32 * t, more[t]);
+                for (int t = 0; t < 4; t++) ld8<T, WHOLE>((const T*)e.residual + row * N, n + 32 * t, N, more[t]);
             }
             if constexpr (KIND == kInputGrad && ACT != CAT_ACT_NONE) {
                 const float step = e.scales_in[row * G + group];
 #pragma unroll
                 for (int t = 0; t < 4; t++) {
-                    const uint2 c = *(const uint2*)(e.codes_in + row * N + n + 32 * t);
+                    if constexpr (WHOLE) {
+                        const uint2 c = *(const uint2*)(e.codes_in + row * N + n + 32 * t);
 #pragma unroll
-                    for (int i = 0; i < 4; i++) more[t][i] = code_value(c.x, i) * step, more[t][4 + i] = code_value(c.y, i) * step;
+                        for (int i = 0; i < 4; i++) more[t][i] = code_value(c.x, i) * step, more[t][4 + i] = code_value(c.y, i) * step;
+                    } else {
+                        ld_codes<8>(e.codes_in + row * N, n + 32 * t, N, step, more[t]);
+                    }
                 }
             }
 #pragma unroll
@@ -280,7 +295,7 @@ __device__ __forceinline__ void finish_whole(const Epilogue& e, f32x4 (&acc)[MT]
                     if constexpr (KIND == kInputGrad) v[i] *= act_grad<ACT, fast>(more[t][i]);
                     if (res) v[i] += more[t][i];
                 }
-                st8((T*)e.out + row * N + n + 32 * t, v);
+                st8<T, WHOLE>((T*)e.out + row * N, n + 32 * t, N, v);
             }
             __builtin_amdgcn_sched_barrier(0);
         }
@@ -299,8 +314,7 @@ __global__ __launch_bounds__((TM / WM) * (TN / 128) * 64, 2) void k_gemm(const G
     constexpr int WN = 128, W = (TM / WM) * (TN / WN), MT = WM / 16, NT = WN / 16;
     constexpr int kStep = kStepBytes / (int)sizeof(T);
     constexpr int kBuf = (TM + TN) * kStepBytes;
-    constexpr int kPatchPitch = WN * 4 + 16, kPatch = 4 * kPatchPitch;
-    __shared__ __attribute__((aligned(1024))) char lds_mem[2 * kBuf + 2 * 1024 + W * kPatch];
+    __shared__ __attribute__((aligned(1024))) char lds_mem[2 * kBuf + 2 * 1024];
     const lds_char lds = (lds_char)lds_mem, lds_bias = lds + 2 * kBuf;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave / (TN / WN), wn = wave % (TN / WN);
@@ -407,7 +421,8 @@ __global__ __launch_bounds__((TM / WM) * (TN / 128) * 64, 2) void k_gemm(const G
                 __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);  // a DS read
             }
             __builtin_amdgcn_sched_barrier(0);
-            __syncthreads();
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the next step's loads, of this wave: not left to the compiler, which
+            __syncthreads();                                  // does not see what the turning reads read
             // (after the last step: of the next tile, and read again there)
             const lds_char then_p = lds + (cur ^ kBuf), then_q = then_p + TN * kStepBytes;
             const auto part = [&](auto which) {
@@ -456,36 +471,9 @@ __global__ __launch_bounds__((TM / WM) * (TN / 128) * 64, 2) void k_gemm(const G
                 }
             }
         } else if (nw + WN <= a.n && a.n % 8 == 0) {
-            finish_whole<T, KIND, MT>(a.e, acc, m0 + wm * WM + r, a.m, nl, a.n, g);
+            finish_rows<T, KIND, MT, true>(a.e, acc, m0 + wm * WM + r, a.m, nl, a.n, g);
         } else if (nw < a.n) {
-            const lds_char patch = lds_bias + 2 * 1024 + wave * kPatch;
-#pragma unroll 1
-            for (int mt = 0; mt < MT; mt++) {
-                const int64_t n = nw + r * 8;
-#pragma unroll 1
-                for (int s = 0; s < 4; s++) {  // four rows at a time
-                    if ((r >> 2) == s) {
-#pragma unroll
-                        for (int j = 0; j < MT; j++)  // (a uniform branch: moving the sums down instead costs as many registers again)
-                            if (j == mt) {
-#pragma unroll
-                                for (int nt = 0; nt < NT; nt++)
-                                    *(__attribute__((address_space(3))) f32x4*)(patch + (r & 3) * kPatchPitch +
-                                                                                ((nt >> 1) * 32 + 8 * g + 4 * (nt & 1)) * 4) = acc[j][nt];
-                            }
-                    }
-                    // the patch is the wave's own, and a wave's LDS accesses are done in order
-                    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-                    __builtin_amdgcn_wave_barrier();
-                    const int64_t m = m0 + wm * WM + mt * 16 + s * 4 + g;
-                    const lds_char from = patch + g * kPatchPitch + r * 32;
-                    const f32x4 lo = *(__attribute__((address_space(3))) f32x4*)from, hi = *(__attribute__((address_space(3))) f32x4*)(from + 16);
-                    float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-                    finish<T, KIND, 8, true, false>(a.e, m, n, a.n, m < a.m, v);
-                    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-                    __builtin_amdgcn_wave_barrier();
-                }
-            }
+            finish_rows<T, KIND, MT, false>(a.e, acc, m0 + wm * WM + r, a.m, nl, a.n, g);
         }
         if (t + stride >= end) break;
         tile_m = next_m, tile_n = next_n;

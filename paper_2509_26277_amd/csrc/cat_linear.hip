@@ -187,6 +187,27 @@ struct Plan {
     int sum_parts;
     int64_t sum_rows;
 };
+// Large or small tiles, and the shares of k, by the time that each choice is expected to take.  A CU works on a large tile or
+// on one or two small ones, so `rounds` of 256 tiles follow one another, each so many steps of k (128 bytes) and an end; what the
+// join of shares moves comes on top.  Measured, us a step: bfloat16 large 1.55 (turned operands 1.7), small 0.5 (0.6) where two
+// share a CU and 0.65 (0.8) where one has it alone; float 1.75.  A tile's end: 6, 2 and 4 us.  Sums of shares: written and read
+// at 4 TB/s, and a launch.  (us, by the rule and beside it: weight gradient 4096 x 1024 over 16384 rows, bfloat16, four shares of
+// large tiles 150, two of small ones 179; 4096 x 1000 over 512, float, one share 48, two 67; 300 x 4096 over 4096, bfloat16, two
+// shares of small tiles 35, one 42, four 37, large tiles 52 at best; 1024 x 8192 over 8192 small tiles 123, large ones 136.)
+void choose_tiles(GemmKind kind, int64_t m, int64_t n, int64_t steps, cat_dtype dt, bool& large, int& splits) {
+    double best = -1.0;
+    for (int l = 0; l < (dt == CAT_BF16 ? 2 : 1); l++) {
+        const int64_t edge = l ? 256 : 128, tiles = ((m + edge - 1) / edge) * ((n + edge - 1) / edge);
+        const double end = dt == CAT_F32 ? 4.0 : l ? 6.0 : 2.0;
+        for (int s = 1; s <= 32 && (s == 1 || steps / s >= 4); s++) {
+            const int64_t rounds = (tiles * s + 255) / 256;
+            const double step = dt == CAT_F32 ? 1.75 : l ? (kind == kForward ? 1.55 : 1.7) : kind == kForward ? (rounds > 1 ? 0.5 : 0.65) : (rounds > 1 ? 0.6 : 0.8);
+            const double us = rounds * (((steps + s - 1) / s) * step + end) + (s > 1 ? 4.0 + (double)s * m * n * 2e-6 : 0.0);
+            if (best < 0.0 || us < best) best = us, large = l, splits = s;
+            if (rounds > 2 && s > 1) break;  // (more shares only add to what is joined)
+        }
+    }
+}
 // q: rows_q x cols_q, p: rows_p x cols_p as they lie in memory; out is m x n, contracted over k
 Plan plan(GemmKind kind, int64_t m, int64_t n, int64_t k, int64_t rows_q, int64_t cols_q, int64_t rows_p, int64_t cols_p, cat_dtype dt,
           bool from_codes) {
@@ -206,14 +227,7 @@ Plan plan(GemmKind kind, int64_t m, int64_t n, int64_t k, int64_t rows_q, int64_
         pl.lay_q = cols_q != whole(cols_q, dt);
         pl.lay_p = from_codes || cols_p != whole(cols_p, dt);
         pl.ldq = whole(cols_q, dt), pl.ldp = whole(cols_p, dt);
-        const int64_t big = ((m + 255) / 256) * ((n + 255) / 256);
-        pl.large = dt == CAT_BF16 && big >= 192;
-        const int64_t tiles = pl.large ? big : ((m + 127) / 128) * ((n + 127) / 128);
-        int64_t s = 512 / (tiles > 0 ? tiles : 1);  // (no rows: no tiles)
-        const int64_t most = k / (8 * step);
-        if (pl.large) s = 1;
-        s = s < most ? s : most;
-        pl.splits = (int)(s < 1 ? 1 : s > 32 ? 32 : s);
+        choose_tiles(kind, m, n, (k + step - 1) / step, dt, pl.large, pl.splits);
         pl.k_split = ((k + pl.splits - 1) / pl.splits + step - 1) / step * step;
         if (pl.k_split < step) pl.k_split = step;
         pl.splits = (int)((k + pl.k_split - 1) / pl.k_split);
