@@ -114,25 +114,37 @@ __global__ __launch_bounds__(256) void k_join(const float* __restrict__ parts, i
 }
 
 // ---- operands laid out anew ----
-// Rows of a whole number of 16-byte groups (zeros behind a row's end) from rows that are not, or act of a checkpoint.
+// Rows of a whole number of 16-byte groups (zeros behind a row's end) from rows that are not, or act of a checkpoint.  A launch
+// takes up to two operands, the first by the first `blocks` workgroups.
+template <typename T>
+struct Layout {
+    const T* src;
+    const int8_t* codes;  // instead of src: a checkpoint, through act
+    const float* scales;
+    int64_t rows, cols, ld;
+    T* dst;
+    unsigned blocks;
+};
 template <typename T, bool FROM8>
-__global__ __launch_bounds__(256) void k_lay_out(const T* __restrict__ src, const int8_t* __restrict__ codes, const float* __restrict__ scales, int act,
-                                                 int64_t rows, int64_t cols, int64_t ld, T* __restrict__ dst) {
+__global__ __launch_bounds__(256) void k_lay_out(const Layout<T> first, const Layout<T> second, int act) {
     constexpr int V = kVec<T>;
-    const int64_t per = ld / V, n = rows * per, G = (cols + kPackGroup - 1) / kPackGroup;
-    for (int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x; t < n; t += (int64_t)gridDim.x * 256) {
+    const bool other = blockIdx.x >= first.blocks;
+    const Layout<T>& a = other ? second : first;
+    const int64_t block = other ? blockIdx.x - first.blocks : blockIdx.x;
+    const int64_t per = a.ld / V, n = a.rows * per, G = (a.cols + kPackGroup - 1) / kPackGroup;
+    for (int64_t t = block * 256 + threadIdx.x; t < n; t += (int64_t)a.blocks * 256) {
         const int64_t row = n < (1ll << 32) ? (uint32_t)t / (uint32_t)per : t / per, j = (t - row * per) * V;
         float v[V];
         if constexpr (FROM8) {
-            ld_codes<V>(codes + row * cols, j, cols, scales[row * G + j / kPackGroup], v);
+            ld_codes<V>(a.codes + row * a.cols, j, a.cols, a.scales[row * G + j / kPackGroup], v);
             with_act(act, [&](auto which) {  // act(0) = 0 behind the row's end
 #pragma unroll
                 for (int e = 0; e < V; e++) v[e] = act_value<decltype(which)::value, sizeof(T) == 2>(v[e]);
             });
         } else {
-            ld_group_to(src + row * cols, j, cols, v);
+            ld_group_to(a.src + row * a.cols, j, a.cols, v);
         }
-        st_group(dst + row * ld + j, v);
+        st_group(a.dst + row * a.ld + j, v);
     }
 }
 
@@ -263,19 +275,32 @@ Plan plan_weight(int64_t M, int64_t N, int64_t K, cat_dtype dt, bool from_codes)
 }
 
 template <typename T>
-cat_status lay_out(const void* src, const int8_t* codes, const float* scales, int act, int64_t rows, int64_t cols, int64_t ld, void* dst, hipStream_t st) {
-    const unsigned b = blocks_of(rows * (ld / kVec<T>));
-    if (codes)
-        hipLaunchKernelGGL((k_lay_out<T, true>), dim3(b), dim3(256), 0, st, (const T*)src, codes, scales, act, rows, cols, ld, (T*)dst);
-    else
-        hipLaunchKernelGGL((k_lay_out<T, false>), dim3(b), dim3(256), 0, st, (const T*)src, codes, scales, act, rows, cols, ld, (T*)dst);
-    CAT_LAUNCH_CHECK("k_lay_out");
+Layout<T> layout_of(const void* src, const int8_t* codes, const float* scales, int64_t rows, int64_t cols, int64_t ld, void* dst) {
+    return {(const T*)src, codes, scales, rows, cols, ld, (T*)dst, blocks_of(rows * (ld / kVec<T>))};
+}
+// q and p as the plan has them, those that lie otherwise; p from a checkpoint if codes are given
+template <typename T>
+cat_status lay_out(const Plan& pl, const void* q, int64_t rows_q, int64_t cols_q, const void* p, const int8_t* codes, const float* scales, int act,
+                   int64_t rows_p, int64_t cols_p, char* ws, hipStream_t st) {
+    const Layout<T> lq = layout_of<T>(q, nullptr, nullptr, rows_q, cols_q, pl.ldq, ws + pl.at_q);
+    const Layout<T> lp = layout_of<T>(p, codes, scales, rows_p, cols_p, pl.ldp, ws + pl.at_p), none = {};
+    if (pl.lay_p && codes) {
+        hipLaunchKernelGGL((k_lay_out<T, true>), dim3(lp.blocks), dim3(256), 0, st, lp, none, act);
+        CAT_LAUNCH_CHECK("k_lay_out");
+    }
+    const bool more = pl.lay_p && !codes;
+    if (pl.lay_q || more) {
+        const Layout<T>& first = pl.lay_q ? lq : lp;
+        const Layout<T>& second = pl.lay_q && more ? lp : none;
+        hipLaunchKernelGGL((k_lay_out<T, false>), dim3(first.blocks + second.blocks), dim3(256), 0, st, first, second, 0);
+        CAT_LAUNCH_CHECK("k_lay_out");
+    }
     return CAT_OK;
 }
-cat_status lay_out(cat_dtype dt, const void* src, const int8_t* codes, const float* scales, int act, int64_t rows, int64_t cols, int64_t ld, void* dst,
-                   hipStream_t st) {
-    return dt == CAT_F32 ? lay_out<float>(src, codes, scales, act, rows, cols, ld, dst, st)
-                         : lay_out<bf16_t>(src, codes, scales, act, rows, cols, ld, dst, st);
+cat_status lay_out(cat_dtype dt, const Plan& pl, const void* q, int64_t rows_q, int64_t cols_q, const void* p, const int8_t* codes,
+                   const float* scales, int act, int64_t rows_p, int64_t cols_p, char* ws, hipStream_t st) {
+    return dt == CAT_F32 ? lay_out<float>(pl, q, rows_q, cols_q, p, codes, scales, act, rows_p, cols_p, ws, st)
+                         : lay_out<bf16_t>(pl, q, rows_q, cols_q, p, codes, scales, act, rows_p, cols_p, ws, st);
 }
 
 template <typename T, int KIND>
@@ -362,10 +387,7 @@ cat_status cat_linear(const void* x, const void* w, const float* bias, const voi
     char* ws = (char*)workspace;
     const Epilogue e = {y, bias, residual, codes, scales, nullptr, nullptr, (int)act};
     if (pl.few) return dt == CAT_F32 ? few_rows<float>(pl, x, w, M, N, K, e, ws, st) : few_rows<bf16_t>(pl, x, w, M, N, K, e, ws, st);
-    if (pl.lay_q) {
-        CAT_TRY(lay_out(dt, x, nullptr, nullptr, 0, M, K, pl.ldq, ws + pl.at_q, st));
-        CAT_TRY(lay_out(dt, w, nullptr, nullptr, 0, N, K, pl.ldp, ws + pl.at_p, st));
-    }
+    CAT_TRY(lay_out(dt, pl, x, M, K, w, nullptr, nullptr, 0, N, K, ws, st));
     return multiply_tiles(kForward, pl, dt, pl.lay_q ? ws + pl.at_q : x, M, pl.lay_p ? ws + pl.at_p : w, N, M, N, K, e, ws, st);
 }
 
@@ -392,8 +414,7 @@ cat_status cat_linear_backward_input(const void* dy, const void* w, const int8_t
     hipStream_t st = (hipStream_t)hip_stream;
     char* ws = (char*)workspace;
     const Epilogue e = {dx, nullptr, nullptr, nullptr, nullptr, codes, scales, (int)act};
-    if (pl.lay_q) CAT_TRY(lay_out(dt, dy, nullptr, nullptr, 0, M, N, pl.ldq, ws + pl.at_q, st));
-    if (pl.lay_p) CAT_TRY(lay_out(dt, w, nullptr, nullptr, 0, N, K, pl.ldp, ws + pl.at_p, st));
+    CAT_TRY(lay_out(dt, pl, dy, M, N, w, nullptr, nullptr, 0, N, K, ws, st));
     return multiply_tiles(kInputGrad, pl, dt, pl.lay_q ? ws + pl.at_q : dy, M, pl.lay_p ? ws + pl.at_p : w, N, M, K, N, e, ws, st);
 }
 
@@ -431,8 +452,7 @@ cat_status cat_linear_backward_weight(const void* dy, const void* x, const int8_
         CAT_LAUNCH_CHECK("k_column_sums");
         CAT_TRY(launch_sum_parts(parts, pl.sum_parts, N, N, dbias, nullptr, st));
     }
-    if (pl.lay_q) CAT_TRY(lay_out(dt, dy, nullptr, nullptr, 0, M, N, pl.ldq, ws + pl.at_q, st));
-    if (pl.lay_p) CAT_TRY(lay_out(dt, x, codes, scales, (int)act, M, K, pl.ldp, ws + pl.at_p, st));
+    CAT_TRY(lay_out(dt, pl, dy, M, N, x, codes, scales, (int)act, M, K, ws, st));
     const Epilogue e = {dw, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, 0};
     return multiply_tiles(kWeightGrad, pl, dt, pl.lay_q ? ws + pl.at_q : dy, M, pl.lay_p ? ws + pl.at_p : x, M, N, K, M, e, ws, st);
 }
