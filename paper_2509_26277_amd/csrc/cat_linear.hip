@@ -114,7 +114,7 @@ __global__ __launch_bounds__(256) void k_join(const float* __restrict__ parts, i
 }
 
 // ---- operands laid out anew ----
-// Rows of a whole number of 16-byte groups (zeros behind a row's end) from rows that are not, or act of a checkpoint.  A launch
+// Rows of whole_lines() (zeros behind a row's end) from rows that are no whole 16-byte groups, or act of a checkpoint.  A launch
 // takes up to two operands, the first by the first `blocks` workgroups.
 template <typename T>
 struct Layout {
@@ -186,6 +186,12 @@ int64_t whole(int64_t cols, cat_dtype dt) {
     const int64_t v = 16 / entry_bytes(dt);
     return (cols + v - 1) / v * v;
 }
+// the row length of an operand laid out anew: whole steps of 128 bytes, so that a step of a row is one line of the caches and
+// not parts of two
+int64_t whole_lines(int64_t cols, cat_dtype dt) {
+    const int64_t v = 128 / entry_bytes(dt);
+    return (cols + v - 1) / v * v;
+}
 
 constexpr int64_t kFewRows = 64;
 
@@ -238,7 +244,8 @@ Plan plan(GemmKind kind, int64_t m, int64_t n, int64_t k, int64_t rows_q, int64_
     } else {
         pl.lay_q = cols_q != whole(cols_q, dt);
         pl.lay_p = from_codes || cols_p != whole(cols_p, dt);
-        pl.ldq = whole(cols_q, dt), pl.ldp = whole(cols_p, dt);
+        if (pl.lay_q) pl.ldq = whole_lines(cols_q, dt);
+        if (pl.lay_p) pl.ldp = whole_lines(cols_p, dt);
         choose_tiles(kind, m, n, (k + step - 1) / step, dt, pl.large, pl.splits);
         pl.k_split = ((k + pl.splits - 1) / pl.splits + step - 1) / step * step;
         if (pl.k_split < step) pl.k_split = step;
