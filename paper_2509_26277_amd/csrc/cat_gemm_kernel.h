@@ -259,29 +259,63 @@ __device__ __forceinline__ void finish_rows(const Epilogue& e, f32x4 (&acc)[MT][
             }
         }
     }
+    const bool res = KIND == kForward && e.residual;
+    // What the tile reads besides its sums (the residual; the argument of the derivative), as it lies, for all of its rows at
+    // once: they come from memory, and row by row each of them would be waited for.
+    constexpr bool kAhead = WHOLE && (KIND == kInputGrad || KIND == kForward);
+    constexpr int kWords = !kAhead ? 1 : KIND == kInputGrad ? 2 : 2 * (int)sizeof(T);
+    uint32_t raw[kAhead ? MT : 1][4][kWords];
+    float steps[MT];
+    const auto request = [&] {
+        if constexpr (kAhead) {
+#pragma unroll
+            for (int mt = 0; mt < MT; mt++) {
+                const int64_t row = m + 16 * mt < M ? m + 16 * mt : M - 1;
+#pragma unroll
+                for (int t = 0; t < 4; t++) {
+                    if constexpr (KIND == kInputGrad) {
+                        const uint2 c = *(const uint2*)(e.codes_in + row * N + n + 32 * t);
+                        raw[mt][t][0] = c.x, raw[mt][t][1] = c.y;
+                    } else {
+                        const uint4* q = (const uint4*)((const T*)e.residual + row * N + n + 32 * t);
+#pragma unroll
+                        for (int i = 0; i < kWords / 4; i++)
+                            raw[mt][t][4 * i] = q[i].x, raw[mt][t][4 * i + 1] = q[i].y, raw[mt][t][4 * i + 2] = q[i].z, raw[mt][t][4 * i + 3] = q[i].w;
+                    }
+                }
+                if constexpr (KIND == kInputGrad) steps[mt] = e.scales_in[row * G + group];
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
     const auto rows = [&](auto which) {
         constexpr int ACT = decltype(which)::value;
         constexpr bool fast = sizeof(T) == 2;
+        if (KIND == kInputGrad ? ACT != CAT_ACT_NONE : res) request();
 #pragma unroll
         for (int mt = 0; mt < MT; mt++) {
             const int64_t row = m + 16 * mt;
             if (row >= M) continue;
-            float more[4][8];  // the residual, or the argument of the derivative
-            const bool res = KIND == kForward && e.residual;
-            if (res) {
+            float more[4][8];
+            if constexpr (kAhead && KIND == kForward) {
+#pragma unroll
+                for (int t = 0; t < 4; t++)
+#pragma unroll
+                    for (int i = 0; i < 8; i++)
+                        more[t][i] = sizeof(T) == 4 ? __uint_as_float(raw[mt][t][i % kWords])
+                                                    : __uint_as_float(i % 2 ? raw[mt][t][i / 2] & 0xFFFF0000u : raw[mt][t][i / 2] << 16);
+            } else if (res) {
 #pragma unroll
                 for (int t = 0; t < 4; t++) ld8<T, WHOLE>((const T*)e.residual + row * N, n + 32 * t, N, more[t]);
             }
             if constexpr (KIND == kInputGrad && ACT != CAT_ACT_NONE) {
-                const float step = e.scales_in[row * G + group];
 #pragma unroll
                 for (int t = 0; t < 4; t++) {
                     if constexpr (WHOLE) {
-                        const uint2 c = *(const uint2*)(e.codes_in + row * N + n + 32 * t);
 #pragma unroll
-                        for (int i = 0; i < 4; i++) more[t][i] = code_value(c.x, i) * step, more[t][4 + i] = code_value(c.y, i) * step;
+                        for (int i = 0; i < 8; i++) more[t][i] = code_value(raw[mt][t][i / 4], i % 4) * steps[mt];
                     } else {
-                        ld_codes<8>(e.codes_in + row * N, n + 32 * t, N, step, more[t]);
+                        ld_codes<8>(e.codes_in + row * N, n + 32 * t, N, e.scales_in[row * G + group], more[t]);
                     }
                 }
             }
