@@ -392,11 +392,11 @@ __global__ __launch_bounds__((TM / WM) * (TN / 128) * 64, 2) void k_gemm(const G
     int ahead = steps;
     sp.tile(a.p, a.p_bytes, (int64_t)tile_n * TN, k0, sp.base, sp.left);
     sq.tile(a.q, a.q_bytes, (int64_t)tile_m * TM, k0, sq.base, sq.left);
-    uint32_t next_m, next_n;
     const char *next_p, *next_q;
     int64_t next_p_left, next_q_left;
-    const auto look_ahead = [&] {
-        place(t + stride < end ? t + stride : t, next_m, next_n);
+    const auto look_ahead = [&](uint32_t next) {
+        uint32_t next_m, next_n;
+        place(next < end ? next : t, next_m, next_n);
         sp.tile(a.p, a.p_bytes, (int64_t)next_n * TN, k0, next_p, next_p_left);
         sq.tile(a.q, a.q_bytes, (int64_t)next_m * TM, k0, next_q, next_q_left);
     };
@@ -409,7 +409,7 @@ __global__ __launch_bounds__((TM / WM) * (TN / 128) * 64, 2) void k_gemm(const G
         sp.begin(kl), sq.begin(kl);
         ahead--;
     };
-    look_ahead();
+    look_ahead(t + stride);
     begin();
 #pragma unroll
     for (int i = 0; i < 4; i++) sp.one(lds, wave, i), sq.one(lds + TN * kStepBytes, wave, i);
@@ -426,7 +426,7 @@ __global__ __launch_bounds__((TM / WM) * (TN / 128) * 64, 2) void k_gemm(const G
         int lane_again = lane;
         asm volatile("" : "+v"(lane_again));
         addresses(lane_again);
-        look_ahead();
+        look_ahead(t + (steps > 1 ? 1 : 2) * stride);  // (tiles of one step: the next one's is requested already)
         // the tile's bias into LDS, for its end (without one, and with shares of k, which the joining kernel finishes: zeros)
         if (KIND == kForward && wave == 0) {
             const int64_t there = a.e.bias && a.splits == 1 ? (a.n - n0) * 4 : 0;
@@ -515,7 +515,7 @@ __global__ __launch_bounds__((TM / WM) * (TN / 128) * 64, 2) void k_gemm(const G
             finish_rows<T, KIND, MT, false>(a.e, acc, m0 + wm * WM + r, a.m, nl, a.n, g);
         }
         if (t + stride >= end) break;
-        tile_m = next_m, tile_n = next_n;
+        place(t + stride, tile_m, tile_n);
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the loads ahead: no wave ends while LDS is still written for it
 #endif

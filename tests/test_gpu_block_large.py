@@ -39,6 +39,23 @@ def test_shares_of_k_of_large_tiles(ragged):
     assert_close(db, dy.double().sum(0), (U32 * (k + 8) * dy.double().abs().sum(0)).cpu(), "db")
 
 
+@pytest.mark.parametrize("k", [8, 20, 64, 72])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_many_tiles_of_few_steps(k, dtype):
+    """More tiles than workgroups, each of one step of k or two."""
+    M, N = 5000, 4100
+    x, w = _normal(M, k, 1, dtype=dtype), _normal(N, k, 2, k ** -0.5, dtype=dtype)
+    half = half_step(dtype)
+
+    def check(got, a, b, what):
+        want, size = a.double() @ b.double(), a.double().abs() @ b.double().abs()
+        assert_close(got, want, (half * want.abs() + U32 * (k + 8) * size).cpu(), what)
+
+    check(cat_linear(x, w), x, w.t(), "y")
+    check(cat_linear_backward_input(x, w.t().contiguous()), x, w.t(), "dx")
+    check(cat_linear_backward_weight(x.t().contiguous(), x=w.t().contiguous())[0], x, w.t(), "dw")
+
+
 def _same_rows(big, small, at):
     assert torch.equal(big[at:at + len(small)], small)
 
