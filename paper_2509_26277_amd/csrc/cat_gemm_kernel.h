@@ -264,7 +264,6 @@ __device__ __forceinline__ void finish_rows(const Epilogue& e, f32x4 (&acc)[MT][
             }
         }
     }
-    const bool res = KIND == kForward && e.residual;
     // What the tile reads besides its sums (the residual; the argument of the derivative), as it lies, for all of its rows at
     // once: they come from memory, and row by row each of them would be waited for.
     constexpr bool kAhead = WHOLE && (KIND == kInputGrad || KIND == kForward);
@@ -293,23 +292,23 @@ __device__ __forceinline__ void finish_rows(const Epilogue& e, f32x4 (&acc)[MT][
             __builtin_amdgcn_sched_barrier(0);
         }
     };
-    const auto rows = [&](auto which) {
+    const auto rows = [&](auto which, auto with_residual) {
         constexpr int ACT = decltype(which)::value;
-        constexpr bool fast = sizeof(T) == 2;
-        if (KIND == kInputGrad ? ACT != CAT_ACT_NONE : res) request();
+        constexpr bool fast = sizeof(T) == 2, res = decltype(with_residual)::value;
+        if constexpr (KIND == kInputGrad ? ACT != CAT_ACT_NONE : res) request();
 #pragma unroll
         for (int mt = 0; mt < MT; mt++) {
             const int64_t row = m + 16 * mt;
             if (row >= M) continue;
             float more[4][8];
-            if constexpr (kAhead && KIND == kForward) {
+            if constexpr (kAhead && res) {
 #pragma unroll
                 for (int t = 0; t < 4; t++)
 #pragma unroll
                     for (int i = 0; i < 8; i++)
                         more[t][i] = sizeof(T) == 4 ? __uint_as_float(raw[mt][t][i % kWords])
                                                     : __uint_as_float(i % 2 ? raw[mt][t][i / 2] & 0xFFFF0000u : raw[mt][t][i / 2] << 16);
-            } else if (res) {
+            } else if constexpr (res) {
 #pragma unroll
                 for (int t = 0; t < 4; t++) ld8<T, WHOLE>((const T*)e.residual + row * N, n + 32 * t, N, more[t]);
             }
@@ -332,7 +331,7 @@ __device__ __forceinline__ void finish_rows(const Epilogue& e, f32x4 (&acc)[MT][
                     v[i] = acc[mt][2 * t + (i >> 2)][i & 3];
                     if constexpr (KIND == kForward) v[i] = act_value<ACT, fast>(v[i]);
                     if constexpr (KIND == kInputGrad) v[i] *= act_grad<ACT, fast>(more[t][i]);
-                    if (res) v[i] += more[t][i];
+                    if constexpr (res) v[i] += more[t][i];
                 }
                 st8<T, WHOLE>((T*)e.out + row * N, n + 32 * t, N, v);
             }
@@ -340,9 +339,11 @@ __device__ __forceinline__ void finish_rows(const Epilogue& e, f32x4 (&acc)[MT][
         }
     };
     if constexpr (KIND == kWeightGrad)
-        rows(std::integral_constant<int, CAT_ACT_NONE>());
+        rows(std::integral_constant<int, CAT_ACT_NONE>(), std::false_type());
+    else if (KIND == kForward && e.residual)
+        with_act(e.act, [&](auto which) { rows(which, std::true_type()); });
     else
-        with_act(e.act, rows);
+        with_act(e.act, [&](auto which) { rows(which, std::false_type()); });
 }
 
 // Workgroups stay for all of their tiles: a tile's first loads are under way while the one before it is finished and stored.
