@@ -14,10 +14,11 @@
 // with 16-byte loads and stores.
 //
 // Measured (TFLOP/s; a library product of 8192^3: bfloat16 1385, float 154).  bfloat16, tiles of 256 x 256: forward 8192^3 1400 to
-// 1490, 4096^3 1370 to 1410; input gradient of 8192^3 1190 to 1260, weight gradient 1220.  Float: 2048^3 128.  The steps are bound
-// by the matrix cores and the LDS traffic beside them; what comes on top is the epilogue, whose instructions the matrix cores wait
-// for: GELU 30 to 55 us of 16384 x 8192 over 2048, its derivative 35 of 16384 x 4096 over 1024.  (Through LDS, 16 rows at a time, a
-// tile's epilogue took 11 to 27 us, as long as 8 to 16 steps of k.)
+// 1490, 4096^3 1370 to 1410; input gradient 8192^3 1380, weight gradient 1360 (1260 and 1220 with the places of both operands two
+// chunks apart, where paired tiles met on the same banks).  Float: 2048^3 128.  The matrix cores are busy in 57 % of the cycles of
+// 16384 x 8192 over 2048 with GELU, at 1.95 GHz; what comes on top of the steps is the epilogue, whose instructions they wait for:
+// GELU 30 to 55 us there, its derivative 35 of 16384 x 4096 over 1024.  (Through LDS, 16 rows at a time, a tile's epilogue took 11 to
+// 27 us, as long as 8 to 16 steps of k.)
 #pragma once
 #include "cat_gemm.h"
 
@@ -31,7 +32,7 @@ constexpr int kStepBytes = 128;
 constexpr uint32_t kOutside = 0x80000000u;  // an offset that no operand's buffer reaches
 
 // One operand's way into LDS: ROWS rows (columns of a turned operand) x one step, by W waves.
-template <typename T, bool TURNED, int ROWS, int W>
+template <typename T, bool TURNED, bool PAIRED, int ROWS, int W>
 struct Stage {
     static constexpr int kLoads = ROWS * kStepBytes / 1024 / W;  // 1 KB a load of a wave
     static constexpr int kStep = kStepBytes / (int)sizeof(T);
@@ -43,7 +44,11 @@ struct Stage {
     int64_t left;
 
     static __device__ __forceinline__ int key(int row) { return (row & 3) | ((row >> 1) & 4); }
-    static __device__ __forceinline__ int swizzle(int k) { return sizeof(T) == 2 ? 2 * ((k + (k >> 3)) & 3) : 4 * ((k >> 2) & 3); }
+    // f(k).  A bfloat16 fragment's 16 lanes read four k of four chunks each (paired tiles: half of every chunk) or of two whole
+    // ones: places 64 and 32 bytes apart keep them on banks of their own.
+    static __device__ __forceinline__ int swizzle(int k) {
+        return sizeof(T) == 2 ? (PAIRED ? 4 : 2) * ((k + (k >> 3)) & 3) : 4 * ((k >> 2) & 3);
+    }
 
     // Offsets inside a tile.  Rows behind the operand's last and rows of k behind its last lie behind the buffer's end.  Columns
     // of a turned operand behind its last do not; like those rows, they only reach entries of out that are not stored.
@@ -91,7 +96,7 @@ struct Fragments {
     // tile16: the wave's first tile of 16 rows (PAIRED: an even one)
     __device__ __forceinline__ void init(int tile16, int lane) {
         const int r = lane & 15, g = lane >> 4;
-        using S = Stage<T, TURNED, ROWS, 4>;
+        using S = Stage<T, TURNED, PAIRED, ROWS, 4>;
         if constexpr (!TURNED && !PAIRED) {
 #pragma unroll
             for (int h = 0; h < 2; h++) at[h] = (tile16 * 16 + r) * kStepBytes + ((h * 4 + g) ^ S::key(r)) * 16;
@@ -101,6 +106,12 @@ struct Fragments {
                 const int row = 8 * (r >> 2) + (r & 3) + 4 * (i >> 1);
                 at[i] = (tile16 * 16 + row) * kStepBytes + (((i & 1) * 4 + g) ^ S::key(row)) * 16;
             }
+        } else if constexpr (sizeof(T) == 2 && PAIRED) {
+            // turned: this lane supplies columns 8 q .. 8 q + 3 (odd tile: + 4) of 32 at k (+ 4, + 32), 8 bytes; f(k) changes the
+            // place of 32 columns among 128
+            const int k = 8 * (lane >> 4) + (r >> 2), q = r & 3;
+#pragma unroll
+            for (int i = 0; i < 4; i++) at[i] = k * (ROWS * 2) + ((4 * ((tile16 >> 1) + i) + q) ^ S::swizzle(k)) * 16;
         } else {
             // turned: columns are addressed in pieces of 4 (bfloat16, 8 bytes, supplied by one lane) or by themselves (float);
             // bits 5 and 6 of a column's place change with f(k), so tiles 0..3 of every 64 columns have an address each
@@ -109,7 +120,7 @@ struct Fragments {
                 const int tile = tile16 + t;
                 if constexpr (sizeof(T) == 2) {
                     const int k = 8 * g + (r >> 2), q = r & 3;  // this lane supplies columns 4 q .. 4 q + 3 of the tile at k (+ 4, + 32)
-                    const int col = PAIRED ? 32 * (tile >> 1) + 8 * q + 4 * (tile & 1) : 16 * tile + 4 * q;
+                    const int col = 16 * tile + 4 * q;
                     at[t] = k * (ROWS * 2) + ((col >> 3) ^ S::swizzle(k)) * 16 + (col & 7) * 2;
                 } else {
                     const int k = 4 * g;
@@ -122,8 +133,10 @@ struct Fragments {
     // tiles FROM, FROM + 1 of half step H
     template <int H, int FROM, int NF>
     __device__ __forceinline__ void read2(lds_char lds, f32x4 (&f)[NF]) const {
-        if constexpr (TURNED && sizeof(T) == 2) {
-            turned2<H * 32 * ROWS * 2 + (FROM >> 2) * 128, 4 * ROWS * 2>((uint32_t)(uintptr_t)lds, at[FROM & 3], at[(FROM & 3) + 1], f[FROM], f[FROM + 1]);
+        if constexpr (TURNED && sizeof(T) == 2 && PAIRED) {
+            turned2<H * 32 * ROWS * 2, 4 * ROWS * 2, 8>((uint32_t)(uintptr_t)lds, at[FROM / 2], at[FROM / 2], f[FROM], f[FROM + 1]);
+        } else if constexpr (TURNED && sizeof(T) == 2) {
+            turned2<H * 32 * ROWS * 2 + (FROM >> 2) * 128, 4 * ROWS * 2, 0>((uint32_t)(uintptr_t)lds, at[FROM & 3], at[(FROM & 3) + 1], f[FROM], f[FROM + 1]);
         } else {
 #pragma unroll
             for (int t = FROM; t < FROM + 2; t++) {
@@ -142,8 +155,14 @@ struct Fragments {
     __device__ __forceinline__ void read(lds_char lds, f32x4 (&f)[NF]) const {
         if constexpr (TURNED && sizeof(T) == 2 && NF % 4 == 0) {
             const uint32_t base = (uint32_t)(uintptr_t)lds;
-            turned4<H * 32 * ROWS * 2, 4 * ROWS * 2>(base, f[0], f[1], f[2], f[3]);
-            if constexpr (NF == 8) turned4<H * 32 * ROWS * 2 + 128, 4 * ROWS * 2>(base, f[4], f[5], f[6], f[7]);
+            constexpr int off = H * 32 * ROWS * 2, next = 4 * ROWS * 2;
+            if constexpr (PAIRED) {
+                turned4<off, next, 8>(base, at[0], at[0], at[1], at[1], f[0], f[1], f[2], f[3]);
+                if constexpr (NF == 8) turned4<off, next, 8>(base, at[2], at[2], at[3], at[3], f[4], f[5], f[6], f[7]);
+            } else {
+                static_assert(NF == 4, "");
+                turned4<off, next, 0>(base, at[0], at[1], at[2], at[3], f[0], f[1], f[2], f[3]);
+            }
         } else {
             read2<H, 0>(lds, f);
             if constexpr (NF > 2) read2<H, 2>(lds, f);
@@ -152,35 +171,36 @@ struct Fragments {
     }
     // The turning reads as blocks that end with their own wait: behind the builtin the compiler puts a wait for all loads into
     // LDS under way, the next step's among them, which was a third of the time of a gradient's step.
-    template <int OFF, int NEXT>
+    // (ODD: what an odd tile's address has more)
+    template <int OFF, int NEXT, int ODD>
     __device__ __forceinline__ void turned2(uint32_t base, uint32_t at0, uint32_t at1, f32x4& f0, f32x4& f1) const {
         f32x2 a0, a1, b0, b1;
         asm volatile(
             "ds_read_b64_tr_b16 %0, %4 offset:%6\n\t"
             "ds_read_b64_tr_b16 %1, %4 offset:%7\n\t"
-            "ds_read_b64_tr_b16 %2, %5 offset:%6\n\t"
-            "ds_read_b64_tr_b16 %3, %5 offset:%7\n\t"
+            "ds_read_b64_tr_b16 %2, %5 offset:%8\n\t"
+            "ds_read_b64_tr_b16 %3, %5 offset:%9\n\t"
             "s_waitcnt lgkmcnt(0)"
             : "=&v"(a0), "=&v"(a1), "=&v"(b0), "=&v"(b1)
-            : "v"(base + at0), "v"(base + at1), "n"(OFF), "n"(OFF + NEXT)
+            : "v"(base + at0), "v"(base + at1), "n"(OFF), "n"(OFF + NEXT), "n"(OFF + ODD), "n"(OFF + NEXT + ODD)
             : "memory");
         f0 = f32x4{a0[0], a0[1], a1[0], a1[1]}, f1 = f32x4{b0[0], b0[1], b1[0], b1[1]};
     }
-    template <int OFF, int NEXT>
-    __device__ __forceinline__ void turned4(uint32_t base, f32x4& f0, f32x4& f1, f32x4& f2, f32x4& f3) const {
+    template <int OFF, int NEXT, int ODD>
+    __device__ __forceinline__ void turned4(uint32_t base, uint32_t at0, uint32_t at1, uint32_t at2, uint32_t at3, f32x4& f0, f32x4& f1, f32x4& f2, f32x4& f3) const {
         f32x2 a0, a1, b0, b1, c0, c1, d0, d1;
         asm volatile(
             "ds_read_b64_tr_b16 %0, %8 offset:%12\n\t"
             "ds_read_b64_tr_b16 %1, %8 offset:%13\n\t"
-            "ds_read_b64_tr_b16 %2, %9 offset:%12\n\t"
-            "ds_read_b64_tr_b16 %3, %9 offset:%13\n\t"
+            "ds_read_b64_tr_b16 %2, %9 offset:%14\n\t"
+            "ds_read_b64_tr_b16 %3, %9 offset:%15\n\t"
             "ds_read_b64_tr_b16 %4, %10 offset:%12\n\t"
             "ds_read_b64_tr_b16 %5, %10 offset:%13\n\t"
-            "ds_read_b64_tr_b16 %6, %11 offset:%12\n\t"
-            "ds_read_b64_tr_b16 %7, %11 offset:%13\n\t"
+            "ds_read_b64_tr_b16 %6, %11 offset:%14\n\t"
+            "ds_read_b64_tr_b16 %7, %11 offset:%15\n\t"
             "s_waitcnt lgkmcnt(0)"
             : "=&v"(a0), "=&v"(a1), "=&v"(b0), "=&v"(b1), "=&v"(c0), "=&v"(c1), "=&v"(d0), "=&v"(d1)
-            : "v"(base + at[0]), "v"(base + at[1]), "v"(base + at[2]), "v"(base + at[3]), "n"(OFF), "n"(OFF + NEXT)
+            : "v"(base + at0), "v"(base + at1), "v"(base + at2), "v"(base + at3), "n"(OFF), "n"(OFF + NEXT), "n"(OFF + ODD), "n"(OFF + NEXT + ODD)
             : "memory");
         f0 = f32x4{a0[0], a0[1], a1[0], a1[1]}, f1 = f32x4{b0[0], b0[1], b1[0], b1[1]};
         f2 = f32x4{c0[0], c0[1], c1[0], c1[1]}, f3 = f32x4{d0[0], d0[1], d1[0], d1[1]};
@@ -372,8 +392,8 @@ __global__ __launch_bounds__((TM / WM) * (TN / 128) * 64, 2) void k_gemm(const G
     };
 
     const int64_t k0 = (int64_t)blockIdx.y * a.k_split, k_all = a.k - k0 < a.k_split ? a.k - k0 : a.k_split;
-    Stage<T, PT, TN, W> sp;
-    Stage<T, QT, TM, W> sq;
+    Stage<T, PT, true, TN, W> sp;
+    Stage<T, QT, false, TM, W> sq;
     Fragments<T, PT, true, TN> fp;
     Fragments<T, QT, false, TM> fq;
     const auto addresses = [&](int of_lane) {
@@ -383,8 +403,8 @@ __global__ __launch_bounds__((TM / WM) * (TN / 128) * 64, 2) void k_gemm(const G
         fq.init(wm * MT, of_lane);
     };
     addresses(lane);
-    constexpr int kAll = MT * NT, kLoads = Stage<T, PT, TN, W>::kLoads;
-    static_assert(kLoads == 4 && Stage<T, QT, TM, W>::kLoads == 4, "");
+    constexpr int kAll = MT * NT, kLoads = decltype(sp)::kLoads;
+    static_assert(kLoads == 4 && decltype(sq)::kLoads == 4, "");
 
     // The next step to be requested, of this tile or of the next one (behind the last tile: of that one again, not used).
     const int steps = (int)((k_all + kStep - 1) / kStep), tail = (int)(k_all - (int64_t)(steps - 1) * kStep);
