@@ -207,11 +207,12 @@ struct Plan {
 };
 // Large or small tiles, and the shares of k, by the time that each choice is expected to take.  A CU works on a large tile or
 // on one or two small ones, so `rounds` of 256 tiles follow one another, each so many steps of k (128 bytes) and an end; what the
-// join of shares moves comes on top.  Measured, us a step: bfloat16 large 1.55 (turned operands 1.7), small 0.5 (0.6) where two
-// share a CU and 0.65 (0.8) where one has it alone; float 1.75.  A tile's end: 6, 2 and 4 us.  Sums of shares: written and read
-// at 4 TB/s, and a launch.  (us, by the rule and beside it: weight gradient 4096 x 1024 over 16384 rows, bfloat16, four shares of
-// large tiles 150, two of small ones 179; 4096 x 1000 over 512, float, one share 48, two 67; 300 x 4096 over 4096, bfloat16, two
-// shares of small tiles 35, one 42, four 37, large tiles 52 at best; 1024 x 8192 over 8192 small tiles 123, large ones 136.)
+// join of shares moves comes on top.  Measured, us a step: bfloat16 large 1.55, small 0.5 (turned operands 0.52) where two share a
+// CU and 0.65 (0.7) where one has it alone; float 1.75.  A tile's end: 6, 2 and 4 us.  Sums of shares: written and read at 4 TB/s,
+// and a launch.  (us, the rule's choice and what stands beside it.  bfloat16: weight gradient 4096 x 1024 over 16384 rows, large
+// tiles in four shares 142, small in two 153, in one 173; input gradient 1024 x 8192 over 8192, small 132, large in two shares 141; 300 x
+// 4096 over 4096, small in two shares 35, in one 42, large 51 at best; weight gradient 5000 x 2000 over 3000 rows, large 72, small
+// 83.  Float: 4096 x 1000 over 512, one share 48, two 67; 300 x 4096 over 4096, five shares 122, one 257, eight 128.)
 void choose_tiles(GemmKind kind, int64_t m, int64_t n, int64_t steps, cat_dtype dt, bool& large, int& splits) {
     double best = -1.0;
     for (int l = 0; l < (dt == CAT_BF16 ? 2 : 1); l++) {
@@ -219,7 +220,7 @@ void choose_tiles(GemmKind kind, int64_t m, int64_t n, int64_t steps, cat_dtype 
         const double end = dt == CAT_F32 ? 4.0 : l ? 6.0 : 2.0;
         for (int s = 1; s <= 32 && (s == 1 || steps / s >= 4); s++) {
             const int64_t rounds = (tiles * s + 255) / 256;
-            const double step = dt == CAT_F32 ? 1.75 : l ? (kind == kForward ? 1.55 : 1.7) : kind == kForward ? (rounds > 1 ? 0.5 : 0.65) : (rounds > 1 ? 0.6 : 0.8);
+            const double step = dt == CAT_F32 ? 1.75 : l ? 1.55 : kind == kForward ? (rounds > 1 ? 0.5 : 0.65) : (rounds > 1 ? 0.52 : 0.7);
             const double us = rounds * (((steps + s - 1) / s) * step + end) + (s > 1 ? 4.0 + (double)s * m * n * 2e-6 : 0.0);
             if (best < 0.0 || us < best) best = us, large = l, splits = s;
             if (rounds > 2 && s > 1) break;  // (more shares only add to what is joined)
