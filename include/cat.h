@@ -613,7 +613,8 @@ size_t cat_debug_pca_route_offset(int64_t N, int64_t D, int32_t p, cat_dtype dt,
  * 0.044715 z^3))), CAT_ACT_SILU z / (1 + exp(-z)).  The derivative of CAT_ACT_RELU at 0 is 0.
  * One size of workspace covers both gradients of a product.  M, N (rows), K and D stay below 2^31; offsets are 64-bit.
  * Errors: CAT_ERR_INVALID_ARG (shape, type, null or misaligned pointer, codes without scales, both or none of rows and
- * checkpoint, unknown activation, eps), CAT_ERR_WORKSPACE, CAT_ERR_DEVICE. */
+ * checkpoint, unknown activation, eps), CAT_ERR_UNSUPPORTED (products: K or N of more than 2^23 bytes a row), CAT_ERR_WORKSPACE,
+ * CAT_ERR_DEVICE. */
 #define CAT_PACK_GROUP 128
 typedef enum {
     CAT_ACT_NONE = 0,
