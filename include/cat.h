@@ -606,7 +606,9 @@ size_t cat_debug_pca_route_offset(int64_t N, int64_t D, int32_t p, cat_dtype dt,
  * cat_linear_backward_input   dx = (dy w) * act'(c): dy M x N, w N x K, dx M x K; c (M x K) the checkpoint of the rows whose
  *               activation was the product's input; without codes act must be CAT_ACT_NONE.
  * cat_linear_backward_weight  dw = dy^T u (N x K of dt), dbias = sum over rows of dy (N floats, nullable); u = x (M x K), or
- *               act(c) of a checkpoint c.  With bfloat16 rows u is rounded to bfloat16 for the matrix cores.
+ *               act(c) of a checkpoint c.  With bfloat16 rows act(c) is rounded to bfloat16 once more, as the rows were that the
+ *               product took forward (what is differentiated is the product of those).  With float rows it is not; a
+ *               checkpoint goes with either type, so dy given as float is the choice for a gradient without that rounding.
  * cat_activation_backward     dz = dy * act'(c), for an activation whose output goes elsewhere than into a product.
  *
  * Activations: CAT_ACT_GELU is z Phi(z) (erf), CAT_ACT_GELU_TANH its approximation 0.5 z (1 + tanh(sqrt(2 / pi) (z +

@@ -823,7 +823,9 @@ def cat_linear_backward_input(dy, w, act="none", packed=None, out=None, workspac
 
 def cat_linear_backward_weight(dy, x=None, packed=None, act="none", want_bias=True, out=None, workspace=None):
     """Gradients of a product's weight and bias (cat_linear_backward_weight) from its input ``x``, or from the checkpoint
-    ``packed`` of the rows whose ``act`` the input was.  Returns (dw, dbias), dbias float32, None without ``want_bias``."""
+    ``packed`` of the rows whose ``act`` the input was.  Returns (dw, dbias), dbias float32, None without ``want_bias``.
+    With a bfloat16 ``dy`` the activation is rounded to bfloat16 for the product, as the forward pass had it; with a float32
+    ``dy`` (a checkpoint goes with either) it is not, and dw is float32."""
     lib = load_library()
     M, N, dt = _rows(dy, "dy")
     given = x if x is not None else packed[0] if packed is not None else None
