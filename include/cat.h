@@ -612,7 +612,8 @@ size_t cat_debug_pca_route_offset(int64_t N, int64_t D, int32_t p, cat_dtype dt,
  * cat_activation_backward     dz = dy * act'(c), for an activation whose output goes elsewhere than into a product.
  *
  * Activations: CAT_ACT_GELU is z Phi(z) (erf), CAT_ACT_GELU_TANH its approximation 0.5 z (1 + tanh(sqrt(2 / pi) (z +
- * 0.044715 z^3))), CAT_ACT_SILU z / (1 + exp(-z)).  The derivative of CAT_ACT_RELU at 0 is 0.
+ * 0.044715 z^3))), CAT_ACT_SILU z / (1 + exp(-z)); of -infinity these are NaN (-inf * 0), of infinity infinity.  The derivative
+ * of CAT_ACT_RELU at 0 is 0.
  * One size of workspace covers both gradients of a product.  M, N (rows), K and D stay below 2^31; offsets are 64-bit.
  * Errors: CAT_ERR_INVALID_ARG (shape, type, null or misaligned pointer, codes without scales, both or none of rows and
  * checkpoint, unknown activation, eps), CAT_ERR_UNSUPPORTED (products: K or N of more than 2^23 bytes a row), CAT_ERR_WORKSPACE,

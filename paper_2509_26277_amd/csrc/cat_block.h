@@ -202,8 +202,9 @@ __device__ __forceinline__ void ld_codes(const int8_t* row, int64_t j, int64_t D
 
 // ---- activations ----
 // In fp32 throughout.  The saturated ends come out of the exponentials by themselves (exp -> inf gives 1 / inf = 0); a NaN
-// stays.  FAST, for bfloat16 results: the epilogue of a product is bound by these instructions (its matrix cores wait), and
-// the library's erf is some forty of them.
+// stays, and of -infinity GELU and SiLU are -inf * 0, a NaN, whatever the type (a sum that left the floats is not hidden).
+// FAST, for bfloat16 results: the epilogue of a product is bound by these instructions (its matrix cores wait), and the
+// library's erf is some forty of them.
 __device__ __forceinline__ float logistic(float z) { return __fdividef(1.f, 1.f + __expf(-z)); }
 constexpr float kInvSqrt2 = 0.70710678118654752f, kInvSqrt2Pi = 0.39894228040143268f;
 constexpr float kTanhIn = 0.79788456080286536f, kTanhCube = 0.044715f;
@@ -228,7 +229,7 @@ __device__ __forceinline__ float act_value(float z) {
     if constexpr (ACT == CAT_ACT_RELU) {
         return z > 0.f ? z : (z != z ? z : 0.f);
     } else if constexpr (ACT == CAT_ACT_GELU && FAST) {  // z - z Phi(-z), or z Phi(z)
-        const float x = fminf(fabsf(z), 1e30f);           // (no inf * 0)
+        const float x = fabsf(fminf(z, 1e30f));           // (no inf * 0 for +inf)
         return fmaf(-x, normal_exp(z) * tail_factor(x), fmaxf(z, 0.f));
     } else if constexpr (ACT == CAT_ACT_GELU) {
         return 0.5f * z * (1.f + erff(z * kInvSqrt2));

@@ -1,13 +1,18 @@
 """The block's operators at values where formulas end: infinities, the largest floats, groups that hold a NaN, and activations
 of either type at their precision."""
+import math
+
 import pytest
 import torch
 
-from paper_2509_26277_amd import cat_linear_backward_weight, cat_pack8
+from paper_2509_26277_amd import cat_linear, cat_linear_backward_weight, cat_pack8
 
-from block_util import ACT_ERR, U32, act_ref, assert_close, half_step, unpack_ref
+from block_util import ACT_ERR, ACTS, TYPES, U32, act_ref, assert_close, half_step, unpack_ref
 
 pytestmark = pytest.mark.gpu
+
+INF, NAN = float("inf"), float("nan")
+FAR = [INF, -INF, NAN, 3e38, -3e38, 1e20, -1e20, 1000.0, -1000.0, 200.0, -200.0, 90.0, -90.0, 50.0, -50.0]
 
 
 def test_a_checkpoint_s_activation_in_either_type():
@@ -30,3 +35,24 @@ def test_a_checkpoint_s_activation_in_either_type():
     border = dy.double().cpu().abs().t() @ ((u + off).bfloat16().double() - (u - off).bfloat16().double())
     got = cat_linear_backward_weight(dy, packed=packed, act="gelu", want_bias=False)[0]
     assert_close(got, rounded, half_step(torch.bfloat16) * rounded.abs() + err + border, "bfloat16 rows")
+
+
+@pytest.mark.parametrize("N", [128, 131])
+@pytest.mark.parametrize("M", [15, 150])
+@pytest.mark.parametrize("act", ACTS)
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_values_far_out(dtype, act, M, N):
+    """One activation, whatever the type and the kernel: of -infinity GELU and SiLU are -inf * 0, a NaN."""
+    z = torch.tensor(FAR).repeat(M // len(FAR))[:, None].to(TYPES[dtype]).cuda()
+    y = cat_linear(z, torch.ones(N, 1, dtype=z.dtype, device="cuda"), act=act).double().cpu()
+    z = z.double().cpu()[:, 0]
+    for i in range(M):
+        v, got = float(z[i]), y[i]
+        if v != v or (v == -INF and act not in ("none", "relu")):
+            assert bool(torch.isnan(got).all()), (act, v, got[0])
+        elif act == "none" or v > 0:
+            # (50 and more: the logistic function and the normal distribution are one but for less than a half step)
+            assert bool((got == v).all()) if math.isinf(v) or act in ("none", "relu") else bool(
+                ((got - v).abs() <= (4 * U32 + half_step(TYPES[dtype])) * v).all()), (act, v, got[0])
+        else:
+            assert bool((got.abs() < 1e-18).all()), (act, v, got[0])  # (50 e^-50 is 1e-20)
