@@ -205,7 +205,15 @@ __device__ __forceinline__ void ld_codes(const int8_t* row, int64_t j, int64_t D
 // stays, and of -infinity GELU and SiLU are -inf * 0, a NaN, whatever the type (a sum that left the floats is not hidden).
 // FAST, for bfloat16 results: the epilogue of a product is bound by these instructions (its matrix cores wait), and the
 // library's erf is some forty of them.
-__device__ __forceinline__ float logistic(float z) { return __fdividef(1.f, 1.f + __expf(-z)); }
+// The hardware's exponential is off by half a step of fp32 for every unit of its argument: nothing to a bfloat16 result, but 44
+// half steps of a float SiLU at z = -80, which therefore takes the library's and the correctly rounded quotient (us, derivative
+// of 65536 x 1000: 113 -> 121).  The other float forms keep it, being no worse for it: over [-9, 9] GELU' is off by 1.9 half
+// steps of one (1.8 with an exact exponential), tanh GELU by 157 of its value (149: the rounding of its cubic argument).
+template <bool HARDWARE>
+__device__ __forceinline__ float logistic(float z) {
+    if constexpr (HARDWARE) return __fdividef(1.f, 1.f + __expf(-z));
+    else return __fdiv_rn(1.f, 1.f + expf(-z));
+}
 constexpr float kInvSqrt2 = 0.70710678118654752f, kInvSqrt2Pi = 0.39894228040143268f;
 constexpr float kTanhIn = 0.79788456080286536f, kTanhCube = 0.044715f;
 // gelu with tanh: 0.5 z (1 + tanh u) = z * logistic(2 u), u = sqrt(2 / pi) (z + 0.044715 z^3)
@@ -234,9 +242,9 @@ __device__ __forceinline__ float act_value(float z) {
     } else if constexpr (ACT == CAT_ACT_GELU) {
         return 0.5f * z * (1.f + erff(z * kInvSqrt2));
     } else if constexpr (ACT == CAT_ACT_GELU_TANH) {
-        return z * logistic(tanh_arg2(z));
+        return z * logistic<true>(tanh_arg2(z));
     } else if constexpr (ACT == CAT_ACT_SILU) {
-        return z * logistic(z);
+        return z * logistic<FAST>(z);
     } else {
         return z;
     }
@@ -252,10 +260,10 @@ __device__ __forceinline__ float act_grad(float z) {
         return fmaf(z * kInvSqrt2Pi, __expf(-0.5f * z * z), 0.5f * (1.f + erff(z * kInvSqrt2)));
     } else if constexpr (ACT == CAT_ACT_GELU_TANH) {
         // (beyond |z| = 32 the factor p (1 - p) is zero in fp32, and z * z must not turn it into 0 * inf)
-        const float p = logistic(tanh_arg2(z)), c = fminf(fmaxf(z, -32.f), 32.f);
+        const float p = logistic<true>(tanh_arg2(z)), c = fminf(fmaxf(z, -32.f), 32.f);
         return fmaf(c * p * (1.f - p), 2.f * kTanhIn * fmaf(3.f * kTanhCube * c, c, 1.f), p);
     } else if constexpr (ACT == CAT_ACT_SILU) {
-        const float p = logistic(z);
+        const float p = logistic<FAST>(z);
         return p * fmaf(z, 1.f - p, 1.f);
     } else {
         return 1.f;

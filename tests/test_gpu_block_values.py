@@ -5,7 +5,7 @@ import math
 import pytest
 import torch
 
-from paper_2509_26277_amd import cat_linear, cat_linear_backward_weight, cat_pack8
+from paper_2509_26277_amd import cat_activation_backward, cat_linear, cat_linear_backward_weight, cat_pack8
 
 from block_util import ACT_ERR, ACTS, TYPES, U32, act_ref, assert_close, half_step, unpack_ref
 
@@ -56,3 +56,25 @@ def test_values_far_out(dtype, act, M, N):
                 ((got - v).abs() <= (4 * U32 + half_step(TYPES[dtype])) * v).all()), (act, v, got[0])
         else:
             assert bool((got.abs() < 1e-18).all()), (act, v, got[0])  # (50 e^-50 is 1e-20)
+
+
+@pytest.mark.parametrize("M", [25, 150])
+def test_silu_of_float_rows_is_a_float_silu(M):
+    """z / (1 + exp(-z)): two half steps of the exponential and one each of the sum, the quotient and the product, at any |z|."""
+    z = torch.linspace(-80.0, 80.0, M).reshape(M, 1).cuda()
+    want = act_ref(z.double().cpu(), "silu")[0].expand(M, 130)
+    got = cat_linear(z, torch.ones(130, 1, device="cuda"), act="silu")
+    assert_close(got, want, 8 * U32 * want.abs(), "silu")
+
+
+def test_derivative_of_silu_of_float_rows():
+    """p (1 + z (1 - p)), p = 1 / (1 + exp(-z)) as above: the inner sum is off by a few half steps of 1 + |z|."""
+    z = torch.linspace(-80.0, 80.0, 161).reshape(161, 1).cuda()  # (a row each: its checkpoint's scale is its own)
+    packed = cat_pack8(z)
+    held = unpack_ref(*packed).float().double()  # (the value that the kernel reads: code times scale, a float)
+    p = torch.sigmoid(held)
+    got = cat_activation_backward(torch.ones_like(z), packed, "silu")
+    assert_close(got, act_ref(held, "silu")[1], 8 * U32 * p * (1.0 + held.abs()), "silu'")
+    for act in ("gelu", "gelu_tanh"):
+        got = cat_activation_backward(torch.ones_like(z), packed, act)
+        assert_close(got, act_ref(held, act)[1], ACT_ERR * (1.0 + held.abs()), act)
