@@ -590,8 +590,9 @@ size_t cat_debug_pca_route_offset(int64_t N, int64_t D, int32_t p, cat_dtype dt,
  * cat_pack8     codes (N x D int8) and scales (N x ceil(D / 128) float) of x (N x D of dt).  128 consecutive channels of
  *               a row (CAT_PACK_GROUP; the last group may be shorter) share a scale s = a / 127, a the group's
  *               largest magnitude; a channel's code is the integer nearest to x * (127 / a), ties to even, and stands for
- *               code * s.  Both quotients and the product are rounded to float.  A group with a < 2^-100 is held as zeros;
- *               a NaN or an infinity makes all values of its group NaN.
+ *               code * s.  Both quotients and the product are rounded to float (s downwards for the largest float as a, so that
+ *               127 s is finite).  A group with a < 2^-100 is held as zeros; a NaN or an infinity makes all values of its
+ *               group NaN.
  * cat_unpack8   x = code * scale, rounded to dt.
  * cat_layer_norm         mu and v the mean and the (biased) variance of a row, rstd = 1 / sqrt(v + eps),
  *               y = (x - mu) * rstd * weight + bias.  weight, bias (D floats) nullable: 1 and 0.  mean, rstd (N floats)

@@ -141,7 +141,8 @@ __device__ __forceinline__ uint32_t lanes_max(uint32_t v) {
 // Groups of 128 consecutive channels of a row share a scale s = a / 127 with a the group's largest magnitude; a channel's
 // code is x * (127 / a), rounded to the nearest integer (ties to even), its value code * s.  Both quotients are correctly
 // rounded, so a group's codes do not depend on which kernel wrote them.  a < 2^-100 (where 127 / a comes near the largest
-// float): zeros.  A NaN or an infinity makes the group's scale one, and every value of the group NaN (0 * inf too).
+// float): zeros.  A NaN or an infinity makes the group's scale one, and every value of the group NaN (0 * inf too).  The
+// largest float's 127th, rounded up, times 127 would be an infinity: the float below it is that group's scale.
 constexpr int kPackGroup = CAT_PACK_GROUP;
 struct PackScale {
     float up, step;
@@ -151,7 +152,7 @@ __device__ __forceinline__ PackScale pack_scale(uint32_t magnitude) {
     PackScale s;
     const bool held = !(amax < 0x1p-100f);
     s.up = held ? __fdiv_rn(127.f, amax) : 0.f;
-    s.step = held ? __fdiv_rn(amax, 127.f) : 0.f;
+    s.step = magnitude == 0x7F7FFFFFu ? 0x1.020406p+121f : held ? __fdiv_rn(amax, 127.f) : 0.f;
     return s;
 }
 // Codes in the low bytes: |x| * (127 / a) rounds to at most 127, and the sum with 1.5 * 2^23, whose last place is 1, rounds it

@@ -5,7 +5,7 @@ import math
 import pytest
 import torch
 
-from paper_2509_26277_amd import cat_activation_backward, cat_linear, cat_linear_backward_weight, cat_pack8
+from paper_2509_26277_amd import cat_activation_backward, cat_layer_norm, cat_linear, cat_linear_backward_weight, cat_pack8, cat_unpack8
 
 from block_util import ACT_ERR, ACTS, TYPES, U32, act_ref, assert_close, half_step, unpack_ref
 
@@ -78,3 +78,30 @@ def test_derivative_of_silu_of_float_rows():
     for act in ("gelu", "gelu_tanh"):
         got = cat_activation_backward(torch.ones_like(z), packed, act)
         assert_close(got, act_ref(held, act)[1], ACT_ERR * (1.0 + held.abs()), act)
+
+
+LARGEST = torch.finfo(torch.float32).max
+
+
+def test_the_largest_float_comes_back_finite():
+    """As a mask's lowest value has it: 127 steps of a group's scale stay a float, from whichever kernel the group is."""
+    x = torch.ones(4, 300)
+    x[0, 5], x[1, 130], x[2, 299], x[2, 0] = LARGEST, -LARGEST, LARGEST, -LARGEST
+    x = x.cuda()
+    codes, scales = cat_pack8(x)
+    for t in TYPES.values():
+        y = cat_unpack8(codes, scales, dtype=t)
+        # (as bfloat16 the values round to the next power of two, which is infinity)
+        assert bool(torch.isfinite(cat_unpack8(codes, scales)).all())
+        assert torch.equal(y, cat_unpack8(codes, scales).to(t))
+    got = cat_unpack8(codes, scales).double().cpu()
+    want = x.double().cpu()
+    big = want.abs() > 1.0
+    assert bool(((got - want).abs()[big] <= 2.0 ** -22 * LARGEST).all())
+    assert bool((got[3] == 1.0).all())
+    packed = cat_layer_norm(x, pack=True)[3]
+    assert torch.equal(packed[0], codes) and torch.equal(packed[1], scales)
+    for M in (4, 68):  # through a product with the unit matrix
+        rows = x.repeat(M // 4, 1)
+        packed = cat_linear(rows, torch.eye(300, device="cuda"), pack=True)[1]
+        assert torch.equal(packed[0], codes.repeat(M // 4, 1)) and torch.equal(packed[1], scales.repeat(M // 4, 1))
