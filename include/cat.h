@@ -601,7 +601,8 @@ size_t cat_debug_pca_route_offset(int64_t N, int64_t D, int32_t p, cat_dtype dt,
  * cat_layer_norm_packed  y from the checkpoint of x and its saved mean and rstd.
  * cat_layer_norm_backward  with xhat = (x - mean) * rstd, g = dy * weight (x: the rows, or their checkpoint: one of the two):
  *               dx = rstd * (g - mean_row(g) - xhat * mean_row(g * xhat)) + residual_grad (nullable, N x D of dt),
- *               dweight = sum over rows of dy * xhat, dbias = sum over rows of dy (D floats, each nullable).
+ *               dweight = sum over rows of dy * xhat, dbias = sum over rows of dy (D floats, each nullable; without either a
+ *               workspace of 256 bytes is enough).
  * cat_linear    z = x w^T + bias (x: M x K, w: N x K, bias: N floats, nullable), y = act(z) + residual (M x N, nullable).
  *               codes, scales: both or neither, the checkpoint of z (of its fp32 values).
  * cat_linear_backward_input   dx = (dy w) * act'(c): dy M x N, w N x K, dx M x K; c (M x K) the checkpoint of the rows whose

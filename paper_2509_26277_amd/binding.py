@@ -777,7 +777,7 @@ def cat_layer_norm_backward(dy, mean, rstd, weight=None, x=None, packed=None, re
     dx = torch.empty_like(dy)
     dw, db = (torch.empty((D,), dtype=torch.float32, device=dy.device) if want_params else None for _ in range(2))
     if workspace is None:
-        workspace = _workspace(lib.cat_layer_norm_backward_workspace_bytes(N, D, dt), dy.device)
+        workspace = _workspace(lib.cat_layer_norm_backward_workspace_bytes(N, D, dt) if want_params else 256, dy.device)
     _check(lib.cat_layer_norm_backward(*args, dx.data_ptr(), None if dw is None else dw.data_ptr(), None if db is None else db.data_ptr(),
                                        workspace.data_ptr(), workspace.numel(), _stream()))
     return dx, dw, db

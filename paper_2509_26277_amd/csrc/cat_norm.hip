@@ -448,7 +448,7 @@ int norm_groups(int64_t N, NormShape s, int most) {
     return (int)(b < most ? b : most);
 }
 // long rows: shares of the rows that k_norm_columns takes
-constexpr int kColumnParts = 64;
+int column_parts(int64_t N) { return (int)(N < 64 ? N : 64); }
 
 unsigned norm_blocks(int64_t N) { return (unsigned)(N < kNormMaxBlocks ? N : kNormMaxBlocks); }
 
@@ -507,7 +507,7 @@ cat_status launch_norm_backward(const T* dy, const T* x, const int8_t* codes, co
                            weight, radd, dx);
         CAT_LAUNCH_CHECK("k_norm_backward_long");
         if (parts) {
-            P = (int)(N < kColumnParts ? N : kColumnParts);
+            P = column_parts(N);
             hipLaunchKernelGGL((k_norm_columns<T, FROM8>), dim3((unsigned)((D + kNormThreads - 1) / kNormThreads), (unsigned)P), dim3(kNormThreads), 0,
                                st, dy, x, codes, scales, mean, rstd, N, D, parts);
         }
@@ -569,7 +569,7 @@ cat_status cat_layer_norm_packed(const int8_t* codes, const float* scales, const
 size_t cat_layer_norm_backward_workspace_bytes(int64_t N, int64_t D, cat_dtype dt) {
     if (check_rows("cat_layer_norm_backward_workspace_bytes", N, D, dt) != CAT_OK) return 0;
     const NormShape s = dt == CAT_F32 ? norm_shape<float, true>(D) : norm_shape<bf16_t, true>(D);
-    const int P = s.tpr ? norm_groups(N, s, kNormParts) : kColumnParts;
+    const int P = s.tpr ? norm_groups(N, s, kNormParts) : column_parts(N);
     return ((size_t)(P > 0 ? P : 1) * 2 * (size_t)D * sizeof(float) + 255) & ~(size_t)255;
 }
 
@@ -591,7 +591,8 @@ cat_status cat_layer_norm_backward(const void* dy, const void* x, const int8_t* 
     CAT_TRY(check_ptr(who, "dweight", dweight, false));
     CAT_TRY(check_ptr(who, "dbias", dbias, false));
     if (N > 0 && (dx == dy || dx == x || dx == residual_grad)) return set_error(CAT_ERR_INVALID_ARG, "%s: dx may not alias an input", who);
-    CAT_TRY(check_workspace(who, workspace, workspace_bytes, cat_layer_norm_backward_workspace_bytes(N, D, dt)));
+    // (the workspace holds the parts of the parameters' gradients alone)
+    CAT_TRY(check_workspace(who, workspace, workspace_bytes, dweight || dbias ? cat_layer_norm_backward_workspace_bytes(N, D, dt) : 256));
     hipStream_t st = (hipStream_t)hip_stream;
     if (N == 0) {
         if (dweight) CAT_TRY(launch_fill_zero(dweight, (size_t)D * sizeof(float), st));
