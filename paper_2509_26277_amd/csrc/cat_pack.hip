@@ -33,30 +33,36 @@ cat_status check_workspace(const char* who, const void* ws, size_t have, size_t 
     return CAT_OK;
 }
 
-// Sums of the workgroups' parts (P x n), columns below `split` to `lo`, the others to `hi`: a workgroup 32 columns, its 32
-// half-waves every 32nd part each, a fixed order.  (512 parts of 2048 columns: see the measurements in the norm's file)
+// Sums of the workgroups' parts (P x n), columns below `split` to `lo`, the others to `hi`: a workgroup 32 columns at a time, its
+// 32 half-waves every 32nd part each, a fixed order.  (512 parts of 2048 columns: see the measurements in the norm's file)
 __global__ __launch_bounds__(1024) void k_sum_parts(const float* __restrict__ parts, int P, int64_t n, int64_t split, float* __restrict__ lo,
                                                     float* __restrict__ hi) {
     __shared__ float s[32][33];
     const int c = threadIdx.x % 32, h = threadIdx.x / 32;
-    const int64_t at = (int64_t)blockIdx.x * 32 + c;
-    float t = 0.f;
-    if (at < n) {
+    for (int64_t first = (int64_t)blockIdx.x * 32;;) {
+        const int64_t at = first + c;
+        float t = 0.f;
+        if (at < n) {
 #pragma unroll 8
-        for (int p = h; p < P; p += 32) t += parts[(int64_t)p * n + at];
-    }
-    s[h][c] = t;
-    __syncthreads();
-    t = s[c][h];  // the 32 sums of a column side by side
+            for (int p = h; p < P; p += 32) t += parts[(int64_t)p * n + at];
+        }
+        s[h][c] = t;
+        __syncthreads();
+        t = s[c][h];  // the 32 sums of a column side by side
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) t += __shfl_xor(t, o, 32);
-    const int64_t out = (int64_t)blockIdx.x * 32 + h;
-    if (c || out >= n) return;
-    float* to = out < split ? lo : hi;
-    if (to) to[out < split ? out : out - split] = t;
+        for (int o = 16; o > 0; o >>= 1) t += __shfl_xor(t, o, 32);
+        const int64_t out = first + h;
+        float* to = out < split ? lo : hi;
+        if (c == 0 && out < n && to) to[out < split ? out : out - split] = t;
+        first += (int64_t)gridDim.x * 32;
+        if (first >= n) break;
+        __syncthreads();
+    }
 }
+// (a launch has fewer than 2^32 threads: 2^21 workgroups, further columns by stride)
 cat_status launch_sum_parts(const float* parts, int P, int64_t n, int64_t split, float* lo, float* hi, hipStream_t st) {
-    hipLaunchKernelGGL(k_sum_parts, dim3((unsigned)((n + 31) / 32)), dim3(1024), 0, st, parts, P, n, split, lo, hi);
+    const int64_t blocks = (n + 31) / 32;
+    hipLaunchKernelGGL(k_sum_parts, dim3((unsigned)(blocks < (1 << 21) ? blocks : 1 << 21)), dim3(1024), 0, st, parts, P, n, split, lo, hi);
     CAT_LAUNCH_CHECK("k_sum_parts");
     return CAT_OK;
 }

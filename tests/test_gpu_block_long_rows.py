@@ -1,4 +1,4 @@
-"""The norm's backward pass of rows beyond 8192 entries: few rows, no parameters."""
+"""The norm's backward pass of rows beyond 8192 entries: few rows, more columns than a launch has threads for, no parameters."""
 import pytest
 import torch
 
@@ -21,7 +21,8 @@ def _case(N, D, dtype, seed):
     return x, dy, w
 
 
-@pytest.mark.parametrize("dtype,N,D", [("f32", 1, 9001), ("bf16", 3, 20002), ("bf16", 130, 8200), ("f32", 64, 8196)])
+# (2, 2^26 + 4): two sums for every column are more than 2^27, 32 of them a workgroup of 1024 threads
+@pytest.mark.parametrize("dtype,N,D", [("f32", 2, (1 << 26) + 4), ("f32", 1, 9001), ("bf16", 3, 20002), ("bf16", 130, 8200), ("f32", 64, 8196)])
 def test_sums_over_rows(dtype, N, D):
     """dweight and dbias: a column's N terms, each off by three roundings of xhat and one of its own, in a chain of N at most."""
     x, dy, w = _case(N, D, dtype, D)
