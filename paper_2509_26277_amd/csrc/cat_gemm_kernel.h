@@ -434,6 +434,7 @@ __global__ __launch_bounds__((TM / WM) * (TN / 128) * 64, 2) void k_gemm(const G
     begin();
 #pragma unroll
     for (int i = 0; i < 4; i++) sp.one(lds, wave, i), sq.one(lds + TN * kStepBytes, wave, i);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // (as before the barrier of a step below)
     __syncthreads();
     begin();
 #pragma unroll
