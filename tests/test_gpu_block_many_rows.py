@@ -10,7 +10,7 @@ from block_util import TYPES, U32, half_step
 pytestmark = pytest.mark.gpu
 
 # One length for each of the kernels (threads a row x 16-byte groups a thread).  A workgroup holds 256 / threads rows, one at
-# least, and there are 1024 of them forward, 512 backward: two and a half rounds forward and five backward, the last one begun.
+# least, and there are 1024 of them forward, 512 backward: two and a half rounds forward, five or more backward.
 LENGTHS = {"bf16": [(62, 8), (120, 16), (251, 32), (512, 64), (1000, 64), (2047, 64), (4001, 256), (8190, 256)],
            "f32": [(31, 8), (60, 16), (127, 32), (256, 64), (511, 64), (1001, 64), (2040, 64), (4001, 256), (8190, 256)]}
 CASES = [(t, D, (1024 * 256 // threads) * 5 // 2 + 3) for t in LENGTHS for D, threads in LENGTHS[t]]

@@ -105,3 +105,40 @@ def test_the_largest_float_comes_back_finite():
         rows = x.repeat(M // 4, 1)
         packed = cat_linear(rows, torch.eye(300, device="cuda"), pack=True)[1]
         assert torch.equal(packed[0], codes.repeat(M // 4, 1)) and torch.equal(packed[1], scales.repeat(M // 4, 1))
+
+
+@pytest.mark.parametrize("D", [300, 515, 3000, 9000])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_a_group_with_a_nan_or_an_infinity_from_the_norm(dtype, D):
+    """The definition's: scales of NaN or infinity, every value of the group a NaN, the other groups as they would be."""
+    x = torch.randn(5, D, generator=torch.Generator().manual_seed(D)).to(TYPES[dtype]).cuda()
+    clean = cat_pack8(x)
+    x[1, 130], x[2, D - 1], x[3, 0] = NAN, -INF, INF
+    packed = cat_layer_norm(x, pack=True)[3]
+    alone = cat_pack8(x)
+    bad = torch.zeros(5, -(-D // 128), dtype=torch.bool, device="cuda")
+    bad[1, 1] = bad[2, -1] = bad[3, 0] = True
+    per = bad.repeat_interleave(128, 1)[:, :D]
+    for codes, scales in (packed, alone):
+        assert torch.equal(codes[~per], clean[0][~per]) and torch.equal(scales[~bad], clean[1][~bad])
+        assert not bool(torch.isfinite(scales[bad]).any())
+        assert torch.equal(torch.isnan(cat_unpack8(codes, scales)), per)
+
+
+@pytest.mark.parametrize("M,N,K", [(5, 300, 40), (200, 300, 40), (200, 304, 2048), (600, 1024, 64)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_a_group_with_a_nan_or_an_infinity_from_a_product(dtype, M, N, K):
+    g = torch.Generator().manual_seed(N)
+    x, w = (torch.randn(r, K, generator=g).to(TYPES[dtype]).cuda() for r in (M, N))
+    y0, clean = cat_linear(x, w, pack=True)
+    x[3, 7], w[140, 0] = NAN, INF
+    y, (codes, scales) = cat_linear(x, w, pack=True)
+    bad = torch.zeros(M, -(-N // 128), dtype=torch.bool, device="cuda")
+    bad[3] = bad[:, 1] = True
+    per = bad.repeat_interleave(128, 1)[:, :N]
+    assert torch.equal(codes[~per], clean[0][~per]) and torch.equal(scales[~bad], clean[1][~bad])
+    assert not bool(torch.isfinite(scales[bad]).any())
+    assert torch.equal(torch.isnan(cat_unpack8(codes, scales)), per)
+    hit = torch.zeros(M, N, dtype=torch.bool, device="cuda")
+    hit[3] = hit[:, 140] = True
+    assert torch.equal(y[~hit], y0[~hit]) and bool(torch.isnan(y[3]).all())
