@@ -214,8 +214,10 @@ def _dev(t, dtype=None, shape=None, name="tensor"):
 
 
 def _stream():
-    """The current stream's handle, without the Stream object around it (2.5 us of a small call's 13)."""
-    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+    """The current stream's handle; where this torch gives it by itself, without the Stream object around it (2.5 us of a small
+    call's 13)."""
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return torch.cuda.current_stream().cuda_stream if raw is None else raw(torch.cuda.current_device())
 
 
 def select_path(path):
