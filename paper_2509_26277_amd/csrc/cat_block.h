@@ -12,7 +12,6 @@ namespace cat {
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-typedef short i16x8 __attribute__((ext_vector_type(8)));
 
 // Two floats to two bfloat16 values, ties to even; NaN and infinities stay what they are (one v_cvt_pk_bf16_f32).
 __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {

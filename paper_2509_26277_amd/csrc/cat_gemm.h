@@ -41,8 +41,8 @@ struct GemmArgs {
 
 constexpr int64_t kGemmMaxRowBytes = 1 << 23;  // offsets inside a tile of 256 rows stay below 2^31
 
-// E (4 or 8) neighbouring entries of a row of out, from column n on (a multiple of E), through the epilogue (BIAS: theirs is not in the sums yet).  PACK: the 16
-// lanes of a DPP row hold 128 columns of one row of out, all of them active.
+// E (4 or 8) neighbouring entries of a row of out, from column n on (a multiple of E), through the epilogue.  PACK: the 16 lanes of
+// a DPP row hold 128 columns of one row of out, all of them active.
 template <typename T, int E>
 __device__ __forceinline__ void ld_entries(const T* row, int64_t n, int64_t N, float (&v)[E]) {
     if constexpr (E == kVec<T>) {
@@ -72,11 +72,11 @@ __device__ __forceinline__ void st_entries(T* row, int64_t n, int64_t N, const f
             if (n + e < N) st_round(row + n + e, v[e]);
     }
 }
-template <typename T, int KIND, int E, bool PACK, bool BIAS = true>
+template <typename T, int KIND, int E, bool PACK>
 __device__ __forceinline__ void finish(const Epilogue& e, int64_t m, int64_t n, int64_t N, bool valid, float (&v)[E]) {
     const int64_t at = m * N;
     if constexpr (KIND == kForward) {
-        if (BIAS && e.bias) {
+        if (e.bias) {
             float b[E];
             ld_params<E>(e.bias, valid ? n : 0, N, 0.f, b);
 #pragma unroll

@@ -44,7 +44,7 @@ __device__ __forceinline__ f32x4 few_multiply(f32x4 a, f32x4 b, f32x4 c) {
 }
 template <typename T, int MB>
 __global__ __launch_bounds__(kFewWaves * kWave) void k_few_rows(const T* __restrict__ x, const T* __restrict__ w, int64_t M, int64_t N, int64_t K,
-                                                                int64_t k_split, int splits, float* __restrict__ parts, const Epilogue e) {
+                                                                int64_t k_split, float* __restrict__ parts, const Epilogue e) {
     constexpr int kStep = 4 * kVec<T>, U = MB == 1 ? 8 : 4;
     __shared__ f32x4 sums[kFewWaves][MB][kWave];
     const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave, r = lane & 15, g = lane >> 4;
@@ -345,11 +345,11 @@ cat_status few_rows(const Plan& pl, const void* x, const void* w, int64_t M, int
     const dim3 grid((unsigned)((N + 15) / 16), (unsigned)pl.splits), block(kFewWaves * kWave);
     float* parts = pl.splits > 1 || e.codes_out ? (float*)(ws + pl.at_parts) : nullptr;
     if (M <= 16)
-        hipLaunchKernelGGL((k_few_rows<T, 1>), grid, block, 0, st, (const T*)x, (const T*)w, M, N, K, pl.k_split, pl.splits, parts, e);
+        hipLaunchKernelGGL((k_few_rows<T, 1>), grid, block, 0, st, (const T*)x, (const T*)w, M, N, K, pl.k_split, parts, e);
     else if (M <= 32)
-        hipLaunchKernelGGL((k_few_rows<T, 2>), grid, block, 0, st, (const T*)x, (const T*)w, M, N, K, pl.k_split, pl.splits, parts, e);
+        hipLaunchKernelGGL((k_few_rows<T, 2>), grid, block, 0, st, (const T*)x, (const T*)w, M, N, K, pl.k_split, parts, e);
     else
-        hipLaunchKernelGGL((k_few_rows<T, 4>), grid, block, 0, st, (const T*)x, (const T*)w, M, N, K, pl.k_split, pl.splits, parts, e);
+        hipLaunchKernelGGL((k_few_rows<T, 4>), grid, block, 0, st, (const T*)x, (const T*)w, M, N, K, pl.k_split, parts, e);
     CAT_LAUNCH_CHECK("k_few_rows");
     return parts ? join<T, kForward>(parts, pl.splits, M, N, e, st) : CAT_OK;
 }

@@ -7,8 +7,9 @@
 //
 // All of it is bound by memory: a row is read once, stays in registers for both of its statistics (the variance is that
 // of the centred entries, not a difference of large sums) and for the result.  TPR threads share a row, each with VPL
-// 16-byte groups of it: 8 lanes for the shortest rows (8 rows a wave), a wave up to four groups a lane, a workgroup of
-// four waves (sums over LDS) up to 8192 entries, and beyond that a workgroup that reads the row again for every use.
+// 16-byte groups of it: 8 lanes for the shortest rows (8 rows a wave); forward a wave up to 2048 entries (32 a lane) and a
+// workgroup of four waves (sums over LDS) up to 8192; backward, with its sums and two or three rows ahead, a wave up to 1024,
+// four waves up to 4096 and eight up to 8192.  Longer rows have a workgroup each that reads the row again for every use.
 //
 // Measured, with a large copy at 5.2 TB/s: forward 131072 x 2048 bf16 200 us (5.4 TB/s); 65536 x 1024 bf16 forward with
 // checkpoint 64 us (5.2), backward from it 97 us (4.9) and 5 us for its sums; 16411 x 1001 fp32 42 us (3.5) and 58 us (3.7): few
