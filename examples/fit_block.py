@@ -1,8 +1,9 @@
-"""Fits a weight-quantised transformer block to its full-precision outputs, then corrects what is left cluster by cluster.
+"""Fits the weight-quantised feed-forward half of a transformer block to its full-precision outputs, then corrects what is left
+cluster by cluster.
 
     python examples/fit_block.py [--rows 8192] [--dim 256] [--steps 40] [--bits 4]
 
-The block (norm, two products, residual; ``paper_2509_26277_amd/block.py``) runs in bfloat16 with weights of a few bits a
+The half block (norm, two products, residual; ``paper_2509_26277_amd/block.py``) runs in bfloat16 with weights of a few bits a
 row; its gradients come from checkpoints in 8 bits and go straight through the quantiser to the float weights.  The
 outputs of the fitted block are the low-bit rows of ``cat_fit``, those of the full-precision block its targets.  Weights and
 calibration rows are drawn at random.  Prints the mean squared error to the full-precision outputs after each stage.

@@ -575,11 +575,11 @@ cat_status cat_debug_pca_patience(int64_t looks);
 enum { CAT_PCA_COLUMNS = 0, CAT_PCA_ALONE = 1, CAT_PCA_GRID = 2 };
 size_t cat_debug_pca_route_offset(int64_t N, int64_t D, int32_t p, cat_dtype dt, int32_t sweeps);
 
-/* ---- a transformer block's training step, with its activations kept in 8 bits ----
- * Transformers are quantised block by block: the block's parameters are fitted on the calibration rows, and the rows that
- * the fitted network gives are the LQ rows of cat_fit (App. H of the paper: ViT, DeiT, Swin).  These are the operators of
- * such a step: layer norm, the product with bias, activation and residual, their gradients, and checkpoints in 8 bits
- * of what the backward passes read again.
+/* ---- the feed-forward half of a transformer block's training step, with its activations kept in 8 bits ----
+ * The networks whose outputs are corrected are transformers among others (App. H of the paper: ViT, DeiT, Swin).  These are
+ * the operators with which the feed-forward half of a block is fitted on calibration rows, its outputs then being the LQ rows
+ * of cat_fit: layer norm, the product with bias, activation and residual, their gradients, and checkpoints in 8 bits of what
+ * the backward passes read again.  Attention and a quantiser's own gradients are not among them.
  *
  * Beside the conventions at the top: zero rows are allowed (sums over rows are then zero, arrays of rows may be NULL); a row may have any length,
  * also an odd number of bfloat16 entries; every array that is given starts on a 16-byte boundary; parameters of the

@@ -16,8 +16,8 @@
 // Measured (TFLOP/s; a library product of 8192^3: bfloat16 1385, float 154).  bfloat16, tiles of 256 x 256: forward 8192^3 1400 to
 // 1490, 4096^3 1370 to 1410; input gradient 8192^3 1380, weight gradient 1360 (1260 and 1220 with the places of both operands two
 // chunks apart, where paired tiles met on the same banks).  Float: 2048^3 128.  The matrix cores are busy in 57 % of the cycles of
-// 16384 x 8192 over 2048 with GELU, at 1.95 GHz; what comes on top of the steps is the epilogue, whose instructions they wait for:
-// GELU 30 to 55 us there, its derivative 35 of 16384 x 4096 over 1024.  (Through LDS, 16 rows at a time, a tile's epilogue took 11 to
+// 16384 x 8192 over 2048 with GELU, at 2.0 GHz; what comes on top of the steps is the epilogue, whose instructions they wait for:
+// GELU 21 us of 16384 x 4096 over 1024 (126 without), codes 14, a derivative 40 (121 without).  (Through LDS, 16 rows at a time, a tile's epilogue took 11 to
 // 27 us, as long as 8 to 16 steps of k.)
 #pragma once
 #include "cat_gemm.h"

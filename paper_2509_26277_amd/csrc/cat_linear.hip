@@ -16,7 +16,7 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 // ---- few rows ----
 // A workgroup takes 16 rows of w, its waves shares of k (blockIdx.y: shares of it).  w goes through the registers in the
 // layout of the matrix instruction's first operand, 64 bytes of a row a load; rows of x are the second operand, from the
-// caches.  The waves' sums meet in LDS.  (One row, 8192 x 2048 bf16: 8.2 us, 4.1 TB/s of w; the bytes alone 6.5.)
+// caches.  The waves' sums meet in LDS.  (One row, 8192 x 2048 bf16: 8.4 us, 4.0 TB/s of w; the bytes alone 6.5.)
 constexpr int kFewWaves = 4;
 template <typename T>
 __device__ __forceinline__ f32x4 few_load(const T* row, int64_t k, int64_t K) {

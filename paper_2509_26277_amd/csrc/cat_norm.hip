@@ -11,9 +11,10 @@
 // workgroup of four waves (sums over LDS) up to 8192; backward, with its sums and two or three rows ahead, a wave up to 1024,
 // four waves up to 4096 and eight up to 8192.  Longer rows have a workgroup each that reads the row again for every use.
 //
-// Measured, with a large copy at 5.2 TB/s: forward 131072 x 2048 bf16 200 us (5.4 TB/s); 65536 x 1024 bf16 forward with
-// checkpoint 64 us (5.2), backward from it 97 us (4.9) and 5 us for its sums; 16411 x 1001 fp32 42 us (3.5) and 58 us (3.7): few
-// rows a workgroup, so that starting and ending count.  One row: 4 us, a launch.
+// Measured, with a large copy at 5.2 TB/s: forward 131072 x 2048 bf16 201 us (5.3 TB/s); 65536 x 1024 bf16 forward with
+// checkpoint 58 us, backward from it 101 (4.7 TB/s) and 5 for its sums; fp32 the same rows 138 us (4.4) and 174 with its sums
+// (5.0).  16411 x 1001 fp32 41 us and 57 with the sums (3.6 and 3.7): 1000 columns take as long, 1024, where no lane stands idle,
+// 36 and 49.  One row: 4 us, a launch.
 #include "cat_block.h"
 
 namespace cat {
