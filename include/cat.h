@@ -593,7 +593,7 @@ size_t cat_debug_pca_route_offset(int64_t N, int64_t D, int32_t p, cat_dtype dt,
  *               code * s.  Both quotients and the product are rounded to float (s downwards for the largest float as a, so that
  *               127 s is finite).  A group with a < 2^-100 is held as zeros; a NaN or an infinity makes all values of its
  *               group NaN.
- * cat_unpack8   x = code * scale, rounded to dt.
+ * cat_unpack8   x = code * scale, rounded to dt.  codes may start anywhere, scales on a float's boundary.
  * cat_layer_norm         mu and v the mean and the (biased) variance of a row, rstd = 1 / sqrt(v + eps),
  *               y = (x - mu) * rstd * weight + bias.  weight, bias (D floats) nullable: 1 and 0.  mean, rstd (N floats)
  *               nullable.  codes, scales: both or neither, the checkpoint of x as cat_pack8 gives it.
@@ -654,6 +654,56 @@ cat_status cat_linear_backward_weight(const void *dy, const void *x, const int8_
                                       float *dbias, void *workspace, size_t workspace_bytes, void *hip_stream);
 cat_status cat_activation_backward(const void *dy, const int8_t *codes, const float *scales, int64_t N, int64_t D,
                                    cat_dtype dt, cat_activation act, void *dz, void *hip_stream);
+
+/* ---- the gated feed-forward half, and products of 8-bit integers ----
+ * The gated half of a block, act(x Wg^T + bg) * (x Wv^T + bv) through a last product, is fitted like the plain one above: the
+ * operators here stand in the place of cat_linear with an activation and of its gradients, the other products (the last one
+ * forward, the gradients of x and of w from dz) are cat_linear and cat_linear_backward_* as they are.  The products of 8-bit
+ * integers are those of the block when it runs quantised, its outputs being the LQ rows of cat_fit.
+ *
+ * Conventions, activations, NaN, alignment, zero rows and errors as for the operators above.  Arrays are contiguous; weights
+ * are N x K (2F x K: the F rows of the gate, then the F rows of the value), biases N (2F) floats, nullable.
+ *
+ * cat_quantize_rows  codes (N x D int8) and scales (N floats) of x (N x D of dt): a code is the integer nearest to
+ *               x * (127 / a), ties to even, a the row's largest magnitude, and stands for code * s, s = a / 127.  Roundings, rows
+ *               with a < 2^-100 (zeros), NaN and infinities (a row of NaN) as a group of cat_pack8 has them.  A weight goes
+ *               through it once, its rows being output channels.
+ * cat_layer_norm_quantize  the same of cat_layer_norm's y, before its rounding to dt.
+ * cat_linear8   z = (sum over k of x w) * x_scales * w_scales + bias, y = act(z) + residual (M x N of dt, nullable).  x: M x K, w:
+ *               N x K, any 8-bit integers (-128 too); the sums are exact, K at most 131071; x_scales: M floats, w_scales: N.
+ * cat_gated_linear   g and v the products of x (M x K) with the gate's and the value's rows of w, plus bias; y = act(g) * v (M x F).
+ *               codes, scales: both or neither, the checkpoints of g and of v (of their fp32 values), one behind the other: 2 x
+ *               M x F int8 and 2 x M x ceil(F / 128) floats, each half as cat_pack8 gives it.
+ * cat_gated_linear8  y = act(g) * v of 8-bit integers, x and w as for cat_linear8 (w_scales: 2F).
+ * cat_gated_backward_input   dh = dy w (dy: M x N, w: N x F, the last product's), dz (M x 2F of dt) = dh * v * act'(g) beside
+ *               dh * act(g), g and v from the checkpoints; dbias (2F floats, nullable): the sums over rows of dz, before its
+ *               rounding to dt.
+ * cat_gated_backward_weight  dw = dy^T (act(g) * v) (N x F of dt), dbias = sum over rows of dy (N floats, nullable).  With bfloat16
+ *               rows act(g) * v is rounded to bfloat16, as cat_linear_backward_weight has it.
+ * One size of workspace covers both gradients, and cat_gated_linear with and without checkpoints; F is below 2^23 bytes of dt.
+ * CAT_ERR_UNSUPPORTED also for K of more than 131071 8-bit integers. */
+cat_status cat_quantize_rows(const void *x, int64_t N, int64_t D, cat_dtype dt, int8_t *codes, float *scales, void *hip_stream);
+cat_status cat_layer_norm_quantize(const void *x, int64_t N, int64_t D, cat_dtype dt, const float *weight, const float *bias,
+                                   float eps, int8_t *codes, float *scales, void *hip_stream);
+size_t cat_linear8_workspace_bytes(int64_t M, int64_t N, int64_t K);
+cat_status cat_linear8(const int8_t *x, const float *x_scales, const int8_t *w, const float *w_scales, const float *bias,
+                       const void *residual, int64_t M, int64_t N, int64_t K, cat_dtype dt, cat_activation act, void *y,
+                       void *workspace, size_t workspace_bytes, void *hip_stream);
+size_t cat_gated_linear_workspace_bytes(int64_t M, int64_t F, int64_t K, cat_dtype dt);
+cat_status cat_gated_linear(const void *x, const void *w, const float *bias, int64_t M, int64_t F, int64_t K, cat_dtype dt,
+                            cat_activation act, void *y, int8_t *codes, float *scales, void *workspace,
+                            size_t workspace_bytes, void *hip_stream);
+size_t cat_gated_linear8_workspace_bytes(int64_t M, int64_t F, int64_t K);
+cat_status cat_gated_linear8(const int8_t *x, const float *x_scales, const int8_t *w, const float *w_scales,
+                             const float *bias, int64_t M, int64_t F, int64_t K, cat_dtype dt, cat_activation act, void *y,
+                             void *workspace, size_t workspace_bytes, void *hip_stream);
+size_t cat_gated_backward_workspace_bytes(int64_t M, int64_t N, int64_t F, cat_dtype dt);
+cat_status cat_gated_backward_input(const void *dy, const void *w, const int8_t *codes, const float *scales, int64_t M,
+                                    int64_t N, int64_t F, cat_dtype dt, cat_activation act, void *dz, float *dbias,
+                                    void *workspace, size_t workspace_bytes, void *hip_stream);
+cat_status cat_gated_backward_weight(const void *dy, const int8_t *codes, const float *scales, int64_t M, int64_t N,
+                                     int64_t F, cat_dtype dt, cat_activation act, void *dw, float *dbias, void *workspace,
+                                     size_t workspace_bytes, void *hip_stream);
 
 /* Message of the last non-OK status on the calling thread ("" if none).  The
  * pointer stays valid until the next failing call on the same thread. */

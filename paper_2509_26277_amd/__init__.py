@@ -35,6 +35,13 @@ from .binding import (  # noqa: F401
     cat_linear_backward_input,
     cat_linear_backward_weight,
     cat_activation_backward,
+    cat_quantize_rows,
+    cat_layer_norm_quantize,
+    cat_linear8,
+    cat_gated_linear,
+    cat_gated_linear8,
+    cat_gated_backward_input,
+    cat_gated_backward_weight,
     cat_fit_workspace_bytes,
     cat_apply_workspace_bytes,
     library_path,

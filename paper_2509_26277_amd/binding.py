@@ -34,7 +34,10 @@ EXPORTS = ("cat_select_path", "cat_fit_workspace_bytes", "cat_apply_workspace_by
            "cat_debug_pca_route_offset", "cat_stream_probe",
            "cat_pack8", "cat_unpack8", "cat_layer_norm", "cat_layer_norm_packed", "cat_layer_norm_backward_workspace_bytes",
            "cat_layer_norm_backward", "cat_linear_workspace_bytes", "cat_linear", "cat_linear_backward_workspace_bytes",
-           "cat_linear_backward_input", "cat_linear_backward_weight", "cat_activation_backward")
+           "cat_linear_backward_input", "cat_linear_backward_weight", "cat_activation_backward",
+           "cat_quantize_rows", "cat_layer_norm_quantize", "cat_linear8_workspace_bytes", "cat_linear8",
+           "cat_gated_linear_workspace_bytes", "cat_gated_linear", "cat_gated_linear8_workspace_bytes", "cat_gated_linear8",
+           "cat_gated_backward_workspace_bytes", "cat_gated_backward_input", "cat_gated_backward_weight")
 
 
 class CatError(RuntimeError):
@@ -182,6 +185,28 @@ def load_library():
     lib.cat_linear_backward_weight.restype = c.c_int
     lib.cat_activation_backward.argtypes = [vp, vp, vp, i64, i64, dt, c.c_int, vp, vp]
     lib.cat_activation_backward.restype = c.c_int
+    lib.cat_quantize_rows.argtypes = [vp, i64, i64, dt, vp, vp, vp]
+    lib.cat_quantize_rows.restype = c.c_int
+    lib.cat_layer_norm_quantize.argtypes = [vp, i64, i64, dt, vp, vp, f32, vp, vp, vp]
+    lib.cat_layer_norm_quantize.restype = c.c_int
+    lib.cat_linear8_workspace_bytes.argtypes = [i64, i64, i64]
+    lib.cat_linear8_workspace_bytes.restype = sz
+    lib.cat_linear8.argtypes = [vp, vp, vp, vp, vp, vp, i64, i64, i64, dt, c.c_int, vp, vp, sz, vp]
+    lib.cat_linear8.restype = c.c_int
+    lib.cat_gated_linear_workspace_bytes.argtypes = [i64, i64, i64, dt]
+    lib.cat_gated_linear_workspace_bytes.restype = sz
+    lib.cat_gated_linear.argtypes = [vp, vp, vp, i64, i64, i64, dt, c.c_int, vp, vp, vp, vp, sz, vp]
+    lib.cat_gated_linear.restype = c.c_int
+    lib.cat_gated_linear8_workspace_bytes.argtypes = [i64, i64, i64]
+    lib.cat_gated_linear8_workspace_bytes.restype = sz
+    lib.cat_gated_linear8.argtypes = [vp, vp, vp, vp, vp, i64, i64, i64, dt, c.c_int, vp, vp, sz, vp]
+    lib.cat_gated_linear8.restype = c.c_int
+    lib.cat_gated_backward_workspace_bytes.argtypes = [i64, i64, i64, dt]
+    lib.cat_gated_backward_workspace_bytes.restype = sz
+    lib.cat_gated_backward_input.argtypes = [vp, vp, vp, vp, i64, i64, i64, dt, c.c_int, vp, vp, vp, sz, vp]
+    lib.cat_gated_backward_input.restype = c.c_int
+    lib.cat_gated_backward_weight.argtypes = [vp, vp, vp, i64, i64, i64, dt, c.c_int, vp, vp, vp, sz, vp]
+    lib.cat_gated_backward_weight.restype = c.c_int
     lib.cat_last_error.argtypes = []
     lib.cat_last_error.restype = c.c_char_p
     _lib = lib
@@ -855,3 +880,173 @@ def cat_activation_backward(dy, packed, act):
     dz = torch.empty_like(dy)
     _check(load_library().cat_activation_backward(pd, pc, ps, N, D, dt, _act(act), dz.data_ptr(), _stream()))
     return dz
+
+
+# ---------------------------------------------------------------------------
+# the gated feed-forward half, and products of 8-bit integers
+# ---------------------------------------------------------------------------
+def _one_device(*tensors):
+    """Refuses tensors that lie on another device than the current one, on whose stream the call would run."""
+    here = torch.cuda.current_device() if torch.cuda.is_available() else None
+    for t in tensors:
+        if t is not None and t.device.index != here:
+            raise ValueError(f"tensor on {t.device}, but the current device is cuda:{here}")
+
+
+def _out_type(dtype):
+    if dtype not in (torch.float32, torch.bfloat16):
+        raise TypeError(f"the result must be float32 or bfloat16, got {dtype}")
+    return CAT_F32 if dtype == torch.float32 else CAT_BF16
+
+
+def _two(t, name):
+    if t.dim() != 2:
+        raise ValueError(f"{name} must have two dimensions, got {tuple(t.shape)}")
+    return t.shape
+
+
+def _room(workspace, nbytes, device):
+    """The caller's workspace, or one of the stated size."""
+    if workspace is None:
+        return _workspace(nbytes, device)
+    if not workspace.is_cuda or not workspace.is_contiguous() or workspace.dtype != torch.uint8:
+        raise ValueError("workspace must be a contiguous device tensor of uint8")
+    return workspace
+
+
+def cat_quantize_rows(x):
+    """Rows to 8-bit integers with a scale a row (cat_quantize_rows): (codes, scales), codes of x's shape, row m standing for
+    ``codes[m] * scales[m]``.  A weight (its rows output channels) goes through it once."""
+    N, D, dt = _rows(x, "x")
+    px = _dev(x, name="x")
+    _one_device(x)
+    codes, scales = torch.empty((N, D), dtype=torch.int8, device=x.device), torch.empty((N,), dtype=torch.float32, device=x.device)
+    _check(load_library().cat_quantize_rows(px, N, D, dt, codes.data_ptr(), scales.data_ptr(), _stream()))
+    return codes, scales
+
+
+def cat_layer_norm_quantize(x, weight=None, bias=None, eps=1e-5):
+    """Layer norm of every row straight to 8-bit integers with a scale a row (cat_layer_norm_quantize): (codes, scales)."""
+    N, D, dt = _rows(x, "x")
+    px, pw, pb = _dev(x, name="x"), _dev(weight, torch.float32, (D,), "weight"), _dev(bias, torch.float32, (D,), "bias")
+    _one_device(x, weight, bias)
+    codes, scales = torch.empty((N, D), dtype=torch.int8, device=x.device), torch.empty((N,), dtype=torch.float32, device=x.device)
+    _check(load_library().cat_layer_norm_quantize(px, N, D, dt, pw, pb, float(eps), codes.data_ptr(), scales.data_ptr(), _stream()))
+    return codes, scales
+
+
+def cat_linear8(x, x_scales, w, w_scales, bias=None, act="none", residual=None, dtype=torch.bfloat16, out=None, workspace=None):
+    """act((x w^T) * x_scales * w_scales + bias) + residual of 8-bit integers x (M x K) and w (N x K) (cat_linear8), scales and
+    bias float32, residual and result (M x N) of ``dtype``, float32 or bfloat16."""
+    lib = load_library()
+    (M, K), N, dt = _two(x, "x"), _two(w, "w")[0], _out_type(dtype)
+    px, pw = _dev(x, torch.int8, name="x"), _dev(w, torch.int8, (N, K), "w")
+    ps, pt = _dev(x_scales, torch.float32, (M,), "x_scales"), _dev(w_scales, torch.float32, (N,), "w_scales")
+    pb, pr = _dev(bias, torch.float32, (N,), "bias"), _dev(residual, dtype, (M, N), "residual")
+    act = _act(act)
+    if out is None:
+        out = torch.empty((M, N), dtype=dtype, device=x.device)
+    workspace = _room(workspace, lib.cat_linear8_workspace_bytes(M, N, K), x.device)
+    _one_device(x, x_scales, w, w_scales, bias, residual, out, workspace)
+    _check(lib.cat_linear8(px, ps, pw, pt, pb, pr, M, N, K, dt, act, _dev(out, dtype, (M, N), "out"), workspace.data_ptr(), workspace.numel(),
+                           _stream()))
+    return out
+
+
+def _halves(w, name):
+    """(F, K) of the gate's and the value's rows one behind the other."""
+    rows, K = _two(w, name)
+    if rows % 2:
+        raise ValueError(f"{name} must have two rows for every channel, the gate's and the value's, got {rows}")
+    return rows // 2, K
+
+
+def cat_gated_linear(x, w, bias=None, act="silu", pack=False, out=None, workspace=None):
+    """act(g) * v with g and v the products of x (M x K) and the first and the last F rows of w (2F x K), plus bias (2F,
+    float32) (cat_gated_linear).  Returns y (M x F); with ``pack`` (y, packed), ``packed`` the checkpoints of g and v that the
+    gradients take: codes (2 x M x F) and scales, each half as cat_unpack8 takes it."""
+    lib = load_library()
+    M, K, dt = _rows(x, "x")
+    F = _halves(w, "w")[0]
+    px, pw, pb = _dev(x, name="x"), _dev(w, x.dtype, (2 * F, K), "w"), _dev(bias, torch.float32, (2 * F,), "bias")
+    act = _act(act)
+    if out is None:
+        out = torch.empty((M, F), dtype=x.dtype, device=x.device)
+    packed = _empty_gate(M, F, x.device) if pack else None
+    pc, ps = (packed[0].data_ptr(), packed[1].data_ptr()) if pack else (None, None)
+    workspace = _room(workspace, lib.cat_gated_linear_workspace_bytes(M, F, K, dt), x.device)
+    _one_device(x, w, bias, out, workspace)
+    _check(lib.cat_gated_linear(px, pw, pb, M, F, K, dt, act, _dev(out, x.dtype, (M, F), "out"), pc, ps, workspace.data_ptr(), workspace.numel(),
+                                _stream()))
+    return (out, packed) if pack else out
+
+
+def cat_gated_linear8(x, x_scales, w, w_scales, bias=None, act="silu", dtype=torch.bfloat16, out=None, workspace=None):
+    """cat_gated_linear of 8-bit integers x (M x K) and w (2F x K) with their scales (cat_gated_linear8); the result (M x F) is of
+    ``dtype``, float32 or bfloat16."""
+    lib = load_library()
+    (M, K), F, dt = _two(x, "x"), _halves(w, "w")[0], _out_type(dtype)
+    px, pw = _dev(x, torch.int8, name="x"), _dev(w, torch.int8, (2 * F, K), "w")
+    ps, pt = _dev(x_scales, torch.float32, (M,), "x_scales"), _dev(w_scales, torch.float32, (2 * F,), "w_scales")
+    pb = _dev(bias, torch.float32, (2 * F,), "bias")
+    act = _act(act)
+    if out is None:
+        out = torch.empty((M, F), dtype=dtype, device=x.device)
+    workspace = _room(workspace, lib.cat_gated_linear8_workspace_bytes(M, F, K), x.device)
+    _one_device(x, x_scales, w, w_scales, bias, out, workspace)
+    _check(lib.cat_gated_linear8(px, ps, pw, pt, pb, M, F, K, dt, act, _dev(out, dtype, (M, F), "out"), workspace.data_ptr(), workspace.numel(),
+                                 _stream()))
+    return out
+
+
+def _empty_gate(M, F, device):
+    return (torch.empty((2, M, F), dtype=torch.int8, device=device),
+            torch.empty((2, M, (F + CAT_PACK_GROUP - 1) // CAT_PACK_GROUP), dtype=torch.float32, device=device))
+
+
+def _gate(packed, M, F=None):
+    """F and the pointers of the checkpoints of a gate and its value."""
+    codes, scales = packed
+    if codes.dim() != 3:
+        raise ValueError(f"codes must have three dimensions, got {tuple(codes.shape)}")
+    F = codes.shape[2] if F is None else F
+    return (F, _dev(codes, torch.int8, (2, M, F), "codes"),
+            _dev(scales, torch.float32, (2, M, (F + CAT_PACK_GROUP - 1) // CAT_PACK_GROUP), "scales"))
+
+
+def cat_gated_backward_input(dy, w, packed, act="silu", want_bias=True, out=None, workspace=None):
+    """Gradients of both projections of a gate (cat_gated_backward_input), from the gradient ``dy`` (M x N) of the product of
+    act(g) * v with w (N x F) and the checkpoints of g and v.  Returns (dz, dbias): dz (M x 2F) that of g beside that of v, dbias
+    (2F, float32) its sums over rows, None without ``want_bias``."""
+    lib = load_library()
+    M, N, dt = _rows(dy, "dy")
+    pd, pw = _dev(dy, name="dy"), _dev(w, dy.dtype, (N, w.shape[-1]), "w")
+    F, pc, ps = _gate(packed, M, w.shape[-1])
+    act = _act(act)
+    if out is None:
+        out = torch.empty((M, 2 * F), dtype=dy.dtype, device=dy.device)
+    db = torch.empty((2 * F,), dtype=torch.float32, device=dy.device) if want_bias else None
+    workspace = _room(workspace, lib.cat_gated_backward_workspace_bytes(M, N, F, dt), dy.device)
+    _one_device(dy, w, *packed, out, workspace)
+    _check(lib.cat_gated_backward_input(pd, pw, pc, ps, M, N, F, dt, act, _dev(out, dy.dtype, (M, 2 * F), "out"),
+                                        None if db is None else db.data_ptr(), workspace.data_ptr(), workspace.numel(), _stream()))
+    return out, db
+
+
+def cat_gated_backward_weight(dy, packed, act="silu", want_bias=True, out=None, workspace=None):
+    """Gradients of the weight and bias of the product that takes act(g) * v (cat_gated_backward_weight), from the checkpoints of g
+    and v.  Returns (dw, dbias): dw (N x F) of dy's type, dbias float32, None without ``want_bias``.  Rounding of act(g) * v as in
+    cat_linear_backward_weight."""
+    lib = load_library()
+    M, N, dt = _rows(dy, "dy")
+    pd = _dev(dy, name="dy")
+    F, pc, ps = _gate(packed, M)
+    act = _act(act)
+    if out is None:
+        out = torch.empty((N, F), dtype=dy.dtype, device=dy.device)
+    db = torch.empty((N,), dtype=torch.float32, device=dy.device) if want_bias else None
+    workspace = _room(workspace, lib.cat_gated_backward_workspace_bytes(M, N, F, dt), dy.device)
+    _one_device(dy, *packed, out, workspace)
+    _check(lib.cat_gated_backward_weight(pd, pc, ps, M, N, F, dt, act, _dev(out, dy.dtype, (N, F), "out"), None if db is None else db.data_ptr(),
+                                         workspace.data_ptr(), workspace.numel(), _stream()))
+    return out, db

@@ -133,6 +133,10 @@ __device__ __forceinline__ uint32_t lanes_max(uint32_t v) {
         const uint32_t o = (uint32_t)__shfl_xor((int)v, 16, kWave);
         v = v > o ? v : o;
     }
+    if constexpr (L >= 64) {
+        const uint32_t o = (uint32_t)__shfl_xor((int)v, 32, kWave);
+        v = v > o ? v : o;
+    }
     return v;
 }
 

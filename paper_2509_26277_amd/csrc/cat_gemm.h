@@ -6,17 +6,30 @@
 //   forward          x w^T       Q = x,           P = w
 //   input gradient   dy w        Q = dy,          P = w turned
 //   weight gradient  dy^T u      Q = dy turned,   P = u turned
+//   gated            x w^T       Q = x,           P = w, whose first n rows are the gate's and whose last n the value's: out
+//                                has n columns, of both products at once
+//   gate's gradient  dy w        Q = dy,          P = w turned
+// Operands are float, bfloat16 or, forward and gated, 8-bit integers, whose sums are 32-bit integers.
 #pragma once
 #include "cat_block.h"
 
 namespace cat {
 
-enum GemmKind { kForward = 0, kInputGrad = 1, kWeightGrad = 2 };
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+// four sums of E's products
+template <typename E>
+using Sums = std::conditional_t<sizeof(E) == 1, i32x4, f32x4>;
+
+enum GemmKind { kForward = 0, kInputGrad = 1, kWeightGrad = 2, kGated = 3, kGatedGrad = 4 };
 
 // What happens to out on its way to memory, by kind:
 //   kForward     z = out + bias; codes_out: the checkpoint of z; y = act(z) + residual
 //   kInputGrad   out * act'(codes_in)
 //   kWeightGrad  nothing
+//   kGated       g, v = out + bias (2 n entries); codes_out: the checkpoints of g and v, one behind the other; act(g) * v
+//   kGatedGrad   g, v = codes_in (as above): rows of 2 n entries, out * v * act'(g) and out * act(g); their sums over the rows
+//                of a wave, or of a joining workgroup: a row of col_sums each (2 n entries)
+// Sums of 8-bit integers are multiplied by row_scales (of q's row) and col_scales (of p's row) first.
 struct Epilogue {
     void* out;
     const float* bias;
@@ -26,6 +39,9 @@ struct Epilogue {
     const int8_t* codes_in;
     const float* scales_in;
     int act;
+    const float* row_scales;
+    const float* col_scales;
+    float* col_sums;
 };
 
 struct GemmArgs {
@@ -35,7 +51,7 @@ struct GemmArgs {
     int64_t m, n, k;
     int64_t k_split;  // entries of k a share takes (a multiple of the kernel's step); shares beyond the first: blockIdx.y
     int splits;
-    float* parts;  // splits > 1: splits x m x n
+    void* parts;  // instead of an epilogue: sums as they are, splits x m x n (gated: x 2 n), float or 32-bit integers
     Epilogue e;
 };
 
@@ -122,8 +138,9 @@ __device__ __forceinline__ void finish(const Epilogue& e, int64_t m, int64_t n, 
     st_entries<T, E>((T*)e.out + at, n, N, v);
 }
 
-// launchers of the tile kernels, one translation unit a type; `large`: tiles of 256 x 256 (bfloat16 only)
+// launchers of the tile kernels, one translation unit a type; `large`: tiles of 256 x 256 (not float)
 cat_status launch_gemm_f32(GemmKind kind, const GemmArgs& a, hipStream_t st);
 cat_status launch_gemm_bf16(GemmKind kind, bool large, const GemmArgs& a, hipStream_t st);
+cat_status launch_gemm_i8(GemmKind kind, bool large, cat_dtype out, const GemmArgs& a, hipStream_t st);
 
 }  // namespace cat

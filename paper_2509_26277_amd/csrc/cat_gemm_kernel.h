@@ -208,8 +208,10 @@ struct Fragments {
 };
 
 template <typename T>
-__device__ __forceinline__ f32x4 multiply(f32x4 a, f32x4 b, f32x4 c) {
-    if constexpr (sizeof(T) == 2) {
+__device__ __forceinline__ Sums<T> multiply(f32x4 a, f32x4 b, Sums<T> c) {
+    if constexpr (sizeof(T) == 1) {
+        return __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4, a), __builtin_bit_cast(i32x4, b), c, 0, 0, 0);
+    } else if constexpr (sizeof(T) == 2) {
         return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
     } else {
 #pragma unroll
@@ -286,7 +288,7 @@ __device__ __forceinline__ void finish_rows(const Epilogue& e, f32x4 (&acc)[MT][
     }
     // What the tile reads besides its sums (the residual; the argument of the derivative), as it lies, for all of its rows at
     // once: they come from memory, and row by row each of them would be waited for.
-    constexpr bool kAhead = WHOLE && (KIND == kInputGrad || KIND == kForward);
+    constexpr bool kAhead = WHOLE && (KIND == kInputGrad || (KIND == kForward && MT * sizeof(T) <= 8));  // (what the registers hold)
     constexpr int kWords = !kAhead ? 1 : KIND == kInputGrad ? 2 : 2 * (int)sizeof(T);
     uint32_t raw[kAhead ? MT : 1][4][kWords];
     float steps[MT];
@@ -366,22 +368,200 @@ __device__ __forceinline__ void finish_rows(const Epilogue& e, f32x4 (&acc)[MT][
         with_act(e.act, [&](auto which) { rows(which, std::false_type()); });
 }
 
+// The gated product's.  Lane (r, g) holds columns n + 32 t .. + 7, t = 0, 1, of the gate in acc[mt][0..3], of the value in
+// acc[mt][4..7].
+// PACK: the largest magnitudes of a wave's 64 columns of both go to LDS (`mine`, four words a row of the tile: gate and value of the
+// wave's columns, and of the other wave's, which share a scale with them) and come back as the scales of 128.  The barrier waits for
+// LDS alone: the next tile's loads stay under way.
+template <int MT>
+__device__ __forceinline__ void gated_scales(const f32x4 (&acc)[MT][8], int64_t n, int64_t N, lds_char row0, int half, int g, PackScale (&s)[MT][2]) {
+    typedef __attribute__((address_space(3))) volatile uint32_t* words;
+#pragma unroll
+    for (int mt = 0; mt < MT; mt++)
+#pragma unroll
+        for (int part = 0; part < 2; part++) {
+            uint32_t a = 0;
+#pragma unroll
+            for (int nt = 0; nt < 4; nt++)
+#pragma unroll
+                for (int i = 0; i < 4; i++)
+                    if (n + 32 * (nt >> 1) + 4 * (nt & 1) + i < N) a = mag_max(a, acc[mt][part * 4 + nt][i]);
+            const auto by16 = __builtin_amdgcn_permlane16_swap(a, a, false, false);
+            a = by16[0] > by16[1] ? by16[0] : by16[1];
+            const auto by32 = __builtin_amdgcn_permlane32_swap(a, a, false, false);
+            a = by32[0] > by32[1] ? by32[0] : by32[1];
+            if (g == 0) ((words)(row0 + mt * 16 * 16))[half * 2 + part] = a;
+        }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+#pragma unroll
+    for (int mt = 0; mt < MT; mt++)
+#pragma unroll
+        for (int part = 0; part < 2; part++) {
+            const uint32_t a = ((words)(row0 + mt * 16 * 16))[part], b = ((words)(row0 + mt * 16 * 16))[2 + part];
+            s[mt][part] = pack_scale(a > b ? a : b);
+        }
+}
+template <typename T, int MT, bool WHOLE>
+__device__ __forceinline__ void finish_gated(const Epilogue& e, f32x4 (&acc)[MT][8], int64_t m, int64_t M, int64_t n, int64_t N, int g,
+                                             const PackScale (*scales)[2]) {
+    if (scales) {
+        const int64_t G = (N + kPackGroup - 1) / kPackGroup;
+#pragma unroll
+        for (int mt = 0; mt < MT; mt++) {
+            const int64_t row = m + 16 * mt;
+            if (row < M) {
+#pragma unroll
+                for (int part = 0; part < 2; part++) {
+                    const PackScale s = scales[mt][part];
+                    int8_t* codes = e.codes_out + (part * M + row) * N;
+#pragma unroll
+                    for (int t = 0; t < 2; t++) {
+                        float v[8];
+#pragma unroll
+                        for (int i = 0; i < 8; i++) v[i] = acc[mt][part * 4 + 2 * t + (i >> 2)][i & 3];
+                        if constexpr (WHOLE)
+                            *(uint2*)(codes + n + 32 * t) = make_uint2(pack_codes4(v, s.up), pack_codes4(v + 4, s.up));
+                        else if (n + 32 * t < N)
+                            st_codes<8>(codes, n + 32 * t, N, v, s.up);
+                    }
+                    if (n % kPackGroup == 0) e.scales_out[(part * M + row) * G + n / kPackGroup] = s.step;  // (the first wave's g = 0)
+                }
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    }
+    with_act(e.act, [&](auto which) {
+        constexpr int ACT = decltype(which)::value;
+#pragma unroll
+        for (int mt = 0; mt < MT; mt++) {
+            const int64_t row = m + 16 * mt;
+            if (row >= M) continue;
+#pragma unroll
+            for (int t = 0; t < 2; t++) {
+                float v[8];
+#pragma unroll
+                for (int i = 0; i < 8; i++) v[i] = act_value<ACT, sizeof(T) == 2>(acc[mt][2 * t + (i >> 2)][i & 3]) * acc[mt][4 + 2 * t + (i >> 2)][i & 3];
+                if (WHOLE || n + 32 * t < N) st8<T, WHOLE>((T*)e.out + row * N, n + 32 * t, N, v);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    });
+}
+
+// Sums over the 16 lanes of a row of lanes of 16 values each: lane r is left with the sum of value r.  Each step hands on the half
+// of the values that the other lane of a pair goes on with.
+__device__ __forceinline__ float sums_by_lane(float (&v)[16], int r) {
+    const auto halve = [&](auto which) {
+        constexpr int bit = decltype(which)::value;  // value i stays with the lanes whose bit is i's
+        const bool up = r & bit;
+#pragma unroll
+        for (int i = 0; i < bit; i++) {
+            const float keep = up ? v[i + bit] : v[i], give = up ? v[i] : v[i + bit];
+            float got;
+            if constexpr (bit == 8) got = dpp_f32<0x128>(give);       // row_ror 8
+            else if constexpr (bit == 4) got = __shfl_xor(give, 4, kWave);
+            else if constexpr (bit == 2) got = dpp_f32<0x4E>(give);   // quad_perm [2, 3, 0, 1]
+            else got = dpp_f32<0xB1>(give);                           // quad_perm [1, 0, 3, 2]
+            v[i] = keep + got;
+        }
+    };
+    halve(std::integral_constant<int, 8>()), halve(std::integral_constant<int, 4>());
+    halve(std::integral_constant<int, 2>()), halve(std::integral_constant<int, 1>());
+    return v[0];
+}
+// The gate's gradients: lane (r, g) as in finish_rows.  A pair of tiles at a time for all rows, so that the sums over rows are 16
+// registers.  sums: this wave's row of col_sums.
+template <typename T, int MT, bool WHOLE>
+__device__ __forceinline__ void finish_gate_grad(const Epilogue& e, f32x4 (&acc)[MT][8], int64_t m, int64_t M, int64_t n, int64_t N, int r, float* sums) {
+    const int64_t G = (N + kPackGroup - 1) / kPackGroup, group = n / kPackGroup;
+    float steps[MT][2];
+#pragma unroll
+    for (int mt = 0; mt < MT; mt++) {
+        const int64_t row = m + 16 * mt < M ? m + 16 * mt : M - 1;
+        steps[mt][0] = e.scales_in[row * G + group], steps[mt][1] = e.scales_in[(M + row) * G + group];
+    }
+    uint2 raw[2][MT][2];
+    const auto request = [&](int t, uint2(&to)[MT][2]) {
+        if constexpr (WHOLE) {
+#pragma unroll
+            for (int mt = 0; mt < MT; mt++) {
+                const int64_t row = m + 16 * mt < M ? m + 16 * mt : M - 1;
+                to[mt][0] = *(const uint2*)(e.codes_in + row * N + n + 32 * t), to[mt][1] = *(const uint2*)(e.codes_in + (M + row) * N + n + 32 * t);
+            }
+        }
+    };
+    with_act(e.act, [&](auto which) {
+        constexpr int ACT = decltype(which)::value;
+        constexpr bool fast = sizeof(T) == 2;
+        request(0, raw[0]);
+#pragma unroll
+        for (int t = 0; t < 4; t++) {
+            if (t < 3) request(t + 1, raw[(t + 1) & 1]);
+            const int64_t at = n + 32 * t;
+            float s[16];
+#pragma unroll
+            for (int i = 0; i < 16; i++) s[i] = 0.f;
+#pragma unroll
+            for (int mt = 0; mt < MT; mt++) {
+                const int64_t row = m + 16 * mt;
+                if (row < M && (WHOLE || at < N)) {
+                    float gate[8], value[8];
+                    if constexpr (WHOLE) {
+                        const uint2 a = raw[t & 1][mt][0], b = raw[t & 1][mt][1];
+#pragma unroll
+                        for (int i = 0; i < 8; i++) {
+                            gate[i] = code_value(i < 4 ? a.x : a.y, i % 4) * steps[mt][0];
+                            value[i] = code_value(i < 4 ? b.x : b.y, i % 4) * steps[mt][1];
+                        }
+                    } else {
+                        ld_codes<8>(e.codes_in + row * N, at, N, steps[mt][0], gate);
+                        ld_codes<8>(e.codes_in + (M + row) * N, at, N, steps[mt][1], value);
+                    }
+#pragma unroll
+                    for (int i = 0; i < 8; i++) {
+                        const float d = acc[mt][2 * t + (i >> 2)][i & 3], z = gate[i];
+                        gate[i] = d * value[i] * act_grad<ACT, fast>(z);
+                        value[i] = d * act_value<ACT, fast>(z);
+                        s[i] += gate[i], s[8 + i] += value[i];
+                    }
+                    T* out = (T*)e.out + row * 2 * N;
+                    st8<T, WHOLE>(out, at, N, gate);
+                    st8<T, WHOLE>(out + N, at, N, value);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            if (sums) {
+                const float total = sums_by_lane(s, r);
+                const int64_t c = at + (r & 7);
+                if (WHOLE || c < N) sums[(r >> 3) * N + c] = total;
+            }
+        }
+    });
+}
+
 // Workgroups stay for all of their tiles: a tile's first loads are under way while the one before it is finished and stored.
-template <typename T, int KIND, int TM, int TN, int WM>
+template <typename E, typename T, int KIND, int TM, int TN, int WM>
 __global__ __launch_bounds__((TM / WM) * (TN / 128) * 64, 2) void k_gemm(const GemmArgs a) {
 #ifdef __HIP_DEVICE_COMPILE__  // (the host's pass does not know all of the builtins, and would leave out the kernel's stub)
-    constexpr bool PT = KIND != kForward, QT = KIND == kWeightGrad;
+    constexpr bool GATED = KIND == kGated, FORWARD = KIND == kForward || GATED, PT = !FORWARD, QT = KIND == kWeightGrad;
     constexpr int WN = 128, W = (TM / WM) * (TN / WN), MT = WM / 16, NT = WN / 16;
-    constexpr int kStep = kStepBytes / (int)sizeof(T);
+    constexpr int kStep = kStepBytes / (int)sizeof(E);
     constexpr int kBuf = (TM + TN) * kStepBytes;
-    __shared__ __attribute__((aligned(1024))) char lds_mem[2 * kBuf + 2 * 1024];
+    // columns of out a tile, and a wave: gated, half of them, since a wave's 128 are 64 of the gate and the same 64 of the value
+    constexpr int TO = GATED ? TN / 2 : TN, WO = GATED ? WN / 2 : WN;
+    // what a tile's end reads from LDS, for two tiles in turn: the bias, then the scales of p's rows and of q's (8-bit operands)
+    constexpr int kEnd = 1024 * (sizeof(E) == 1 ? 3 : 1);
+    constexpr bool kExchange = GATED && TO == kPackGroup && sizeof(E) > 1;  // (narrower tiles: the joining kernel packs)
+    __shared__ __attribute__((aligned(1024))) char lds_mem[2 * kBuf + 2 * kEnd + (kExchange ? TM * 16 : 0)];
     const lds_char lds = (lds_char)lds_mem, lds_bias = lds + 2 * kBuf;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave / (TN / WN), wn = wave % (TN / WN);
 
     // Workgroups go to the eight XCDs in turn; each XCD takes a run of neighbouring tiles, eight columns of them at a time, so
     // that what its L2 holds of either operand serves many of them.
-    const uint32_t tm = (uint32_t)((a.m + TM - 1) / TM), tn = (uint32_t)((a.n + TN - 1) / TN), tiles = tm * tn;
+    const uint32_t tm = (uint32_t)((a.m + TM - 1) / TM), tn = (uint32_t)((a.n + TO - 1) / TO), tiles = tm * tn;
     const uint32_t xcd = blockIdx.x & 7, share = tiles / 8, more = tiles % 8;
     const uint32_t stride = (gridDim.x - xcd + 7) / 8, end = (xcd + 1) * share + (xcd + 1 < more ? xcd + 1 : more);
     uint32_t t = xcd * share + (xcd < more ? xcd : more) + blockIdx.x / 8;
@@ -392,10 +572,10 @@ __global__ __launch_bounds__((TM / WM) * (TN / 128) * 64, 2) void k_gemm(const G
     };
 
     const int64_t k0 = (int64_t)blockIdx.y * a.k_split, k_all = a.k - k0 < a.k_split ? a.k - k0 : a.k_split;
-    Stage<T, PT, true, TN, W> sp;
-    Stage<T, QT, false, TM, W> sq;
-    Fragments<T, PT, true, TN> fp;
-    Fragments<T, QT, false, TM> fq;
+    Stage<E, PT, true, TN, W> sp;
+    Stage<E, QT, false, TM, W> sq;
+    Fragments<E, PT, true, TN> fp;
+    Fragments<E, QT, false, TM> fq;
     const auto addresses = [&](int of_lane) {
         sp.init(a.ldp, wave, of_lane);
         sq.init(a.ldq, wave, of_lane);
@@ -406,19 +586,25 @@ __global__ __launch_bounds__((TM / WM) * (TN / 128) * 64, 2) void k_gemm(const G
     constexpr int kAll = MT * NT, kLoads = decltype(sp)::kLoads;
     static_assert(kLoads == 4 && decltype(sq)::kLoads == 4, "");
 
+    // The row of p at which a tile's rows in LDS would begin for those that this wave brings: gated, 64 rows of the gate and the same
+    // 64 of the value in turn, a wave's 32 of one or the other.
+    const auto first_p = [&](uint32_t tile) {
+        const int64_t n0 = (int64_t)tile * TO;
+        return GATED ? ((wave >> 1) & 1) * a.n + n0 + (wave >> 2) * 64 + (wave & 1) * 32 - wave * 32 : n0;
+    };
     // The next step to be requested, of this tile or of the next one (behind the last tile: of that one again, not used).
     const int steps = (int)((k_all + kStep - 1) / kStep), tail = (int)(k_all - (int64_t)(steps - 1) * kStep);
     uint32_t tile_m, tile_n;
     place(t, tile_m, tile_n);
     int ahead = steps;
-    sp.tile(a.p, a.p_bytes, (int64_t)tile_n * TN, k0, sp.base, sp.left);
+    sp.tile(a.p, a.p_bytes, first_p(tile_n), k0, sp.base, sp.left);
     sq.tile(a.q, a.q_bytes, (int64_t)tile_m * TM, k0, sq.base, sq.left);
     const char *next_p, *next_q;
     int64_t next_p_left, next_q_left;
     const auto look_ahead = [&](uint32_t next) {
         uint32_t next_m, next_n;
         place(next < end ? next : t, next_m, next_n);
-        sp.tile(a.p, a.p_bytes, (int64_t)next_n * TN, k0, next_p, next_p_left);
+        sp.tile(a.p, a.p_bytes, first_p(next_n), k0, next_p, next_p_left);
         sq.tile(a.q, a.q_bytes, (int64_t)next_m * TM, k0, next_q, next_q_left);
     };
     const auto begin = [&] {
@@ -441,8 +627,8 @@ __global__ __launch_bounds__((TM / WM) * (TN / 128) * 64, 2) void k_gemm(const G
     for (int i = 0; i < 4; i++) sp.one(lds + kBuf, wave, i), sq.one(lds + kBuf + TN * kStepBytes, wave, i);
 
     int cur = 0, odd = 0;
-    for (;; t += stride, odd ^= 1024) {
-        const int64_t m0 = (int64_t)tile_m * TM, n0 = (int64_t)tile_n * TN;
+    for (;; t += stride, odd ^= kEnd) {
+        const int64_t m0 = (int64_t)tile_m * TM, n0 = (int64_t)tile_n * TO;
         // The addresses are made anew for every tile, from a lane number that the compiler takes for another one: kept over a
         // tile's end they would not fit the registers, and their way back from memory would wait for that tile's stores.
         int lane_again = lane;
@@ -451,21 +637,45 @@ __global__ __launch_bounds__((TM / WM) * (TN / 128) * 64, 2) void k_gemm(const G
         look_ahead(t + (steps > 1 ? 1 : 2) * stride);  // (tiles of one step: the next one's is requested already)
         // the tile's bias into LDS, for its end (without one, and with shares of k, which the joining kernel finishes: zeros)
         if (KIND == kForward && wave == 0) {
-            const int64_t there = a.e.bias && a.splits == 1 ? (a.n - n0) * 4 : 0;
+            const int64_t there = a.e.bias && !a.parts ? (a.n - n0) * 4 : 0;
             auto rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)(a.e.bias + n0), 0, there < TN * 4 ? (uint32_t)there : TN * 4, 0x00027000);
             __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_void)(lds_bias + odd), 16, lane_again * 16, 0, 0, 0);
         }
-        f32x4 acc[MT][NT];
+        if constexpr (GATED) {  // (the value's bias and scales start on any float's boundary: a float a lane, a wave 64 rows of p)
+            if (wave < TN / 64) {
+                const int64_t from = n0 + (wave >> 1) * 64, rest = a.n - from, at = (wave & 1) * a.n + from;
+                const uint32_t there = a.parts || rest <= 0 ? 0 : rest < 64 ? (uint32_t)rest * 4 : 256;
+                auto rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)(a.e.bias + at), 0, a.e.bias ? there : 0, 0x00027000);
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_void)(lds_bias + odd + wave * 256), 4, lane_again * 4, 0, 0, 0);
+                if constexpr (sizeof(E) == 1) {
+                    rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)(a.e.col_scales + at), 0, there, 0x00027000);
+                    __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_void)(lds_bias + odd + 1024 + wave * 256), 4, lane_again * 4, 0, 0, 0);
+                }
+            }
+        }
+        if constexpr (sizeof(E) == 1) {
+            if (!GATED && wave == 1) {
+                const int64_t there = a.parts ? 0 : (a.n - n0) * 4;
+                auto rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)(a.e.col_scales + n0), 0, there < TN * 4 ? (uint32_t)there : TN * 4, 0x00027000);
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_void)(lds_bias + odd + 1024), 16, lane_again * 16, 0, 0, 0);
+            }
+            if (wave == W - 1) {
+                const int64_t there = a.parts ? 0 : (a.m - m0) * 4;
+                auto rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)(a.e.row_scales + m0), 0, there < TM * 4 ? (uint32_t)there : TM * 4, 0x00027000);
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_void)(lds_bias + odd + 2048), 16, lane_again * 16, 0, 0, 0);
+            }
+        }
+        Sums<E> sums[MT][NT];
 #pragma unroll
         for (int mt = 0; mt < MT; mt++)
 #pragma unroll
-            for (int nt = 0; nt < NT; nt++) acc[mt][nt] = f32x4{0.f, 0.f, 0.f, 0.f};
+            for (int nt = 0; nt < NT; nt++) sums[mt][nt] = Sums<E>{0, 0, 0, 0};
         // A step's second half is read while the first is multiplied, and the next step's first half while the second half's last
         // rows are: the wait for the next step's loads, and for the waves that still read this one's, stands before those rows, and
         // the loads of the step after it follow, one by one between the products.
         const auto multiply_rows = [&](const f32x4(&p)[NT], const f32x4(&q)[MT], int from, int to) {  // products from .. to - 1
 #pragma unroll
-            for (int i = from; i < to; i++) acc[i / NT][i % NT] = multiply<T>(p[i % NT], q[i / NT], acc[i / NT][i % NT]);
+            for (int i = from; i < to; i++) sums[i / NT][i % NT] = multiply<E>(p[i % NT], q[i / NT], sums[i / NT][i % NT]);
         };
         f32x4 p0[NT], q0[MT], p1[NT], q1[MT];
         fp.template read<0>(lds + cur, p0);
@@ -509,32 +719,65 @@ __global__ __launch_bounds__((TM / WM) * (TN / 128) * 64, 2) void k_gemm(const G
         int lane_end = lane;
         asm volatile("" : "+v"(lane_end));
         const int r = lane_end & 15, g = lane_end >> 4;
-        const int64_t nw = n0 + wn * WN, nl = nw + 8 * g;  // the wave's first column; this lane's of pair t: nl + 32 t
-        if (KIND == kForward) {
-#pragma unroll
-            for (int nt = 0; nt < NT; nt++) {
-                const f32x4 b = *(__attribute__((address_space(3))) f32x4*)(lds_bias + odd + (wn * WN + 8 * g + (nt >> 1) * 32 + 4 * (nt & 1)) * 4);
-#pragma unroll
-                for (int mt = 0; mt < MT; mt++) acc[mt][nt] += b;
-            }
-        }
-        if (a.splits > 1) {  // the sum of a share of k: fp32, joined by a kernel of its own
-            float* part = a.parts + (int64_t)blockIdx.y * a.m * a.n;
+        const int64_t nw = n0 + wn * WO, nl = nw + 8 * g;  // the wave's first column; this lane's of pair t: nl + 32 t (gated: t & 1)
+        if (a.parts) {  // the sums as they are (of a share of k, say): a kernel of its own goes on with them
+            const int64_t width = GATED ? 2 * a.n : a.n;
 #pragma unroll
             for (int mt = 0; mt < MT; mt++) {
                 const int64_t m = m0 + wm * WM + mt * 16 + r;
                 if (m >= a.m) continue;
+                float* part = (float*)a.parts + ((int64_t)blockIdx.y * a.m + m) * width;
 #pragma unroll
                 for (int nt = 0; nt < NT; nt++) {
-                    const int64_t n = nl + (nt >> 1) * 32 + 4 * (nt & 1);
-                    const float v[4] = {acc[mt][nt][0], acc[mt][nt][1], acc[mt][nt][2], acc[mt][nt][3]};
-                    if (n < a.n) st_group_to(part + m * a.n, n, a.n, v);
+                    const int64_t n = nl + ((nt >> 1) & (GATED ? 1 : 3)) * 32 + 4 * (nt & 1);
+                    const f32x4 b = __builtin_bit_cast(f32x4, sums[mt][nt]);
+                    const float v[4] = {b[0], b[1], b[2], b[3]};
+                    if (n < a.n) st_group_to(part + (GATED && nt >= 4 ? a.n : 0), n, a.n, v);
                 }
             }
-        } else if (nw + WN <= a.n && a.n % 8 == 0) {
-            finish_rows<T, KIND, MT, true>(a.e, acc, m0 + wm * WM + r, a.m, nl, a.n, g);
-        } else if (nw < a.n) {
-            finish_rows<T, KIND, MT, false>(a.e, acc, m0 + wm * WM + r, a.m, nl, a.n, g);
+        } else {
+            f32x4 acc[MT][NT];
+#pragma unroll
+            for (int nt = 0; nt < NT; nt++) {
+                f32x4 b = f32x4{0.f, 0.f, 0.f, 0.f}, by = b;
+                const int column = (wn * WN + 8 * g + (nt >> 1) * 32 + 4 * (nt & 1)) * 4;
+                if constexpr (FORWARD) b = *(__attribute__((address_space(3))) f32x4*)(lds_bias + odd + column);
+                if constexpr (sizeof(E) == 1) by = *(__attribute__((address_space(3))) f32x4*)(lds_bias + odd + 1024 + column);
+#pragma unroll
+                for (int mt = 0; mt < MT; mt++) {
+                    if constexpr (sizeof(E) == 1) {  // (the sum of integers rounds once to 32 bits, from 2^24 on; so do both products)
+                        const float scale = *(__attribute__((address_space(3))) float*)(lds_bias + odd + 2048 + (wm * WM + mt * 16 + r) * 4);
+#pragma unroll
+                        for (int i = 0; i < 4; i++) acc[mt][nt][i] = fmaf((float)sums[mt][nt][i], scale * by[i], b[i]);
+                    } else {
+                        acc[mt][nt] = sums[mt][nt];
+                        if constexpr (FORWARD) acc[mt][nt] += b;
+                    }
+                }
+            }
+            const int64_t m = m0 + wm * WM + r;
+            if constexpr (GATED) {
+                PackScale scales[MT][2];
+                const bool pack = kExchange && a.e.codes_out;
+                if constexpr (kExchange) {
+                    if (pack) gated_scales<MT>(acc, nl, a.n, lds_bias + 2 * kEnd + (wm * WM + r) * 16, wn, g, scales);
+                }
+                if (nw + WO <= a.n && a.n % 8 == 0)
+                    finish_gated<T, MT, true>(a.e, acc, m, a.m, nl, a.n, g, pack ? scales : nullptr);
+                else if (nw < a.n)
+                    finish_gated<T, MT, false>(a.e, acc, m, a.m, nl, a.n, g, pack ? scales : nullptr);
+            } else if constexpr (KIND == kGatedGrad) {
+                float* col_sums = a.e.col_sums ? a.e.col_sums + ((int64_t)tile_m * (TM / WM) + wm) * 2 * a.n : nullptr;
+                if (nw + WO <= a.n && a.n % 8 == 0)
+                    finish_gate_grad<T, MT, true>(a.e, acc, m, a.m, nl, a.n, r, col_sums);
+                else if (nw < a.n)
+                    finish_gate_grad<T, MT, false>(a.e, acc, m, a.m, nl, a.n, r, col_sums);
+            } else {
+                if (nw + WN <= a.n && a.n % 8 == 0)
+                    finish_rows<T, KIND, MT, true>(a.e, acc, m, a.m, nl, a.n, g);
+                else if (nw < a.n)
+                    finish_rows<T, KIND, MT, false>(a.e, acc, m, a.m, nl, a.n, g);
+            }
         }
         if (t + stride >= end) break;
         place(t + stride, tile_m, tile_n);
@@ -543,13 +786,14 @@ __global__ __launch_bounds__((TM / WM) * (TN / 128) * 64, 2) void k_gemm(const G
 #endif
 }
 
-template <typename T, int KIND, int TM, int TN, int WM>
+template <typename E, typename T, int KIND, int TM, int TN, int WM>
 cat_status launch_gemm_tiles(const GemmArgs& a, hipStream_t st) {
-    const int64_t tiles = ((a.m + TM - 1) / TM) * ((a.n + TN - 1) / TN);
+    constexpr int TO = KIND == kGated ? TN / 2 : TN;
+    const int64_t tiles = ((a.m + TM - 1) / TM) * ((a.n + TO - 1) / TO);
     if (tiles >= (1ll << 31)) return set_error(CAT_ERR_UNSUPPORTED, "product of %lld x %lld entries has too many tiles", (long long)a.m, (long long)a.n);
     // as many workgroups as the card holds at a time (256 CUs, by LDS one large tile's or two small ones' each)
     const int64_t most = 256 * (TM == 256 ? 1 : 2);
-    hipLaunchKernelGGL((k_gemm<T, KIND, TM, TN, WM>), dim3((unsigned)(a.splits > 1 || tiles < most ? tiles : most), (unsigned)a.splits), dim3((TM / WM) * (TN / 128) * 64), 0, st, a);
+    hipLaunchKernelGGL((k_gemm<E, T, KIND, TM, TN, WM>), dim3((unsigned)(a.splits > 1 || tiles < most ? tiles : most), (unsigned)a.splits), dim3((TM / WM) * (TN / 128) * 64), 0, st, a);
     CAT_LAUNCH_CHECK("k_gemm");
     return CAT_OK;
 }

@@ -199,8 +199,9 @@ cat_status cat_pack8(const void* x, int64_t N, int64_t D, cat_dtype dt, int8_t* 
 cat_status cat_unpack8(const int8_t* codes, const float* scales, int64_t N, int64_t D, cat_dtype dt, void* x, void* hip_stream) {
     const char* who = "cat_unpack8";
     CAT_TRY(check_rows(who, N, D, dt));
-    CAT_TRY(check_ptr(who, "codes", codes, N > 0));
-    CAT_TRY(check_ptr(who, "scales", scales, N > 0));
+    // (the second of two checkpoints one behind the other starts where the first one ends: codes on any byte, scales on any float)
+    if (N > 0 && (!codes || !scales)) return set_error(CAT_ERR_INVALID_ARG, "%s: %s is NULL", who, codes ? "scales" : "codes");
+    if ((uintptr_t)scales % 4) return set_error(CAT_ERR_INVALID_ARG, "%s: scales is not 4-byte aligned", who);
     CAT_TRY(check_ptr(who, "x", x, N > 0));
     if (N == 0) return CAT_OK;
     const int64_t G = (D + kPackGroup - 1) / kPackGroup;

@@ -1,0 +1,161 @@
+"""Products of 8-bit integers, plain and gated, against their definitions in 64 bits."""
+import pytest
+import torch
+
+from paper_2509_26277_amd import binding, cat_gated_linear8, cat_linear8
+
+from block_util import ACT_ERR, ACTS, SLOPE, TYPES, U32, act_ref, half_step
+
+pytestmark = pytest.mark.gpu
+
+# (M, N, K): single rows and few rows, tiles with ragged ends in every direction, lengths that are no whole 16-byte groups, shares
+# of k, one entry; rows of 128 entries a step and one more; large tiles
+SHAPES = [(1, 1, 1), (1, 16, 16), (1, 1000, 2048), (3, 17, 33), (16, 100, 512), (17, 130, 300), (33, 64, 272), (64, 257, 1030), (48, 96, 8192),
+          (65, 128, 128), (66, 1, 7), (100, 129, 129), (128, 128, 256), (129, 257, 144), (300, 513, 1030), (200, 300, 8192), (777, 24, 63),
+          (1025, 640, 144), (3600, 3590, 144), (3584, 3840, 400), (2000, 2003, 12000)]
+
+
+def _codes(M, N, seed, low=-128):
+    g = torch.Generator().manual_seed(seed)
+    return torch.randint(low, 128, (M, N), generator=g).to(torch.int8).cuda()
+
+
+def _floats(*shape, seed, scale=1.0):
+    return (scale * torch.randn(*shape, generator=torch.Generator().manual_seed(seed))).cuda()
+
+
+def _operands(M, N, K, seed=0):
+    """Codes and scales such that the products are of order one, some rows of much larger and smaller scale."""
+    x, w = _codes(M, K, 1 + seed), _codes(N, K, 2 + seed)
+    xs, ws = torch.exp(_floats(M, seed=3 + seed)) / 74, torch.exp(0.5 * _floats(N, seed=4 + seed)) / (74 * K ** 0.5)
+    return x, xs, w, ws
+
+
+def _close(got, want, bound, what):
+    assert got.shape == want.shape, what
+    bad = ~((got.double() - want).abs() <= bound)
+    assert not bool(bad.any()), (what, int(bad.sum()), torch.nonzero(bad)[:3].tolist())
+
+
+def _product(x, xs, w, ws, b):
+    """z and its error: the sum, the scales' product and what comes of both round once each, z with the bias once more."""
+    p = (x.double() @ w.double().t()) * xs.double()[:, None] * ws.double()
+    z = p if b is None else p + b.double()
+    return z, U32 * (3 * p.abs() + z.abs())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("M,N,K", SHAPES)
+def test_product(M, N, K, dtype):
+    act, t = ACTS[(M + N + K) % len(ACTS)], TYPES[dtype]
+    x, xs, w, ws = _operands(M, N, K)
+    b, res = _floats(N, seed=5, scale=0.3), _floats(M, N, seed=6).to(t)
+    z, z_err = _product(x, xs, w, ws, b)
+    u = act_ref(z, act)[0]
+    want = u + res.double()
+    err = SLOPE * z_err + ACT_ERR * (1.0 + z.abs()) + U32 * want.abs()
+    y = cat_linear8(x, xs, w, ws, b, act=act, residual=res, dtype=t)
+    assert y.dtype == t
+    _close(y, want, half_step(t) * want.abs() + err, "y")
+    assert torch.equal(cat_linear8(x, xs, w, ws, b, act=act, residual=res, dtype=t), y)
+    z, z_err = _product(x, xs, w, ws, None)
+    _close(cat_linear8(x, xs, w, ws, dtype=t), z, half_step(t) * z.abs() + z_err, "product")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("M,F,K", [(M, (N + 1) // 2, K) for M, N, K in SHAPES])
+def test_gated_product(M, F, K, dtype):
+    act, t = ACTS[(M + F + K) % len(ACTS)], TYPES[dtype]
+    x, xs, w, ws = _operands(M, 2 * F, K)
+    b = _floats(2 * F, seed=5, scale=0.3)
+    for bias in (b, None):
+        z, z_err = _product(x, xs, w, ws, bias)
+        (g, v), (ge, ve) = z.split(F, 1), z_err.split(F, 1)
+        u = act_ref(g, act)[0]
+        ue = SLOPE * ge + ACT_ERR * (1.0 + g.abs())
+        want = u * v
+        y = cat_gated_linear8(x, xs, w, ws, bias, act=act, dtype=t)
+        _close(y, want, half_step(t) * want.abs() * (1 + U32) + U32 * want.abs() + ue * (v.abs() + ve) + u.abs() * ve, "y")
+        assert torch.equal(cat_gated_linear8(x, xs, w, ws, bias, act=act, dtype=t), y)
+
+
+@pytest.mark.parametrize("act", ACTS)
+@pytest.mark.parametrize("M", [2, 150, 2100])
+def test_every_activation(M, act):
+    N, K = (70, 40) if M < 1000 else (2056, 64)
+    x, xs, w, ws = _operands(M, N, K)
+    z, z_err = _product(x, xs, w, ws, None)
+    for t in TYPES.values():
+        want = act_ref(z, act)[0]
+        _close(cat_linear8(x, xs, w, ws, act=act, dtype=t), want, half_step(t) * want.abs() + SLOPE * z_err + ACT_ERR * (1.0 + z.abs()), act)
+
+
+@pytest.mark.parametrize("M", [3, 200])
+def test_the_longest_sums_are_exact(M):
+    """131071 products of the largest magnitude, of either sign: the sums of all but the last entry stay whole."""
+    K, N = 131071, 20
+    x, w = torch.full((M, K), -128, dtype=torch.int8, device="cuda"), torch.full((N, K), -128, dtype=torch.int8, device="cuda")
+    w[1] = 127
+    one_x, one_w = torch.ones(M, device="cuda"), torch.ones(N, device="cuda")
+    y = cat_linear8(x, one_x, w, one_w, dtype=torch.float32)
+    want = (x[:1].double() @ w.double().t()).float().expand(M, N)  # (rounded once)
+    assert torch.equal(y, want) and float(y[0, 0]) == float(torch.tensor(131071.0 * 16384.0))
+
+
+def test_exact_in_integers():
+    """Scales of one and sums below 2^24: whole numbers, of either kernel, whatever the order."""
+    for M, N, K in [(5, 40, 100), (300, 400, 1000), (2100, 2050, 128)]:
+        x, w = _codes(M, K, 7), _codes(N, K, 8)
+        y = cat_linear8(x, torch.ones(M, device="cuda"), w, torch.ones(N, device="cuda"), dtype=torch.float32)
+        assert torch.equal(y.double(), x.double() @ w.double().t())
+
+
+# more tiles than workgroups, of several steps of k: what a workgroup carries from one tile to the next
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("M,N,K", [(6144, 5120, 1024), (6001, 5003, 600), (4864, 4096, 128), (4867, 4099, 133)])
+def test_many_tiles(M, N, K, dtype):
+    t = TYPES[dtype]
+    x, xs, w, ws = _operands(M, N, K)
+    b, res = _floats(N, seed=5, scale=0.3), _floats(M, N, seed=6).to(t)
+    z, z_err = _product(x, xs, w, ws, b)
+    want = act_ref(z, "silu")[0] + res.double()
+    _close(cat_linear8(x, xs, w, ws, b, act="silu", residual=res, dtype=t), want,
+           half_step(t) * want.abs() + SLOPE * z_err + ACT_ERR * (1.0 + z.abs()) + U32 * want.abs(), "y")
+    if N % 2 == 0:
+        F = N // 2
+        (g, v), (ge, ve) = z.split(F, 1), z_err.split(F, 1)
+        u = act_ref(g, "gelu")[0]
+        want = u * v
+        ue = SLOPE * ge + ACT_ERR * (1.0 + g.abs())
+        _close(cat_gated_linear8(x, xs, w, ws, b, act="gelu", dtype=t), want,
+               half_step(t) * want.abs() * (1 + U32) + U32 * want.abs() + ue * (v.abs() + ve) + u.abs() * ve, "gated")
+
+
+@pytest.mark.parametrize("M", [5, 200])
+def test_nan_and_infinity_go_where_the_formula_takes_them(M):
+    x, xs, w, ws = _operands(M, 150, 200)
+    clean, clean_gated = cat_linear8(x, xs, w, ws, act="relu"), cat_gated_linear8(x, xs, w, ws, act="relu")
+    x[3], xs[3], ws[140] = 0, float("inf"), float("nan")  # a row that held an infinity: zeros times infinity
+    y, h = cat_linear8(x, xs, w, ws, act="relu"), cat_gated_linear8(x, xs, w, ws, act="relu")
+    bad = torch.zeros(M, 150, dtype=torch.bool, device="cuda")
+    bad[3] = bad[:, 140] = True
+    assert torch.equal(torch.isnan(y), bad) and torch.equal(y[~bad], clean[~bad])
+    bad = torch.zeros(M, 75, dtype=torch.bool, device="cuda")
+    bad[3] = bad[:, 65] = True
+    assert torch.equal(torch.isnan(h), bad) and torch.equal(h[~bad], clean_gated[~bad])
+
+
+def test_no_rows():
+    x, w = torch.empty(0, 33, dtype=torch.int8, device="cuda"), torch.ones(8, 33, dtype=torch.int8, device="cuda")
+    none, ws = torch.empty(0, device="cuda"), torch.ones(8, device="cuda")
+    assert cat_linear8(x, none, w, ws).shape == (0, 8) and cat_gated_linear8(x, none, w, ws).shape == (0, 4)
+
+
+def test_a_workspace_of_the_stated_size_is_enough_and_stays_in_its_bounds():
+    lib = binding.load_library()
+    for M, N, K in [(1, 64, 8192), (300, 66, 1030), (150, 130, 8192), (2000, 2004, 12000)]:
+        x, xs, w, ws = _operands(M, N, K)
+        for size, call in ((lib.cat_linear8_workspace_bytes(M, N, K), cat_linear8), (lib.cat_gated_linear8_workspace_bytes(M, N // 2, K), cat_gated_linear8)):
+            buf = torch.full((size + 4096,), 0xA5, dtype=torch.uint8, device="cuda")
+            assert torch.equal(call(x, xs, w, ws, act="none", workspace=buf[:size]), call(x, xs, w, ws, act="none"))
+            assert bool((buf[size:] == 0xA5).all())
