@@ -207,17 +207,22 @@ __device__ __forceinline__ void ld_codes(const int8_t* row, int64_t j, int64_t D
 // ---- activations ----
 // In fp32 throughout.  The saturated ends come out of the exponentials by themselves (exp -> inf gives 1 / inf = 0); a NaN
 // stays, and of -infinity GELU and SiLU are -inf * 0, a NaN, whatever the type (a sum that left the floats is not hidden).
-// FAST, for bfloat16 results: the epilogue of a product is bound by these instructions (its matrix cores wait), and the
+// FAST (1), for bfloat16 results: the epilogue of a product is bound by these instructions (its matrix cores wait), and the
 // library's erf is some forty of them.
 // The hardware's exponential is off by half a step of fp32 for every unit of its argument: nothing to a bfloat16 result, but 44
 // half steps of a float SiLU at z = -80, which therefore takes the library's and the correctly rounded quotient (us, derivative
 // of 65536 x 1000: 113 -> 121).  The other float forms keep it, being no worse for it: over [-9, 9] GELU' is off by 1.9 half
 // steps of one (1.8 with an exact exponential), tanh GELU by 157 of its value (149: the rounding of its cubic argument).
-template <bool HARDWARE>
+// FAST 2, the gated operators' and those of 8-bit integers': the quotient is the hardware's reciprocal, off by a step of fp32 at
+// most, where the others' is ten instructions (us, gradients of a gate 65536 x 1024 over 256, SiLU: SLOW -> QUICK).
+template <int FAST>
 __device__ __forceinline__ float logistic(float z) {
-    if constexpr (HARDWARE) return __fdividef(1.f, 1.f + __expf(-z));
+    if constexpr (FAST == 2) return __builtin_amdgcn_rcpf(1.f + __expf(-z));
+    else if constexpr (FAST) return __fdividef(1.f, 1.f + __expf(-z));
     else return __fdiv_rn(1.f, 1.f + expf(-z));
 }
+template <typename T>
+constexpr int kFast = sizeof(T) == 2 ? 2 : 0;
 constexpr float kInvSqrt2 = 0.70710678118654752f, kInvSqrt2Pi = 0.39894228040143268f;
 constexpr float kTanhIn = 0.79788456080286536f, kTanhCube = 0.044715f;
 // gelu with tanh: 0.5 z (1 + tanh u) = z * logistic(2 u), u = sqrt(2 / pi) (z + 0.044715 z^3)
@@ -236,7 +241,7 @@ __device__ __forceinline__ float tail_factor(float x) {
     return t * g;
 }
 __device__ __forceinline__ float normal_exp(float z) { return __builtin_amdgcn_exp2f(z * z * -0.72134752044448170f); }
-template <int ACT, bool FAST>
+template <int ACT, int FAST>
 __device__ __forceinline__ float act_value(float z) {
     if constexpr (ACT == CAT_ACT_RELU) {
         return z > 0.f ? z : (z != z ? z : 0.f);
@@ -246,14 +251,14 @@ __device__ __forceinline__ float act_value(float z) {
     } else if constexpr (ACT == CAT_ACT_GELU) {
         return 0.5f * z * (1.f + erff(z * kInvSqrt2));
     } else if constexpr (ACT == CAT_ACT_GELU_TANH) {
-        return z * logistic<true>(tanh_arg2(z));
+        return z * logistic<(FAST > 1 ? FAST : 1)>(tanh_arg2(z));
     } else if constexpr (ACT == CAT_ACT_SILU) {
         return z * logistic<FAST>(z);
     } else {
         return z;
     }
 }
-template <int ACT, bool FAST>
+template <int ACT, int FAST>
 __device__ __forceinline__ float act_grad(float z) {
     if constexpr (ACT == CAT_ACT_RELU) {
         return z > 0.f ? 1.f : (z != z ? z : 0.f);
@@ -264,13 +269,33 @@ __device__ __forceinline__ float act_grad(float z) {
         return fmaf(z * kInvSqrt2Pi, __expf(-0.5f * z * z), 0.5f * (1.f + erff(z * kInvSqrt2)));
     } else if constexpr (ACT == CAT_ACT_GELU_TANH) {
         // (beyond |z| = 32 the factor p (1 - p) is zero in fp32, and z * z must not turn it into 0 * inf)
-        const float p = logistic<true>(tanh_arg2(z)), c = fminf(fmaxf(z, -32.f), 32.f);
+        const float p = logistic<(FAST > 1 ? FAST : 1)>(tanh_arg2(z)), c = fminf(fmaxf(z, -32.f), 32.f);
         return fmaf(c * p * (1.f - p), 2.f * kTanhIn * fmaf(3.f * kTanhCube * c, c, 1.f), p);
     } else if constexpr (ACT == CAT_ACT_SILU) {
         const float p = logistic<FAST>(z);
         return p * fmaf(z, 1.f - p, 1.f);
     } else {
         return 1.f;
+    }
+}
+// Both at once, with what they share: value and derivative of the gate's activation.
+template <int ACT, int FAST>
+__device__ __forceinline__ void act_both(float z, float& value, float& grad) {
+    if constexpr (ACT == CAT_ACT_SILU) {
+        const float p = logistic<FAST>(z);
+        value = z * p;
+        grad = p * fmaf(z, 1.f - p, 1.f);
+    } else if constexpr (ACT == CAT_ACT_GELU && FAST) {
+        const float x = fminf(fabsf(z), 1e30f), e = normal_exp(z), g = tail_factor(x), s = e * fmaf(-kInvSqrt2Pi, x, g);
+        value = fmaf(-x, e * g, fmaxf(z, 0.f));
+        grad = z > 0.f ? 1.f - s : s;
+    } else if constexpr (ACT == CAT_ACT_GELU_TANH) {
+        const float p = logistic<(FAST > 1 ? FAST : 1)>(tanh_arg2(z)), c = fminf(fmaxf(z, -32.f), 32.f);
+        value = z * p;
+        grad = fmaf(c * p * (1.f - p), 2.f * kTanhIn * fmaf(3.f * kTanhCube * c, c, 1.f), p);
+    } else {
+        value = act_value<ACT, FAST>(z);
+        grad = act_grad<ACT, FAST>(z);
     }
 }
 // f(std::integral_constant<int, act>) for the activation: one branch, outside the loops over entries

@@ -35,8 +35,10 @@ __global__ __launch_bounds__(256) void k_join_gate_grad(const float* __restrict_
 #pragma unroll
                 for (int i = 0; i < 8; i++) {
                     const float z = gate[i];
-                    gate[i] = d[i] * value[i] * act_grad<ACT, sizeof(T) == 2>(z);
-                    value[i] = d[i] * act_value<ACT, sizeof(T) == 2>(z);
+                    float a, da;
+                    act_both<ACT, kFast<T>>(z, a, da);
+                    gate[i] = d[i] * value[i] * da;
+                    value[i] = d[i] * a;
                 }
             });
             T* out = (T*)e.out + m * 2 * N;

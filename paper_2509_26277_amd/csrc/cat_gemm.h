@@ -88,7 +88,7 @@ __device__ __forceinline__ void st_entries(T* row, int64_t n, int64_t N, const f
             if (n + e < N) st_round(row + n + e, v[e]);
     }
 }
-template <typename T, int KIND, int E, bool PACK>
+template <typename T, int KIND, int E, bool PACK, int FAST = sizeof(T) == 2>
 __device__ __forceinline__ void finish(const Epilogue& e, int64_t m, int64_t n, int64_t N, bool valid, float (&v)[E]) {
     const int64_t at = m * N;
     if constexpr (KIND == kForward) {
@@ -113,7 +113,7 @@ __device__ __forceinline__ void finish(const Epilogue& e, int64_t m, int64_t n, 
         if (!valid || n >= N) return;
         with_act(e.act, [&](auto which) {
 #pragma unroll
-            for (int i = 0; i < E; i++) v[i] = act_value<decltype(which)::value, sizeof(T) == 2>(v[i]);
+            for (int i = 0; i < E; i++) v[i] = act_value<decltype(which)::value, FAST>(v[i]);
         });
         if (e.residual) {
             float r[E];
@@ -130,7 +130,7 @@ __device__ __forceinline__ void finish(const Epilogue& e, int64_t m, int64_t n, 
                 ld_codes<E>(e.codes_in + at, n, N, step, c);
                 with_act(e.act, [&](auto which) {
 #pragma unroll
-                    for (int i = 0; i < E; i++) v[i] *= act_grad<decltype(which)::value, sizeof(T) == 2>(c[i]);
+                    for (int i = 0; i < E; i++) v[i] *= act_grad<decltype(which)::value, FAST>(c[i]);
                 });
             }
         }

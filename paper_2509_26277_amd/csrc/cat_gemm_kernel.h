@@ -250,7 +250,7 @@ __device__ __forceinline__ void st8(T* row, int64_t n, int64_t N, const float (&
         *(f32x4*)(row + n + 4) = f32x4{v[4], v[5], v[6], v[7]};
     }
 }
-template <typename T, int KIND, int MT, bool WHOLE>
+template <typename T, int KIND, int FAST, int MT, bool WHOLE>
 __device__ __forceinline__ void finish_rows(const Epilogue& e, f32x4 (&acc)[MT][8], int64_t m, int64_t M, int64_t n, int64_t N, int g) {
     const int64_t G = (N + kPackGroup - 1) / kPackGroup, group = n / kPackGroup;
     if constexpr (KIND == kForward) {
@@ -316,7 +316,7 @@ __device__ __forceinline__ void finish_rows(const Epilogue& e, f32x4 (&acc)[MT][
     };
     const auto rows = [&](auto which, auto with_residual) {
         constexpr int ACT = decltype(which)::value;
-        constexpr bool fast = sizeof(T) == 2, res = decltype(with_residual)::value;
+        constexpr bool res = decltype(with_residual)::value;
         if constexpr (KIND == kInputGrad ? ACT != CAT_ACT_NONE : res) request();
 #pragma unroll
         for (int mt = 0; mt < MT; mt++) {
@@ -351,8 +351,8 @@ __device__ __forceinline__ void finish_rows(const Epilogue& e, f32x4 (&acc)[MT][
 #pragma unroll
                 for (int i = 0; i < 8; i++) {
                     v[i] = acc[mt][2 * t + (i >> 2)][i & 3];
-                    if constexpr (KIND == kForward) v[i] = act_value<ACT, fast>(v[i]);
-                    if constexpr (KIND == kInputGrad) v[i] *= act_grad<ACT, fast>(more[t][i]);
+                    if constexpr (KIND == kForward) v[i] = act_value<ACT, FAST>(v[i]);
+                    if constexpr (KIND == kInputGrad) v[i] *= act_grad<ACT, FAST>(more[t][i]);
                     if constexpr (res) v[i] += more[t][i];
                 }
                 st8<T, WHOLE>((T*)e.out + row * N, n + 32 * t, N, v);
@@ -442,7 +442,7 @@ __device__ __forceinline__ void finish_gated(const Epilogue& e, f32x4 (&acc)[MT]
             for (int t = 0; t < 2; t++) {
                 float v[8];
 #pragma unroll
-                for (int i = 0; i < 8; i++) v[i] = act_value<ACT, sizeof(T) == 2>(acc[mt][2 * t + (i >> 2)][i & 3]) * acc[mt][4 + 2 * t + (i >> 2)][i & 3];
+                for (int i = 0; i < 8; i++) v[i] = act_value<ACT, kFast<T>>(acc[mt][2 * t + (i >> 2)][i & 3]) * acc[mt][4 + 2 * t + (i >> 2)][i & 3];
                 if (WHOLE || n + 32 * t < N) st8<T, WHOLE>((T*)e.out + row * N, n + 32 * t, N, v);
             }
             __builtin_amdgcn_sched_barrier(0);
@@ -471,8 +471,8 @@ __device__ __forceinline__ float sums_by_lane(float (&v)[16], int r) {
     halve(std::integral_constant<int, 2>()), halve(std::integral_constant<int, 1>());
     return v[0];
 }
-// The gate's gradients: lane (r, g) as in finish_rows.  A pair of tiles at a time for all rows, so that the sums over rows are 16
-// registers.  sums: this wave's row of col_sums.
+// The gate's gradients: lane (r, g) as in finish_rows.  sums: this wave's row of col_sums.  Two pairs of tiles at a time for all rows,
+// so that the sums over rows are 32 registers; a row's codes are under way while the one before it is worked on.
 template <typename T, int MT, bool WHOLE>
 __device__ __forceinline__ void finish_gate_grad(const Epilogue& e, f32x4 (&acc)[MT][8], int64_t m, int64_t M, int64_t n, int64_t N, int r, float* sums) {
     const int64_t G = (N + kPackGroup - 1) / kPackGroup, group = n / kPackGroup;
@@ -482,67 +482,164 @@ __device__ __forceinline__ void finish_gate_grad(const Epilogue& e, f32x4 (&acc)
         const int64_t row = m + 16 * mt < M ? m + 16 * mt : M - 1;
         steps[mt][0] = e.scales_in[row * G + group], steps[mt][1] = e.scales_in[(M + row) * G + group];
     }
-    uint2 raw[2][MT][2];
-    const auto request = [&](int t, uint2(&to)[MT][2]) {
-        if constexpr (WHOLE) {
-#pragma unroll
-            for (int mt = 0; mt < MT; mt++) {
-                const int64_t row = m + 16 * mt < M ? m + 16 * mt : M - 1;
-                to[mt][0] = *(const uint2*)(e.codes_in + row * N + n + 32 * t), to[mt][1] = *(const uint2*)(e.codes_in + (M + row) * N + n + 32 * t);
-            }
-        }
-    };
     with_act(e.act, [&](auto which) {
         constexpr int ACT = decltype(which)::value;
-        constexpr bool fast = sizeof(T) == 2;
-        request(0, raw[0]);
+        uint2 held[2][2][2];
+        const auto request = [&](int at, uint2(&to)[2][2]) {  // at: half * MT + row
+            if constexpr (WHOLE) {
+                const int64_t row = m + 16 * (at % MT) < M ? m + 16 * (at % MT) : M - 1;
+                const int8_t *gate = e.codes_in + row * N + n + 64 * (at / MT), *value = gate + M * N;
 #pragma unroll
-        for (int t = 0; t < 4; t++) {
-            if (t < 3) request(t + 1, raw[(t + 1) & 1]);
-            const int64_t at = n + 32 * t;
-            float s[16];
+                for (int t = 0; t < 2; t++) to[t][0] = *(const uint2*)(gate + 32 * t), to[t][1] = *(const uint2*)(value + 32 * t);
+            }
+        };
+        request(0, held[0]);
 #pragma unroll
-            for (int i = 0; i < 16; i++) s[i] = 0.f;
+        for (int half = 0; half < 2; half++) {
+            float s[2][16];
+#pragma unroll
+            for (int i = 0; i < 32; i++) s[i / 16][i % 16] = 0.f;
 #pragma unroll
             for (int mt = 0; mt < MT; mt++) {
-                const int64_t row = m + 16 * mt;
-                if (row < M && (WHOLE || at < N)) {
-                    float gate[8], value[8];
-                    if constexpr (WHOLE) {
-                        const uint2 a = raw[t & 1][mt][0], b = raw[t & 1][mt][1];
+                const int step = half * MT + mt;
+                if (step + 1 < 2 * MT) request(step + 1, held[(step + 1) & 1]);
+                const bool mine = m + 16 * mt < M;
+                const int64_t row = mine ? m + 16 * mt : M - 1;
+                T* out = (T*)e.out + row * 2 * N;
+#pragma unroll
+                for (int t = 0; t < 2; t++) {
+                    const int64_t at = n + 64 * half + 32 * t;
+                    if (mine && (WHOLE || at < N)) {
+                        float gate[8], value[8];
+                        if constexpr (WHOLE) {
+                            const uint2 a = held[step & 1][t][0], b = held[step & 1][t][1];
+#pragma unroll
+                            for (int i = 0; i < 8; i++) {
+                                gate[i] = code_value(i < 4 ? a.x : a.y, i % 4) * steps[mt][0];
+                                value[i] = code_value(i < 4 ? b.x : b.y, i % 4) * steps[mt][1];
+                            }
+                        } else {
+                            ld_codes<8>(e.codes_in + row * N, at, N, steps[mt][0], gate);
+                            ld_codes<8>(e.codes_in + (M + row) * N, at, N, steps[mt][1], value);
+                        }
 #pragma unroll
                         for (int i = 0; i < 8; i++) {
-                            gate[i] = code_value(i < 4 ? a.x : a.y, i % 4) * steps[mt][0];
-                            value[i] = code_value(i < 4 ? b.x : b.y, i % 4) * steps[mt][1];
+                            const float d = acc[mt][4 * half + 2 * t + (i >> 2)][i & 3], z = gate[i];
+                            float a, da;
+                            act_both<ACT, kFast<T>>(z, a, da);
+                            gate[i] = d * value[i] * da;
+                            value[i] = d * a;
+                            s[t][i] += gate[i], s[t][8 + i] += value[i];
                         }
-                    } else {
-                        ld_codes<8>(e.codes_in + row * N, at, N, steps[mt][0], gate);
-                        ld_codes<8>(e.codes_in + (M + row) * N, at, N, steps[mt][1], value);
+                        st8<T, WHOLE>(out, at, N, gate);
+                        st8<T, WHOLE>(out + N, at, N, value);
                     }
-#pragma unroll
-                    for (int i = 0; i < 8; i++) {
-                        const float d = acc[mt][2 * t + (i >> 2)][i & 3], z = gate[i];
-                        gate[i] = d * value[i] * act_grad<ACT, fast>(z);
-                        value[i] = d * act_value<ACT, fast>(z);
-                        s[i] += gate[i], s[8 + i] += value[i];
-                    }
-                    T* out = (T*)e.out + row * 2 * N;
-                    st8<T, WHOLE>(out, at, N, gate);
-                    st8<T, WHOLE>(out + N, at, N, value);
+                    __builtin_amdgcn_sched_barrier(0);
                 }
-                __builtin_amdgcn_sched_barrier(0);
             }
             if (sums) {
-                const float total = sums_by_lane(s, r);
-                const int64_t c = at + (r & 7);
-                if (WHOLE || c < N) sums[(r >> 3) * N + c] = total;
+#pragma unroll
+                for (int t = 0; t < 2; t++) {
+                    const float total = sums_by_lane(s[t], r);
+                    const int64_t c = n + 64 * half + 32 * t + (r & 7);
+                    if (WHOLE || c < N) sums[(r >> 3) * N + c] = total;
+                }
             }
+            __builtin_amdgcn_sched_barrier(0);
         }
     });
 }
 
+// The same for bfloat16 rows of whole groups of eight columns.  Nothing is stored before the last codes have come: loads and stores
+// complete in the order of their issue, and a load behind stores would be waited for as long as those (us, 65536 x 1024 over 256
+// without sums: 163; without loads 102, without stores 93).  What is stored waits in the sums' registers, both gradients of an entry
+// in one.
+template <int ACT, int MT>
+__device__ __forceinline__ void finish_gate_grad8(const Epilogue& e, f32x4 (&acc)[MT][8], int64_t m, int64_t M, int64_t n, int64_t N, int r, float* sums) {
+    const int64_t G = (N + kPackGroup - 1) / kPackGroup, group = n / kPackGroup;
+    float steps[MT][2];
+#pragma unroll
+    for (int mt = 0; mt < MT; mt++) {
+        const int64_t row = m + 16 * mt < M ? m + 16 * mt : M - 1;
+        steps[mt][0] = e.scales_in[row * G + group], steps[mt][1] = e.scales_in[(M + row) * G + group];
+    }
+    uint2 held[2][2][2];
+    const auto request = [&](int at, uint2(&to)[2][2]) {  // at: half * MT + row; columns behind the last: those of the row's first group
+        const int64_t row = m + 16 * (at % MT) < M ? m + 16 * (at % MT) : M - 1;
+        const int8_t *gate = e.codes_in + row * N, *value = gate + M * N;
+#pragma unroll
+        for (int t = 0; t < 2; t++) {
+            const int64_t c = n + 64 * (at / MT) + 32 * t, from = c < N ? c : 0;
+            to[t][0] = *(const uint2*)(gate + from), to[t][1] = *(const uint2*)(value + from);
+        }
+    };
+    request(0, held[0]);
+#pragma unroll
+    for (int half = 0; half < 2; half++) {
+        float s[2][16];
+#pragma unroll
+        for (int i = 0; i < 32; i++) s[i / 16][i % 16] = 0.f;
+#pragma unroll
+        for (int mt = 0; mt < MT; mt++) {
+            const int step = half * MT + mt;
+            if (step + 1 < 2 * MT) request(step + 1, held[(step + 1) & 1]);
+#pragma unroll
+            for (int t = 0; t < 2; t++) {
+                if (m + 16 * mt < M) {
+                    const uint2 a = held[step & 1][t][0], b = held[step & 1][t][1];
+#pragma unroll
+                    for (int i = 0; i < 8; i++) {
+                        const int nt = 4 * half + 2 * t + (i >> 2);
+                        const float d = acc[mt][nt][i & 3];
+                        const float gate = code_value(i < 4 ? a.x : a.y, i % 4) * steps[mt][0], value = code_value(i < 4 ? b.x : b.y, i % 4) * steps[mt][1];
+                        float u, du;
+                        act_both<ACT, 2>(gate, u, du);
+                        const float dg = d * value * du, dv = d * u;
+                        s[t][i] += dg, s[t][8 + i] += dv;
+                        uint32_t both = pack_bf16(dg, dv);
+                        asm volatile("" : "+v"(both));  // (here and now: left to the compiler, it is done where it is stored, from all it takes)
+                        acc[mt][nt][i & 3] = __uint_as_float(both);
+                    }
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+        if (sums) {
+#pragma unroll
+            for (int t = 0; t < 2; t++) {
+                const float total = sums_by_lane(s[t], r);
+                const int64_t c = n + 64 * half + 32 * t;
+                if (c < N) sums[(r >> 3) * N + c + (r & 7)] = total;
+            }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    }
+#pragma unroll
+    for (int mt = 0; mt < MT; mt++) {
+        const int64_t row = m + 16 * mt;
+        if (row >= M) continue;
+        bf16_t* out = (bf16_t*)e.out + row * 2 * N + n;
+#pragma unroll
+        for (int t = 0; t < 4; t++) {
+            uint32_t gate[4], value[4];
+#pragma unroll
+            for (int i = 0; i < 4; i++) {
+                const uint32_t lo = __float_as_uint(acc[mt][2 * t + (i >> 1)][2 * (i & 1)]), hi = __float_as_uint(acc[mt][2 * t + (i >> 1)][2 * (i & 1) + 1]);
+                gate[i] = __builtin_amdgcn_perm(hi, lo, 0x05040100u), value[i] = __builtin_amdgcn_perm(hi, lo, 0x07060302u);
+            }
+            if (n + 32 * t < N) {
+                *(uint4*)(out + 32 * t) = make_uint4(gate[0], gate[1], gate[2], gate[3]);
+                *(uint4*)(out + N + 32 * t) = make_uint4(value[0], value[1], value[2], value[3]);
+            }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    }
+}
+
 // Workgroups stay for all of their tiles: a tile's first loads are under way while the one before it is finished and stored.
-template <typename E, typename T, int KIND, int TM, int TN, int WM>
+// ACT >= 0: the gate's gradients of that activation, in rows of whole groups of eight columns (one kernel for all of them leaves the
+// compiler no registers).
+template <typename E, typename T, int KIND, int TM, int TN, int WM, int ACT = -1>
 __global__ __launch_bounds__((TM / WM) * (TN / 128) * 64, 2) void k_gemm(const GemmArgs a) {
 #ifdef __HIP_DEVICE_COMPILE__  // (the host's pass does not know all of the builtins, and would leave out the kernel's stub)
     constexpr bool GATED = KIND == kGated, FORWARD = KIND == kForward || GATED, PT = !FORWARD, QT = KIND == kWeightGrad;
@@ -768,15 +865,19 @@ __global__ __launch_bounds__((TM / WM) * (TN / 128) * 64, 2) void k_gemm(const G
                     finish_gated<T, MT, false>(a.e, acc, m, a.m, nl, a.n, g, pack ? scales : nullptr);
             } else if constexpr (KIND == kGatedGrad) {
                 float* col_sums = a.e.col_sums ? a.e.col_sums + ((int64_t)tile_m * (TM / WM) + wm) * 2 * a.n : nullptr;
-                if (nw + WO <= a.n && a.n % 8 == 0)
-                    finish_gate_grad<T, MT, true>(a.e, acc, m, a.m, nl, a.n, r, col_sums);
-                else if (nw < a.n)
+                if constexpr (ACT >= 0) {
+                    if (nw < a.n) finish_gate_grad8<ACT, MT>(a.e, acc, m, a.m, nl, a.n, r, col_sums);
+                } else if (sizeof(T) == 4 && nw + WO <= a.n && a.n % 8 == 0) {
+                    if constexpr (sizeof(T) == 4) finish_gate_grad<T, MT, true>(a.e, acc, m, a.m, nl, a.n, r, col_sums);
+                } else if (nw < a.n) {
                     finish_gate_grad<T, MT, false>(a.e, acc, m, a.m, nl, a.n, r, col_sums);
+                }
             } else {
+                constexpr int kForm = sizeof(E) == 1 ? kFast<T> : sizeof(T) == 2;
                 if (nw + WN <= a.n && a.n % 8 == 0)
-                    finish_rows<T, KIND, MT, true>(a.e, acc, m, a.m, nl, a.n, g);
+                    finish_rows<T, KIND, kForm, MT, true>(a.e, acc, m, a.m, nl, a.n, g);
                 else if (nw < a.n)
-                    finish_rows<T, KIND, MT, false>(a.e, acc, m, a.m, nl, a.n, g);
+                    finish_rows<T, KIND, kForm, MT, false>(a.e, acc, m, a.m, nl, a.n, g);
             }
         }
         if (t + stride >= end) break;
@@ -786,14 +887,14 @@ __global__ __launch_bounds__((TM / WM) * (TN / 128) * 64, 2) void k_gemm(const G
 #endif
 }
 
-template <typename E, typename T, int KIND, int TM, int TN, int WM>
+template <typename E, typename T, int KIND, int TM, int TN, int WM, int ACT = -1>
 cat_status launch_gemm_tiles(const GemmArgs& a, hipStream_t st) {
     constexpr int TO = KIND == kGated ? TN / 2 : TN;
     const int64_t tiles = ((a.m + TM - 1) / TM) * ((a.n + TO - 1) / TO);
     if (tiles >= (1ll << 31)) return set_error(CAT_ERR_UNSUPPORTED, "product of %lld x %lld entries has too many tiles", (long long)a.m, (long long)a.n);
     // as many workgroups as the card holds at a time (256 CUs, by LDS one large tile's or two small ones' each)
     const int64_t most = 256 * (TM == 256 ? 1 : 2);
-    hipLaunchKernelGGL((k_gemm<E, T, KIND, TM, TN, WM>), dim3((unsigned)(a.splits > 1 || tiles < most ? tiles : most), (unsigned)a.splits), dim3((TM / WM) * (TN / 128) * 64), 0, st, a);
+    hipLaunchKernelGGL((k_gemm<E, T, KIND, TM, TN, WM, ACT>), dim3((unsigned)(a.splits > 1 || tiles < most ? tiles : most), (unsigned)a.splits), dim3((TM / WM) * (TN / 128) * 64), 0, st, a);
     CAT_LAUNCH_CHECK("k_gemm");
     return CAT_OK;
 }

@@ -86,7 +86,7 @@ __device__ __forceinline__ void finish_gate(const Epilogue& e, int64_t m, int64_
     float v[W];
     with_act(e.act, [&](auto which) {
 #pragma unroll
-        for (int i = 0; i < W; i++) v[i] = act_value<decltype(which)::value, sizeof(T) == 2>(gate[i]) * value[i];
+        for (int i = 0; i < W; i++) v[i] = act_value<decltype(which)::value, kFast<T>>(gate[i]) * value[i];
     });
     st_entries<T, W>((T*)e.out + m * N, n, N, v);
 }
@@ -197,7 +197,7 @@ __global__ __launch_bounds__(kFewWaves * kWave) void k_few_rows(const E* __restr
         scaled<E, 4>(e, m, nn, N, v[0]);
         Epilogue rest = e;
         rest.bias = nullptr;
-        finish<T, kForward, 4, false>(rest, m, nn, N, true, v[0]);
+        finish<T, kForward, 4, false, kFast<T>>(rest, m, nn, N, true, v[0]);
     } else {
         finish<T, kForward, 4, false>(e, m, nn, N, true, v[0]);
     }
@@ -237,7 +237,7 @@ __global__ __launch_bounds__(256) void k_join(const float* __restrict__ parts, i
                 if (n < N) scaled<E, 8>(e, m, n, N, v);
                 Epilogue rest = e;
                 rest.bias = nullptr;
-                finish<T, KIND, 8, true>(rest, m, n, N, t < n16, v);
+                finish<T, KIND, 8, true, kFast<T>>(rest, m, n, N, t < n16, v);
             } else {
                 finish<T, KIND, 8, true>(e, m, n, N, t < n16, v);
             }
@@ -275,7 +275,7 @@ __global__ __launch_bounds__(256) void k_lay_out(const Layout<T> first, const La
             ld_codes<V>(a.codes + row * a.cols, j, a.cols, a.scales[row * G + j / kPackGroup], v);
             with_act(act, [&](auto which) {  // act(0) = 0 behind the row's end
 #pragma unroll
-                for (int e = 0; e < V; e++) v[e] = act_value<decltype(which)::value, sizeof(T) == 2>(v[e]);
+                for (int e = 0; e < V; e++) v[e] = act_value<decltype(which)::value, FROM == kFromGated ? kFast<T> : sizeof(T) == 2>(v[e]);
             });
             if constexpr (FROM == kFromGated) {
                 float value[V];
