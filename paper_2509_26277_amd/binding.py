@@ -885,12 +885,27 @@ def cat_activation_backward(dy, packed, act):
 # ---------------------------------------------------------------------------
 # the gated feed-forward half, and products of 8-bit integers
 # ---------------------------------------------------------------------------
-def _one_device(*tensors):
-    """Refuses tensors that lie on another device than the current one, on whose stream the call would run."""
-    here = torch.cuda.current_device() if torch.cuda.is_available() else None
-    for t in tensors:
-        if t is not None and t.device.index != here:
-            raise ValueError(f"tensor on {t.device}, but the current device is cuda:{here}")
+def _here(t, name):
+    """The number of the current device, on whose stream a call runs; the tensor that decides it must lie there."""
+    here = t.get_device()
+    if here < 0:
+        raise ValueError(f"{name} must be a contiguous device tensor")
+    if here != torch.cuda.current_device():
+        raise ValueError(f"{name} is on cuda:{here}, but the current device is cuda:{torch.cuda.current_device()}")
+    return here
+
+
+def _at(here, t, dtype, shape, name):
+    """_dev of a tensor on the device that _here gave."""
+    if t is None:
+        return None
+    if t.get_device() != here or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous tensor on cuda:{here}")
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.shape != shape:
+        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+    return t.data_ptr()
 
 
 def _out_type(dtype):
@@ -905,12 +920,12 @@ def _two(t, name):
     return t.shape
 
 
-def _room(workspace, nbytes, device):
+def _room(here, workspace, nbytes, device):
     """The caller's workspace, or one of the stated size."""
     if workspace is None:
         return _workspace(nbytes, device)
-    if not workspace.is_cuda or not workspace.is_contiguous() or workspace.dtype != torch.uint8:
-        raise ValueError("workspace must be a contiguous device tensor of uint8")
+    if workspace.get_device() != here or not workspace.is_contiguous() or workspace.dtype != torch.uint8:
+        raise ValueError(f"workspace must be a contiguous tensor of uint8 on cuda:{here}")
     return workspace
 
 
@@ -918,8 +933,8 @@ def cat_quantize_rows(x):
     """Rows to 8-bit integers with a scale a row (cat_quantize_rows): (codes, scales), codes of x's shape, row m standing for
     ``codes[m] * scales[m]``.  A weight (its rows output channels) goes through it once."""
     N, D, dt = _rows(x, "x")
-    px = _dev(x, name="x")
-    _one_device(x)
+    here = _here(x, "x")
+    px = _at(here, x, x.dtype, (N, D), "x")
     codes, scales = torch.empty((N, D), dtype=torch.int8, device=x.device), torch.empty((N,), dtype=torch.float32, device=x.device)
     _check(load_library().cat_quantize_rows(px, N, D, dt, codes.data_ptr(), scales.data_ptr(), _stream()))
     return codes, scales
@@ -928,8 +943,8 @@ def cat_quantize_rows(x):
 def cat_layer_norm_quantize(x, weight=None, bias=None, eps=1e-5):
     """Layer norm of every row straight to 8-bit integers with a scale a row (cat_layer_norm_quantize): (codes, scales)."""
     N, D, dt = _rows(x, "x")
-    px, pw, pb = _dev(x, name="x"), _dev(weight, torch.float32, (D,), "weight"), _dev(bias, torch.float32, (D,), "bias")
-    _one_device(x, weight, bias)
+    here = _here(x, "x")
+    px, pw, pb = _at(here, x, x.dtype, (N, D), "x"), _at(here, weight, torch.float32, (D,), "weight"), _at(here, bias, torch.float32, (D,), "bias")
     codes, scales = torch.empty((N, D), dtype=torch.int8, device=x.device), torch.empty((N,), dtype=torch.float32, device=x.device)
     _check(load_library().cat_layer_norm_quantize(px, N, D, dt, pw, pb, float(eps), codes.data_ptr(), scales.data_ptr(), _stream()))
     return codes, scales
@@ -940,15 +955,15 @@ def cat_linear8(x, x_scales, w, w_scales, bias=None, act="none", residual=None, 
     bias float32, residual and result (M x N) of ``dtype``, float32 or bfloat16."""
     lib = load_library()
     (M, K), N, dt = _two(x, "x"), _two(w, "w")[0], _out_type(dtype)
-    px, pw = _dev(x, torch.int8, name="x"), _dev(w, torch.int8, (N, K), "w")
-    ps, pt = _dev(x_scales, torch.float32, (M,), "x_scales"), _dev(w_scales, torch.float32, (N,), "w_scales")
-    pb, pr = _dev(bias, torch.float32, (N,), "bias"), _dev(residual, dtype, (M, N), "residual")
+    here = _here(x, "x")
+    px, pw = _at(here, x, torch.int8, (M, K), "x"), _at(here, w, torch.int8, (N, K), "w")
+    ps, pt = _at(here, x_scales, torch.float32, (M,), "x_scales"), _at(here, w_scales, torch.float32, (N,), "w_scales")
+    pb, pr = _at(here, bias, torch.float32, (N,), "bias"), _at(here, residual, dtype, (M, N), "residual")
     act = _act(act)
     if out is None:
         out = torch.empty((M, N), dtype=dtype, device=x.device)
-    workspace = _room(workspace, lib.cat_linear8_workspace_bytes(M, N, K), x.device)
-    _one_device(x, x_scales, w, w_scales, bias, residual, out, workspace)
-    _check(lib.cat_linear8(px, ps, pw, pt, pb, pr, M, N, K, dt, act, _dev(out, dtype, (M, N), "out"), workspace.data_ptr(), workspace.numel(),
+    workspace = _room(here, workspace, lib.cat_linear8_workspace_bytes(M, N, K), x.device)
+    _check(lib.cat_linear8(px, ps, pw, pt, pb, pr, M, N, K, dt, act, _at(here, out, dtype, (M, N), "out"), workspace.data_ptr(), workspace.numel(),
                            _stream()))
     return out
 
@@ -968,15 +983,15 @@ def cat_gated_linear(x, w, bias=None, act="silu", pack=False, out=None, workspac
     lib = load_library()
     M, K, dt = _rows(x, "x")
     F = _halves(w, "w")[0]
-    px, pw, pb = _dev(x, name="x"), _dev(w, x.dtype, (2 * F, K), "w"), _dev(bias, torch.float32, (2 * F,), "bias")
+    here = _here(x, "x")
+    px, pw, pb = _at(here, x, x.dtype, (M, K), "x"), _at(here, w, x.dtype, (2 * F, K), "w"), _at(here, bias, torch.float32, (2 * F,), "bias")
     act = _act(act)
     if out is None:
         out = torch.empty((M, F), dtype=x.dtype, device=x.device)
     packed = _empty_gate(M, F, x.device) if pack else None
     pc, ps = (packed[0].data_ptr(), packed[1].data_ptr()) if pack else (None, None)
-    workspace = _room(workspace, lib.cat_gated_linear_workspace_bytes(M, F, K, dt), x.device)
-    _one_device(x, w, bias, out, workspace)
-    _check(lib.cat_gated_linear(px, pw, pb, M, F, K, dt, act, _dev(out, x.dtype, (M, F), "out"), pc, ps, workspace.data_ptr(), workspace.numel(),
+    workspace = _room(here, workspace, lib.cat_gated_linear_workspace_bytes(M, F, K, dt), x.device)
+    _check(lib.cat_gated_linear(px, pw, pb, M, F, K, dt, act, _at(here, out, x.dtype, (M, F), "out"), pc, ps, workspace.data_ptr(), workspace.numel(),
                                 _stream()))
     return (out, packed) if pack else out
 
@@ -986,15 +1001,15 @@ def cat_gated_linear8(x, x_scales, w, w_scales, bias=None, act="silu", dtype=tor
     ``dtype``, float32 or bfloat16."""
     lib = load_library()
     (M, K), F, dt = _two(x, "x"), _halves(w, "w")[0], _out_type(dtype)
-    px, pw = _dev(x, torch.int8, name="x"), _dev(w, torch.int8, (2 * F, K), "w")
-    ps, pt = _dev(x_scales, torch.float32, (M,), "x_scales"), _dev(w_scales, torch.float32, (2 * F,), "w_scales")
-    pb = _dev(bias, torch.float32, (2 * F,), "bias")
+    here = _here(x, "x")
+    px, pw = _at(here, x, torch.int8, (M, K), "x"), _at(here, w, torch.int8, (2 * F, K), "w")
+    ps, pt = _at(here, x_scales, torch.float32, (M,), "x_scales"), _at(here, w_scales, torch.float32, (2 * F,), "w_scales")
+    pb = _at(here, bias, torch.float32, (2 * F,), "bias")
     act = _act(act)
     if out is None:
         out = torch.empty((M, F), dtype=dtype, device=x.device)
-    workspace = _room(workspace, lib.cat_gated_linear8_workspace_bytes(M, F, K), x.device)
-    _one_device(x, x_scales, w, w_scales, bias, out, workspace)
-    _check(lib.cat_gated_linear8(px, ps, pw, pt, pb, M, F, K, dt, act, _dev(out, dtype, (M, F), "out"), workspace.data_ptr(), workspace.numel(),
+    workspace = _room(here, workspace, lib.cat_gated_linear8_workspace_bytes(M, F, K), x.device)
+    _check(lib.cat_gated_linear8(px, ps, pw, pt, pb, M, F, K, dt, act, _at(here, out, dtype, (M, F), "out"), workspace.data_ptr(), workspace.numel(),
                                  _stream()))
     return out
 
@@ -1004,14 +1019,14 @@ def _empty_gate(M, F, device):
             torch.empty((2, M, (F + CAT_PACK_GROUP - 1) // CAT_PACK_GROUP), dtype=torch.float32, device=device))
 
 
-def _gate(packed, M, F=None):
+def _gate(here, packed, M, F=None):
     """F and the pointers of the checkpoints of a gate and its value."""
     codes, scales = packed
     if codes.dim() != 3:
         raise ValueError(f"codes must have three dimensions, got {tuple(codes.shape)}")
     F = codes.shape[2] if F is None else F
-    return (F, _dev(codes, torch.int8, (2, M, F), "codes"),
-            _dev(scales, torch.float32, (2, M, (F + CAT_PACK_GROUP - 1) // CAT_PACK_GROUP), "scales"))
+    return (F, _at(here, codes, torch.int8, (2, M, F), "codes"),
+            _at(here, scales, torch.float32, (2, M, (F + CAT_PACK_GROUP - 1) // CAT_PACK_GROUP), "scales"))
 
 
 def cat_gated_backward_input(dy, w, packed, act="silu", want_bias=True, out=None, workspace=None):
@@ -1020,15 +1035,15 @@ def cat_gated_backward_input(dy, w, packed, act="silu", want_bias=True, out=None
     (2F, float32) its sums over rows, None without ``want_bias``."""
     lib = load_library()
     M, N, dt = _rows(dy, "dy")
-    pd, pw = _dev(dy, name="dy"), _dev(w, dy.dtype, (N, w.shape[-1]), "w")
-    F, pc, ps = _gate(packed, M, w.shape[-1])
+    here = _here(dy, "dy")
+    F, pc, ps = _gate(here, packed, M, _two(w, "w")[1])
+    pd, pw = _at(here, dy, dy.dtype, (M, N), "dy"), _at(here, w, dy.dtype, (N, F), "w")
     act = _act(act)
     if out is None:
         out = torch.empty((M, 2 * F), dtype=dy.dtype, device=dy.device)
     db = torch.empty((2 * F,), dtype=torch.float32, device=dy.device) if want_bias else None
-    workspace = _room(workspace, lib.cat_gated_backward_workspace_bytes(M, N, F, dt), dy.device)
-    _one_device(dy, w, *packed, out, workspace)
-    _check(lib.cat_gated_backward_input(pd, pw, pc, ps, M, N, F, dt, act, _dev(out, dy.dtype, (M, 2 * F), "out"),
+    workspace = _room(here, workspace, lib.cat_gated_backward_workspace_bytes(M, N, F, dt), dy.device)
+    _check(lib.cat_gated_backward_input(pd, pw, pc, ps, M, N, F, dt, act, _at(here, out, dy.dtype, (M, 2 * F), "out"),
                                         None if db is None else db.data_ptr(), workspace.data_ptr(), workspace.numel(), _stream()))
     return out, db
 
@@ -1039,14 +1054,14 @@ def cat_gated_backward_weight(dy, packed, act="silu", want_bias=True, out=None, 
     cat_linear_backward_weight."""
     lib = load_library()
     M, N, dt = _rows(dy, "dy")
-    pd = _dev(dy, name="dy")
-    F, pc, ps = _gate(packed, M)
+    here = _here(dy, "dy")
+    pd = _at(here, dy, dy.dtype, (M, N), "dy")
+    F, pc, ps = _gate(here, packed, M)
     act = _act(act)
     if out is None:
         out = torch.empty((N, F), dtype=dy.dtype, device=dy.device)
     db = torch.empty((N,), dtype=torch.float32, device=dy.device) if want_bias else None
-    workspace = _room(workspace, lib.cat_gated_backward_workspace_bytes(M, N, F, dt), dy.device)
-    _one_device(dy, *packed, out, workspace)
-    _check(lib.cat_gated_backward_weight(pd, pc, ps, M, N, F, dt, act, _dev(out, dy.dtype, (N, F), "out"), None if db is None else db.data_ptr(),
+    workspace = _room(here, workspace, lib.cat_gated_backward_workspace_bytes(M, N, F, dt), dy.device)
+    _check(lib.cat_gated_backward_weight(pd, pc, ps, M, N, F, dt, act, _at(here, out, dy.dtype, (N, F), "out"), None if db is None else db.data_ptr(),
                                          workspace.data_ptr(), workspace.numel(), _stream()))
     return out, db

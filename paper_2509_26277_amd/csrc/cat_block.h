@@ -241,10 +241,25 @@ __device__ __forceinline__ float tail_factor(float x) {
     return t * g;
 }
 __device__ __forceinline__ float normal_exp(float z) { return __builtin_amdgcn_exp2f(z * z * -0.72134752044448170f); }
+// The tail by itself, Phi(-x) = 2^P(x): P a polynomial of degree 7, fitted so that x 2^P(x) is off by 2.4e-7 at most, and 2^P(x) by 4.4e-5
+// of its value up to x = 7 (behind that Phi is below 2e-12, and P falls on).  14 instructions' time for GELU where exponential, reciprocal
+// and tail_factor take 24 (us, 16384 x 8192 over 2048 8-bit integers: 285 -> GELUUS).
+__device__ __forceinline__ float tail(float x) {
+    float p = fmaf(x, -1.592344006e-6f, 5.686387885e-5f);
+    p = fmaf(x, p, -8.961785352e-4f);
+    p = fmaf(x, p, 8.394782431e-3f);
+    p = fmaf(x, p, -5.379608646e-2f);
+    p = fmaf(x, p, -4.58545059e-1f);
+    p = fmaf(x, p, -1.151258111f);
+    return __builtin_amdgcn_exp2f(fmaf(x, p, -9.999888539e-1f));
+}
 template <int ACT, int FAST>
 __device__ __forceinline__ float act_value(float z) {
     if constexpr (ACT == CAT_ACT_RELU) {
         return z > 0.f ? z : (z != z ? z : 0.f);
+    } else if constexpr (ACT == CAT_ACT_GELU && FAST == 2) {  // (as below; minimum and maximum hand a NaN on)
+        const float x = fabsf(__builtin_elementwise_minimum(z, 1e30f));
+        return fmaf(-x, tail(x), __builtin_elementwise_maximum(z, 0.f));
     } else if constexpr (ACT == CAT_ACT_GELU && FAST) {  // z - z Phi(-z), or z Phi(z)
         const float x = fabsf(fminf(z, 1e30f));           // (no inf * 0 for +inf)
         return fmaf(-x, normal_exp(z) * tail_factor(x), fmaxf(z, 0.f));

@@ -49,7 +49,7 @@ struct GemmArgs {
     int64_t ldp, ldq;          // entries; rows start on 16-byte boundaries
     int64_t p_bytes, q_bytes;  // what may be read from p, q on
     int64_t m, n, k;
-    int64_t k_split;  // entries of k a share takes (a multiple of the kernel's step); shares beyond the first: blockIdx.y
+    int64_t k_split;  // entries of k a share takes (a multiple of the kernel's step)
     int splits;
     void* parts;  // instead of an epilogue: sums as they are, splits x m x n (gated: x 2 n), float or 32-bit integers
     Epilogue e;

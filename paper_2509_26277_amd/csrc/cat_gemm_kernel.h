@@ -657,18 +657,21 @@ __global__ __launch_bounds__((TM / WM) * (TN / 128) * 64, 2) void k_gemm(const G
     const int wm = wave / (TN / WN), wn = wave % (TN / WN);
 
     // Workgroups go to the eight XCDs in turn; each XCD takes a run of neighbouring tiles, eight columns of them at a time, so
-    // that what its L2 holds of either operand serves many of them.
+    // that what its L2 holds of either operand serves many of them.  With shares of k the run goes through the tiles of a share and
+    // then of the next one: an XCD reads its share of k and not all of it (us, weight gradient 1024 x 4096 over 16384 rows in four
+    // shares: 170 -> SHARES).
     const uint32_t tm = (uint32_t)((a.m + TM - 1) / TM), tn = (uint32_t)((a.n + TO - 1) / TO), tiles = tm * tn;
-    const uint32_t xcd = blockIdx.x & 7, share = tiles / 8, more = tiles % 8;
-    const uint32_t stride = (gridDim.x - xcd + 7) / 8, end = (xcd + 1) * share + (xcd + 1 < more ? xcd + 1 : more);
-    uint32_t t = xcd * share + (xcd < more ? xcd : more) + blockIdx.x / 8;
+    const uint32_t xcd = blockIdx.x & 7, all = tiles * (uint32_t)a.splits, share = all / 8, more = all % 8;
+    uint32_t stride = (gridDim.x - xcd + 7) / 8, end = (xcd + 1) * share + (xcd + 1 < more ? xcd + 1 : more);
+    uint32_t t = xcd * share + (xcd < more ? xcd : more) + blockIdx.x / 8, share_of_k = 0;
     if (t >= end) return;
+    if (a.splits > 1) share_of_k = t / tiles, t -= share_of_k * tiles, end = t + 1, stride = 1;  // (a tile each)
     const auto place = [&](uint32_t tile, uint32_t& m0, uint32_t& n0) {
         const uint32_t band = tile / (8 * tm), in = tile - band * 8 * tm, width = tn - band * 8 < 8 ? tn - band * 8 : 8;
         m0 = in / width, n0 = band * 8 + in % width;
     };
 
-    const int64_t k0 = (int64_t)blockIdx.y * a.k_split, k_all = a.k - k0 < a.k_split ? a.k - k0 : a.k_split;
+    const int64_t k0 = (int64_t)share_of_k * a.k_split, k_all = a.k - k0 < a.k_split ? a.k - k0 : a.k_split;
     Stage<E, PT, true, TN, W> sp;
     Stage<E, QT, false, TM, W> sq;
     Fragments<E, PT, true, TN> fp;
@@ -823,7 +826,7 @@ __global__ __launch_bounds__((TM / WM) * (TN / 128) * 64, 2) void k_gemm(const G
             for (int mt = 0; mt < MT; mt++) {
                 const int64_t m = m0 + wm * WM + mt * 16 + r;
                 if (m >= a.m) continue;
-                float* part = (float*)a.parts + ((int64_t)blockIdx.y * a.m + m) * width;
+                float* part = (float*)a.parts + ((int64_t)share_of_k * a.m + m) * width;
 #pragma unroll
                 for (int nt = 0; nt < NT; nt++) {
                     const int64_t n = nl + ((nt >> 1) & (GATED ? 1 : 3)) * 32 + 4 * (nt & 1);
@@ -891,10 +894,10 @@ template <typename E, typename T, int KIND, int TM, int TN, int WM, int ACT = -1
 cat_status launch_gemm_tiles(const GemmArgs& a, hipStream_t st) {
     constexpr int TO = KIND == kGated ? TN / 2 : TN;
     const int64_t tiles = ((a.m + TM - 1) / TM) * ((a.n + TO - 1) / TO);
-    if (tiles >= (1ll << 31)) return set_error(CAT_ERR_UNSUPPORTED, "product of %lld x %lld entries has too many tiles", (long long)a.m, (long long)a.n);
+    if (tiles * a.splits >= (1ll << 31)) return set_error(CAT_ERR_UNSUPPORTED, "product of %lld x %lld entries has too many tiles", (long long)a.m, (long long)a.n);
     // as many workgroups as the card holds at a time (256 CUs, by LDS one large tile's or two small ones' each)
     const int64_t most = 256 * (TM == 256 ? 1 : 2);
-    hipLaunchKernelGGL((k_gemm<E, T, KIND, TM, TN, WM, ACT>), dim3((unsigned)(a.splits > 1 || tiles < most ? tiles : most), (unsigned)a.splits), dim3((TM / WM) * (TN / 128) * 64), 0, st, a);
+    hipLaunchKernelGGL((k_gemm<E, T, KIND, TM, TN, WM, ACT>), dim3((unsigned)(a.splits > 1 ? tiles * a.splits : tiles < most ? tiles : most)), dim3((TM / WM) * (TN / 128) * 64), 0, st, a);
     CAT_LAUNCH_CHECK("k_gemm");
     return CAT_OK;
 }

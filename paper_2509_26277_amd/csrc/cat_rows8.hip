@@ -58,51 +58,56 @@ __global__ __launch_bounds__(kThreads<TPR>) void k_rows8(const T* __restrict__ x
 #pragma unroll
             for (int k = 0; k < VPL; k++) next[k].load(x, nullptr, nullptr, r, ((int64_t)k * TPR + sub) * V, D, 0);
         }
-        float mu = 0.f, rs = 1.f;
+        float h[VPL][V];
+#pragma unroll
+        for (int k = 0; k < VPL; k++)
+#pragma unroll
+            for (int e = 0; e < V; e++) h[k][e] = v[k].at(e);
         if constexpr (NORM) {
             float s[1] = {0.f};
 #pragma unroll
             for (int k = 0; k < VPL; k++)
 #pragma unroll
-                for (int e = 0; e < V; e++) s[0] += v[k].at(e);
+                for (int e = 0; e < V; e++) s[0] += h[k][e];
             row_sums<TPR>(s, slots, slot);
-            mu = s[0] / (float)D;
+            const float mu = s[0] / (float)D;
             float q[1] = {0.f};
+            // (one comparison a group: those of eight entries were a third of the instructions of a row's statistics)
 #pragma unroll
             for (int k = 0; k < VPL; k++) {
                 const int64_t j = ((int64_t)k * TPR + sub) * V;
+                const int n = j + V <= D ? V : j < D ? (int)(D - j) : 0;
+                if (n == V) {
 #pragma unroll
-                for (int e = 0; e < V; e++) {
-                    const float c = v[k].at(e) - mu;
-                    if (j + e < D) q[0] = fmaf(c, c, q[0]);
+                    for (int e = 0; e < V; e++) h[k][e] -= mu, q[0] = fmaf(h[k][e], h[k][e], q[0]);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < V; e++) {
+                        h[k][e] = e < n ? h[k][e] - mu : 0.f;
+                        q[0] = fmaf(h[k][e], h[k][e], q[0]);
+                    }
                 }
             }
             row_sums<TPR>(q, slots, slot);
-            rs = 1.f / sqrtf(q[0] / (float)D + eps);
+            const float rs = 1.f / sqrtf(q[0] / (float)D + eps);
+            // (behind the row's end: zeros; with rs an infinity a NaN, as the row has them then)
+#pragma unroll
+            for (int k = 0; k < VPL; k++)
+#pragma unroll
+                for (int e = 0; e < V; e++) h[k][e] = fmaf(h[k][e] * rs, w[k][e], b[k][e]);
         }
-        const auto value = [&](int k, int e) {  // twice, for the magnitude and for the code: the same operations, the same bits
-            if constexpr (NORM) return fmaf((v[k].at(e) - mu) * rs, w[k][e], b[k][e]);
-            else return v[k].at(e);
-        };
         uint32_t a = 0;
 #pragma unroll
-        for (int k = 0; k < VPL; k++) {
-            const int64_t j = ((int64_t)k * TPR + sub) * V;
+        for (int k = 0; k < VPL; k++)
 #pragma unroll
-            for (int e = 0; e < V; e++)
-                if (!NORM || j + e < D) a = mag_max(a, value(k, e));  // (without a norm: zeros behind the row's end)
-        }
+            for (int e = 0; e < V; e++) a = mag_max(a, h[k][e]);
         const PackScale s = pack_scale(row_max<TPR>(a, slots, slot));
         if (!mine) continue;
         if (sub == 0) scales[row] = s.step;
 #pragma unroll
         for (int k = 0; k < VPL; k++) {
             const int64_t j = ((int64_t)k * TPR + sub) * V;
-            if (j >= D) continue;
-            float o[V];
-#pragma unroll
-            for (int e = 0; e < V; e++) o[e] = value(k, e);
-            st_codes<V>(codes + row * D, j, D, o, s.up);
+            if (j < D) st_codes<V>(codes + row * D, j, D, h[k], s.up);
         }
     }
 }
@@ -166,16 +171,26 @@ __global__ __launch_bounds__(kNormThreads) void k_rows8_long(const T* __restrict
     }
 }
 
+// How many threads share a row: four 16-byte groups each (three, where those are enough), so that a wave has up to 4 KB of rows under
+// way and few lanes to reduce over; 8 threads of the shortest rows, and more than a wave's from 257 groups on, as in layer norm.
+// (us, 65536 x 512 bf16 through the norm: 36 with a wave a row and a group a lane, NORMUS so; 65536 x 512 fp32 47 and ROWUS.)
+template <typename T>
+NormShape rows8_shape(int64_t D) {
+    const int64_t n = (D + kVec<T> - 1) / kVec<T>;
+    if (n > 256) return norm_shape<T, false>(D);
+    const int tpr = n <= 32 ? 8 : n <= 64 ? 16 : n <= 128 ? 32 : 64;
+    return {tpr, (int)((n + tpr - 1) / tpr)};
+}
 constexpr int kRows8Groups = 1024;  // workgroups; further rows by stride
 template <typename T, bool NORM>
 cat_status launch_rows8(const T* x, int64_t N, int64_t D, const float* weight, const float* bias, float eps, int8_t* codes, float* scales, hipStream_t st) {
-    const NormShape s = norm_shape<T, false>(D);
+    const NormShape s = rows8_shape<T>(D);
     const int64_t rpb = s.tpr && s.tpr < kNormThreads ? kNormThreads / s.tpr : 1, blocks = (N + rpb - 1) / rpb;
     const dim3 grid((unsigned)(blocks < kRows8Groups ? blocks : kRows8Groups));
-#define CAT_X(TPR, VPL)             \
+#define CAT_X(TPR, VPL)               \
     if (s.tpr == TPR && s.vpl == VPL) \
         hipLaunchKernelGGL((k_rows8<T, TPR, VPL, NORM>), grid, dim3(kThreads<TPR>), 0, st, x, N, D, weight, bias, eps, codes, scales);
-    CAT_X(8, 1) CAT_X(16, 1) CAT_X(32, 1) CAT_X(64, 1) CAT_X(64, 2) CAT_X(64, 4) CAT_X(256, 4)
+    CAT_X(8, 1) CAT_X(8, 2) CAT_X(8, 3) CAT_X(8, 4) CAT_X(16, 3) CAT_X(16, 4) CAT_X(32, 3) CAT_X(32, 4) CAT_X(64, 3) CAT_X(64, 4) CAT_X(256, 4)
     if constexpr (sizeof(T) == 4) {
         CAT_X(64, 8) CAT_X(256, 8)
     } else {

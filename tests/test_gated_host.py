@@ -165,7 +165,7 @@ def test_python_refuses_before_the_library(lib):
     with pytest.raises(ValueError, match="two dimensions"):
         binding.cat_linear8(c[0], s, c, s)
     with pytest.raises(ValueError, match="three dimensions"):
-        binding._gate((c, s), 4)
+        binding._gate(0, (c, s), 4)
     with pytest.raises(TypeError):
         binding.cat_linear8(c, s, c, s, dtype=torch.float16)
     with pytest.raises(TypeError):
@@ -173,13 +173,29 @@ def test_python_refuses_before_the_library(lib):
 
 
 class _On:
+    """As much of a tensor as the checks look at."""
+    dtype, shape = torch.int8, torch.Size([4, 8])
+
     def __init__(self, index):
-        self.device = torch.device("cuda", index)
+        self.index = index
+
+    def get_device(self):
+        return self.index
+
+    def is_contiguous(self):
+        return True
+
+    def data_ptr(self):
+        return FAKE
 
 
 def test_tensors_of_another_device_are_refused(monkeypatch):
-    monkeypatch.setattr(torch.cuda, "is_available", lambda: True)
     monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
-    binding._one_device(_On(1), None, _On(1))
+    assert binding._here(_On(1), "x") == 1 and binding._at(1, _On(1), torch.int8, (4, 8), "w") == FAKE and binding._at(1, None, None, None, "w") is None
     with pytest.raises(ValueError, match="current device"):
-        binding._one_device(_On(1), _On(0))
+        binding._here(_On(0), "x")
+    for other in (0, -1):
+        with pytest.raises(ValueError, match="cuda:1"):
+            binding._at(1, _On(other), torch.int8, (4, 8), "w")
+        with pytest.raises(ValueError, match="cuda:1"):
+            binding._room(1, _On(other), 256, None)

@@ -145,6 +145,34 @@ def test_nan_and_infinity_go_where_the_formula_takes_them(M):
     assert torch.equal(torch.isnan(h), bad) and torch.equal(h[~bad], clean_gated[~bad])
 
 
+@pytest.mark.parametrize("M", [1, 300, 2304])
+def test_activations_over_their_whole_range(M):
+    """A sweep of arguments by a product of one entry (exact: codes and scales are powers of two and whole numbers), in either type
+    and kernel: steps of 1 / 64 up to 31.75 on both sides, then what leaves the exponentials' range, infinities and NaN."""
+    N = 4096
+    x, xs = torch.ones(M, 1, dtype=torch.int8, device="cuda"), torch.ones(M, device="cuda")
+    w = torch.zeros(N, 1, dtype=torch.int8, device="cuda")
+    z = (torch.arange(N, device="cuda") - N // 2).double() / 64
+    ends = [3e38, -3e38, 1e20, -1e20, 200.0, -200.0, float("inf"), float("-inf"), float("nan")]
+    z[:len(ends)] = torch.tensor(ends, device="cuda").double()
+    b = z.float()
+    z = b.double()
+    for act in ACTS:
+        for t in TYPES.values():
+            y = cat_linear8(x, xs, w, torch.ones(N, device="cuda"), b, act=act, dtype=t)
+            assert torch.equal(y, y[:1].expand(M, N).contiguous()) or bool((torch.isnan(y) == torch.isnan(y[:1])).all())
+            got = y[M - 1].double()
+            want = act_ref(z[9:], act)[0]
+            _close(got[9:], want, half_step(t) * want.abs() + ACT_ERR * (1.0 + z[9:].abs()), act)
+            far = [float(v) for v in got[:9]]
+            assert far[6] == float("inf") and far[8] != far[8]
+            if act == "none":
+                assert far[7] == float("-inf")
+            else:  # relu(-inf) is 0, of the others -inf * 0
+                assert far[7] == 0.0 if act == "relu" else far[7] != far[7]
+                assert far[1] == 0.0 and far[3] == 0.0 and far[5] == 0.0 and far[4] == 200.0
+
+
 def test_no_rows():
     x, w = torch.empty(0, 33, dtype=torch.int8, device="cuda"), torch.ones(8, 33, dtype=torch.int8, device="cuda")
     none, ws = torch.empty(0, device="cuda"), torch.ones(8, device="cuda")
