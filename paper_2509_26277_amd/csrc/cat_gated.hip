@@ -78,7 +78,7 @@ extern "C" {
 
 size_t cat_gated_linear_workspace_bytes(int64_t M, int64_t F, int64_t K, cat_dtype dt) {
     if (check_linear("cat_gated_linear_workspace_bytes", M, F, K, dt) != CAT_OK) return 0;
-    const size_t a = plan_gated(M, F, K, dt, false).total, b = plan_gated(M, F, K, dt, true).total;
+    const size_t a = plan_gated(M - tail_rows(kGated, M, F, K, entry_bytes(dt)), F, K, dt, false).total, b = plan_gated(M, F, K, dt, true).total;
     return a > b ? a : b;
 }
 
@@ -93,7 +93,8 @@ cat_status cat_gated_linear(const void* x, const void* w, const float* bias, int
     CAT_TRY(check_ptr(who, "y", y, M > 0));
     CAT_TRY(check_checkpoint(who, codes, scales));
     if (M > 0 && (y == x || y == w || y == bias)) return set_error(CAT_ERR_INVALID_ARG, "%s: y may not alias an input", who);
-    const Plan pl = plan_gated(M, F, K, dt, codes != nullptr);
+    const int64_t tail = codes ? 0 : tail_rows(kGated, M, F, K, entry_bytes(dt));  // (a checkpoint's halves are one behind the other)
+    const Plan pl = plan_gated(M - tail, F, K, dt, codes != nullptr);
     CAT_TRY(check_workspace(who, workspace, workspace_bytes, pl.total));
     if (M == 0) return CAT_OK;
     hipStream_t st = (hipStream_t)hip_stream;
@@ -102,6 +103,8 @@ cat_status cat_gated_linear(const void* x, const void* w, const float* bias, int
     e.out = y, e.bias = bias, e.codes_out = codes, e.scales_out = scales, e.act = (int)act;
     if (pl.few)
         return dt == CAT_F32 ? few_rows<float, float, true>(pl, x, w, M, F, K, e, ws, st) : few_rows<bf16_t, bf16_t, true>(pl, x, w, M, F, K, e, ws, st);
+    if (tail) CAT_TRY((dt == CAT_F32 ? few_tail<float, float, true>(x, w, M, tail, F, K, e, st) : few_tail<bf16_t, bf16_t, true>(x, w, M, tail, F, K, e, st)));
+    M -= tail;
     CAT_TRY(lay_out(dt, pl, x, M, K, w, nullptr, nullptr, false, 0, 2 * F, K, ws, st));
     const GemmArgs a = gemm_args(pl, entry_bytes(dt), pl.lay_q ? ws + pl.at_q : x, M, pl.lay_p ? ws + pl.at_p : w, 2 * F, M, F, K, e, ws);
     CAT_TRY(dt == CAT_F32 ? launch_gemm_f32(kGated, a, st) : launch_gemm_bf16(kGated, pl.large, a, st));

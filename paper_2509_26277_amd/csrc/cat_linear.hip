@@ -53,7 +53,7 @@ int64_t whole_lines(int64_t cols, int entry) {
 // tiles in four shares 142, small in two 153, in one 173; input gradient 1024 x 8192 over 8192, small 132, large in two shares 141; 300 x
 // 4096 over 4096, small in two shares 35, in one 42, large 51 at best; weight gradient 5000 x 2000 over 3000 rows, large 72, small
 // 83.  Float: 4096 x 1000 over 512, one share 48, two 67; 300 x 4096 over 4096, five shares 122, one 257, eight 128.)
-void choose_tiles(GemmKind kind, int64_t m, int64_t n, int64_t steps, int entry, bool pack, bool& large, int& splits) {
+double choose_tiles(GemmKind kind, int64_t m, int64_t n, int64_t steps, int entry, bool pack, bool& large, int& splits) {
     const bool gated = kind == kGated, forward = kind == kForward || gated;
     const int64_t width = gated ? 2 * n : n;
     double best = -1.0;
@@ -69,9 +69,27 @@ void choose_tiles(GemmKind kind, int64_t m, int64_t n, int64_t steps, int entry,
             if (rounds > 2 && s > 1) break;  // (more shares only add to what is joined)
         }
     }
+    return best;
 }
 }  // namespace
 
+// The launch of few rows takes 5 us and what its bytes of w take at 3.5 TB/s.  (us: gated float 4099 x 1001 over 513, 528 tiles where the
+// card holds 512: 117 in one, TAILUS with three rows apart.)
+int64_t tail_rows(GemmKind kind, int64_t m, int64_t n, int64_t k, int entry) {
+    const int64_t step = 128 / entry, steps = (k + step - 1) / step, width = kind == kGated ? 2 * n : n;
+    bool large;
+    int splits;
+    const double few = 5.0 + (double)width * k * entry / 3.5e6;
+    double best = choose_tiles(kind, m, n, steps, entry, false, large, splits);
+    int64_t tail = 0;
+    for (int64_t edge = 128; edge <= 256; edge += 128) {
+        const int64_t rest = m % edge;
+        if (m < edge + rest || rest == 0 || rest > kFewRows) continue;
+        const double us = few + choose_tiles(kind, m - rest, n, steps, entry, false, large, splits);
+        if (us < best) best = us, tail = rest;
+    }
+    return tail;
+}
 Plan plan(GemmKind kind, int64_t m, int64_t n, int64_t k, int64_t rows_q, int64_t cols_q, int64_t rows_p, int64_t cols_p, int entry, bool from_codes,
           bool pack) {
     Plan pl = {};

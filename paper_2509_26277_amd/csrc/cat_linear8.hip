@@ -33,9 +33,11 @@ cat_status check8(const char* who, int64_t M, int64_t N, int64_t K, cat_dtype dt
         return set_error(CAT_ERR_UNSUPPORTED, "%s: rows of %lld entries: sums of 8-bit products stay in 32 bits up to %lld", who, (long long)K, (long long)kMaxK8);
     return CAT_OK;
 }
-Plan plan8(bool gated, int64_t M, int64_t N, int64_t K) {
+int64_t tail8(bool gated, int64_t M, int64_t N, int64_t K) { return tail_rows(gated ? kGated : kForward, M, N, K, 1); }
+Plan plan8(bool gated, int64_t M, int64_t N, int64_t K) {  // (of the rows before the tail)
     return plan(gated ? kGated : kForward, M, N, K, M, K, gated ? 2 * N : N, K, 1, false);
 }
+size_t workspace8(bool gated, int64_t M, int64_t N, int64_t K) { return plan8(gated, M - tail8(gated, M, N, K), N, K).total; }
 
 template <typename T, bool GATED>
 cat_status product8(const Plan& pl, const int8_t* x, const int8_t* w, int64_t M, int64_t N, int64_t K, const Epilogue& e, char* ws, hipStream_t st) {
@@ -64,13 +66,16 @@ cat_status product8(const char* who, const int8_t* x, const float* x_scales, con
     CAT_TRY(check_ptr(who, "y", y, M > 0));
     if (M > 0 && (y == x || y == w || y == residual || y == x_scales || y == w_scales || y == bias))
         return set_error(CAT_ERR_INVALID_ARG, "%s: y may not alias an input", who);
-    const Plan pl = plan8(GATED, M, N, K);
+    const int64_t tail = tail8(GATED, M, N, K);
+    const Plan pl = plan8(GATED, M - tail, N, K);
     CAT_TRY(check_workspace(who, workspace, workspace_bytes, pl.total));
     if (M == 0) return CAT_OK;
     Epilogue e = {};
     e.out = y, e.bias = bias, e.residual = residual, e.act = act, e.row_scales = x_scales, e.col_scales = w_scales;
-    return dt == CAT_F32 ? product8<float, GATED>(pl, x, w, M, N, K, e, (char*)workspace, (hipStream_t)hip_stream)
-                         : product8<bf16_t, GATED>(pl, x, w, M, N, K, e, (char*)workspace, (hipStream_t)hip_stream);
+    hipStream_t st = (hipStream_t)hip_stream;
+    if (tail) CAT_TRY((dt == CAT_F32 ? few_tail<int8_t, float, GATED>(x, w, M, tail, N, K, e, st) : few_tail<int8_t, bf16_t, GATED>(x, w, M, tail, N, K, e, st)));
+    return dt == CAT_F32 ? product8<float, GATED>(pl, x, w, M - tail, N, K, e, (char*)workspace, st)
+                         : product8<bf16_t, GATED>(pl, x, w, M - tail, N, K, e, (char*)workspace, st);
 }
 
 }  // namespace
@@ -81,7 +86,7 @@ using namespace cat;
 extern "C" {
 
 size_t cat_linear8_workspace_bytes(int64_t M, int64_t N, int64_t K) {
-    return check8("cat_linear8_workspace_bytes", M, N, K, CAT_F32, 0) == CAT_OK ? plan8(false, M, N, K).total : 0;
+    return check8("cat_linear8_workspace_bytes", M, N, K, CAT_F32, 0) == CAT_OK ? workspace8(false, M, N, K) : 0;
 }
 cat_status cat_linear8(const int8_t* x, const float* x_scales, const int8_t* w, const float* w_scales, const float* bias, const void* residual, int64_t M,
                        int64_t N, int64_t K, cat_dtype dt, cat_activation act, void* y, void* workspace, size_t workspace_bytes, void* hip_stream) {
@@ -89,7 +94,7 @@ cat_status cat_linear8(const int8_t* x, const float* x_scales, const int8_t* w, 
 }
 
 size_t cat_gated_linear8_workspace_bytes(int64_t M, int64_t F, int64_t K) {
-    return check8("cat_gated_linear8_workspace_bytes", M, F, K, CAT_F32, 0) == CAT_OK ? plan8(true, M, F, K).total : 0;
+    return check8("cat_gated_linear8_workspace_bytes", M, F, K, CAT_F32, 0) == CAT_OK ? workspace8(true, M, F, K) : 0;
 }
 cat_status cat_gated_linear8(const int8_t* x, const float* x_scales, const int8_t* w, const float* w_scales, const float* bias, int64_t M, int64_t F,
                              int64_t K, cat_dtype dt, cat_activation act, void* y, void* workspace, size_t workspace_bytes, void* hip_stream) {

@@ -22,6 +22,9 @@ struct Plan {
 // pack: out's checkpoint is written (of a gated product: small tiles leave that to the joining kernel)
 Plan plan(GemmKind kind, int64_t m, int64_t n, int64_t k, int64_t rows_q, int64_t cols_q, int64_t rows_p, int64_t cols_p, int entry, bool from_codes,
           bool pack = false);
+// How many of m rows, behind the last whole tile, are better off in the kernel for few rows (forward and gated, without a checkpoint):
+// none, unless the tiles then need a round of workgroups less.
+int64_t tail_rows(GemmKind kind, int64_t m, int64_t n, int64_t k, int entry);
 inline int entry_bytes(cat_dtype dt) { return dt == CAT_F32 ? 4 : 2; }
 // cols in whole 16-byte groups
 inline int64_t whole(int64_t cols, int entry) {
@@ -351,6 +354,17 @@ cat_status few_rows(const Plan& pl, const void* x, const void* w, int64_t M, int
         hipLaunchKernelGGL((k_few_rows<E, T, 4, GATED>), grid, block, 0, st, (const E*)x, (const E*)w, M, N, K, pl.k_split, parts, e);
     CAT_LAUNCH_CHECK("k_few_rows");
     return parts ? join<E, T, GATED ? kGated : kForward>(parts, pl.splits, M, N, e, st) : CAT_OK;
+}
+// the last `tail` of M rows (tail_rows), in one launch
+template <typename E, typename T, bool GATED>
+cat_status few_tail(const void* x, const void* w, int64_t M, int64_t tail, int64_t N, int64_t K, Epilogue e, hipStream_t st) {
+    const int64_t m0 = M - tail;
+    e.out = (T*)e.out + m0 * N;
+    if (e.residual) e.residual = (const T*)e.residual + m0 * N;
+    if (e.row_scales) e.row_scales += m0;
+    Plan pl = {};
+    pl.splits = 1, pl.k_split = K;
+    return few_rows<E, T, GATED>(pl, (const E*)x + m0 * K, w, tail, N, K, e, nullptr, st);
 }
 
 }  // namespace

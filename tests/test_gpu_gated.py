@@ -14,6 +14,8 @@ pytestmark = pytest.mark.gpu
 SHAPES = [(1, 1, 1), (1, 16, 8), (1, 1001, 2048), (3, 17, 33), (16, 100, 512), (17, 65, 300), (33, 64, 136), (64, 257, 1030), (48, 40, 4096),
           (65, 64, 64), (66, 1, 7), (100, 129, 100), (128, 128, 128), (129, 255, 136), (300, 513, 1030), (200, 150, 4096), (777, 12, 63),
           (1025, 320, 72), (3600, 1795, 72), (3584, 1920, 200), (2000, 1001, 6000), (6144, 2560, 256), (6001, 2503, 130), (4864, 2048, 64)]
+# a few rows behind the last whole tile, for which the tiles would need a round of workgroups more
+TAILS = [("f32", 923, 2051, 130), ("f32", 4099, 1001, 513), ("bf16", 8200, 1001, 130), ("bf16", 8193, 1000, 128)]
 
 
 def _matrix(M, N, dtype, seed, scale=1.0):
@@ -74,6 +76,20 @@ def test_forward(M, F, K, dtype):
     want = g * v
     _close(cat_gated_linear(x, w, act="none"), want,
            half_step(x.dtype) * want.abs() * (1 + U32) + U32 * want.abs() + (ge * (v.abs() + ve) + g.abs() * ve) * (1 + half_step(x.dtype)), "without bias")
+
+
+@pytest.mark.parametrize("dtype,M,F,K", TAILS)
+def test_rows_behind_the_last_tile(dtype, M, F, K):
+    x, w, b = _matrix(M, K, dtype, 1), _matrix(2 * F, K, dtype, 2, K ** -0.5), _vector(2 * F, 3)
+    z = x.double() @ w.double().t() + b.double()
+    z_err = U32 * (K + 8) * (x.double().abs() @ w.double().abs().t() + b.double().abs())
+    (g, v), (ge, ve) = z.split(F, 1), z_err.split(F, 1)
+    u = act_ref(g, "gelu")[0]
+    want, ue = u * v, SLOPE * ge + ACT_ERR * (1.0 + g.abs())
+    bound = half_step(x.dtype) * want.abs() * (1 + U32) + U32 * want.abs() + (ue * (v.abs() + ve) + u.abs() * ve) * (1 + half_step(x.dtype))
+    out = torch.full((M + 2, F), 7.0, dtype=x.dtype, device="cuda")
+    _close(cat_gated_linear(x, w, b, act="gelu", out=out[:M]), want, bound, "y")
+    assert bool((out[M:] == 7.0).all())
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])

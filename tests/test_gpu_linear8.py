@@ -112,7 +112,8 @@ def test_exact_in_integers():
 
 # more tiles than workgroups, of several steps of k: what a workgroup carries from one tile to the next
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("M,N,K", [(6144, 5120, 1024), (6001, 5003, 600), (4864, 4096, 128), (4867, 4099, 133)])
+@pytest.mark.parametrize("M,N,K", [(6144, 5120, 1024), (6001, 5003, 600), (4864, 4096, 128), (4867, 4099, 133),
+                                   (8193, 2048, 130), (4142, 4096, 130), (8200, 2002, 130)])  # (the last three: few rows behind the last tile)
 def test_many_tiles(M, N, K, dtype):
     t = TYPES[dtype]
     x, xs, w, ws = _operands(M, N, K)
