@@ -90,16 +90,25 @@ int64_t tail_rows(GemmKind kind, int64_t m, int64_t n, int64_t k, int entry) {
     }
     return tail;
 }
+// Up to 64 rows of x: every workgroup of the kernel for few rows reads all of them from the caches, for 16 rows of w, or of gate and
+// value.  32 rows of w halve that where w is long (us, 48 rows of 8-bit integers by 2048 x 8192: 17.4 -> 15.0, 64 by 8192 x 8192: 45 -> 31; not
+// where it is short, 64 by 1024 x 1024: 5.4 and 6.9); from 64 MB of w on, the tiles do it (64 by 8192 x 8192: 28, gated bfloat16 61 -> 47; 48 by
+// 8192 x 2048 bfloat16, gated, not: 17.8 and 21.1).
+constexpr int64_t kFewWideBytes = 1 << 24, kFewMostBytes = 1 << 26;
 Plan plan(GemmKind kind, int64_t m, int64_t n, int64_t k, int64_t rows_q, int64_t cols_q, int64_t rows_p, int64_t cols_p, int entry, bool from_codes,
           bool pack) {
     Plan pl = {};
     const int64_t step = 128 / entry;
-    pl.few = (kind == kForward || kind == kGated) && m <= kFewRows;
+    const int64_t bytes_w = rows_p * cols_p * entry;
+    const bool own = kind == kForward && entry > 1;  // (the products of the block's training step: as they were)
+    pl.few = (kind == kForward || kind == kGated) && m <= kFewRows && (own || m <= 16 || bytes_w < kFewMostBytes);
     pl.ldq = cols_q, pl.ldp = cols_p;
     if (pl.few) {
-        const int64_t wgs = (n + 15) / 16;
-        int64_t s = 512 / wgs;  // few rows of w: shares of k until the card is full, each at least 8 steps a wave
-        const int64_t most = k / (kFewWaves * 8 * step);
+        pl.wide = kind == kForward && entry == 1 && m > 16 && bytes_w >= kFewWideBytes;
+        const int64_t wgs = pl.wide ? (n + 31) / 32 : (n + 15) / 16;
+        // few rows of w: shares of k until the card is full, each at least 8 steps a wave (wide: 2, and half as many)
+        int64_t s = (pl.wide ? 256 : 512) / wgs;
+        const int64_t most = k / (kFewWaves * (pl.wide ? 2 : 8) * step);
         s = s < most ? s : most;
         pl.splits = (int)(s < 1 ? 1 : s > 16 ? 16 : s);
         pl.k_split = ((k + pl.splits - 1) / pl.splits + step - 1) / step * step;

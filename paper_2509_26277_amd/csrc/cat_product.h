@@ -8,7 +8,7 @@ namespace cat {
 // ---- plans (cat_linear.hip) ----
 constexpr int64_t kFewRows = 64;
 struct Plan {
-    bool few, large;
+    bool few, wide, large;     // wide: few rows of x, 32 rows of w a workgroup
     int splits;
     bool joined;               // the tile kernel writes its sums as they are, and the joining kernel goes on with them
     int64_t k_split;
@@ -126,33 +126,35 @@ __device__ __forceinline__ Sums<E> few_multiply(f32x4 a, f32x4 b, Sums<E> c) {
         return c;
     }
 }
-template <typename E, typename T, int MB, bool GATED>
+template <typename E, typename T, int MB, bool GATED, int R>
 __global__ __launch_bounds__(kFewWaves * kWave) void k_few_rows(const E* __restrict__ x, const E* __restrict__ w, int64_t M, int64_t N, int64_t K,
                                                                 int64_t k_split, void* __restrict__ parts, const Epilogue e) {
-    constexpr int kStep = 4 * kVec<E>, U = MB == 1 ? 8 : 4, P = GATED ? 2 : 1;
-    __shared__ Sums<E> sums[kFewWaves][P * MB][kWave];
+    constexpr int kStep = 4 * kVec<E>, U = MB == 1 ? 8 : 4, P = GATED ? 2 : 1, Q = P * R;
+    __shared__ Sums<E> sums[kFewWaves][Q * MB][kWave];
     const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave, r = lane & 15, g = lane >> 4;
-    const int64_t n0 = (int64_t)blockIdx.x * 16;
-    const int64_t n = n0 + r < N ? n0 + r : N - 1;
-    const E *wr[P], *xr[MB];
+    const int64_t n0 = (int64_t)blockIdx.x * (16 * R);
+    const E *wr[Q], *xr[MB];  // [part * R + 16 rows]
 #pragma unroll
-    for (int p = 0; p < P; p++) wr[p] = w + (p * N + n) * K;
+    for (int q = 0; q < Q; q++) {
+        const int64_t n = n0 + q % R * 16 + r;
+        wr[q] = w + (q / R * N + (n < N ? n : N - 1)) * K;
+    }
 #pragma unroll
     for (int b = 0; b < MB; b++) xr[b] = x + (b * 16 + r < M ? b * 16 + r : M - 1) * K;
-    Sums<E> acc[P][MB];
+    Sums<E> acc[Q][MB];
 #pragma unroll
-    for (int i = 0; i < P * MB; i++) acc[i / MB][i % MB] = Sums<E>{0, 0, 0, 0};
+    for (int i = 0; i < Q * MB; i++) acc[i / MB][i % MB] = Sums<E>{0, 0, 0, 0};
 
     const int64_t s0 = (int64_t)blockIdx.y * k_split, s1 = s0 + k_split < K ? s0 + k_split : K;
     const int64_t mine = ((s1 - s0 + kFewWaves - 1) / kFewWaves + kStep - 1) / kStep * kStep;
     int64_t k = s0 + wave * mine;
     const int64_t end = k + mine < s1 ? k + mine : s1;
     for (; k + U * kStep <= end; k += U * kStep) {
-        f32x4 a[U][P], b[U][MB];
+        f32x4 a[U][Q], b[U][MB];
 #pragma unroll
         for (int u = 0; u < U; u++) {
 #pragma unroll
-            for (int p = 0; p < P; p++) a[u][p] = few_load(wr[p], k + u * kStep + g * kVec<E>, K);
+            for (int p = 0; p < Q; p++) a[u][p] = few_load(wr[p], k + u * kStep + g * kVec<E>, K);
 #pragma unroll
             for (int j = 0; j < MB; j++) b[u][j] = few_load(xr[j], k + u * kStep + g * kVec<E>, K);
         }
@@ -161,48 +163,52 @@ __global__ __launch_bounds__(kFewWaves * kWave) void k_few_rows(const E* __restr
 #pragma unroll
             for (int j = 0; j < MB; j++)
 #pragma unroll
-                for (int p = 0; p < P; p++) acc[p][j] = few_multiply<E>(a[u][p], b[u][j], acc[p][j]);
+                for (int p = 0; p < Q; p++) acc[p][j] = few_multiply<E>(a[u][p], b[u][j], acc[p][j]);
     }
     // (only the last share ends inside a step, at the rows' end, where few_load gives zeros)
     for (; k < end; k += kStep) {
-        f32x4 a[P];
+        f32x4 a[Q];
 #pragma unroll
-        for (int p = 0; p < P; p++) a[p] = few_load(wr[p], k + g * kVec<E>, K);
+        for (int p = 0; p < Q; p++) a[p] = few_load(wr[p], k + g * kVec<E>, K);
 #pragma unroll
         for (int j = 0; j < MB; j++) {
             const f32x4 b = few_load(xr[j], k + g * kVec<E>, K);
 #pragma unroll
-            for (int p = 0; p < P; p++) acc[p][j] = few_multiply<E>(a[p], b, acc[p][j]);
+            for (int p = 0; p < Q; p++) acc[p][j] = few_multiply<E>(a[p], b, acc[p][j]);
         }
     }
 #pragma unroll
-    for (int i = 0; i < P * MB; i++) sums[wave][i][lane] = acc[i / MB][i % MB];
+    for (int i = 0; i < Q * MB; i++) sums[wave][i][lane] = acc[i / MB][i % MB];
     __syncthreads();
-    if (wave >= MB) return;
-    const int64_t m = wave * 16 + r, nn = n0 + 4 * g;
-    float v[P][4];
+    // a wave finishes every fourth of the MB x R pieces of 16 rows of x by 16 rows of w
 #pragma unroll
-    for (int p = 0; p < P; p++) {
-        const int i = p * MB + wave;
-        const f32x4 s = __builtin_bit_cast(f32x4, (Sums<E>)((sums[0][i][lane] + sums[1][i][lane]) + (sums[2][i][lane] + sums[3][i][lane])));
+    for (int piece = wave; piece < MB * R; piece += kFewWaves) {
+        const int block = piece / R, of = piece % R;
+        const int64_t m = block * 16 + r, nn = n0 + of * 16 + 4 * g;
+        float v[P][4];
 #pragma unroll
-        for (int q = 0; q < 4; q++) v[p][q] = s[q];
-    }
-    if (m >= M || nn >= N) return;
-    if (parts) {
+        for (int p = 0; p < P; p++) {
+            const int i = (p * R + of) * MB + block;
+            const f32x4 s = __builtin_bit_cast(f32x4, (Sums<E>)((sums[0][i][lane] + sums[1][i][lane]) + (sums[2][i][lane] + sums[3][i][lane])));
 #pragma unroll
-        for (int p = 0; p < P; p++) st_group_to((float*)parts + ((int64_t)blockIdx.y * M + m) * (P * N) + p * N, nn, N, v[p]);
-    } else if constexpr (GATED) {
-        scaled<E, 4>(e, m, nn, N, v[0]);
-        scaled<E, 4>(e, m, N + nn, 2 * N, v[1]);
-        finish_gate<T, 4, false>(e, m, M, nn, N, true, v[0], v[1]);
-    } else if constexpr (sizeof(E) == 1) {
-        scaled<E, 4>(e, m, nn, N, v[0]);
-        Epilogue rest = e;
-        rest.bias = nullptr;
-        finish<T, kForward, 4, false, kFast<T>>(rest, m, nn, N, true, v[0]);
-    } else {
-        finish<T, kForward, 4, false>(e, m, nn, N, true, v[0]);
+            for (int q = 0; q < 4; q++) v[p][q] = s[q];
+        }
+        if (m >= M || nn >= N) continue;
+        if (parts) {
+#pragma unroll
+            for (int p = 0; p < P; p++) st_group_to((float*)parts + ((int64_t)blockIdx.y * M + m) * (P * N) + p * N, nn, N, v[p]);
+        } else if constexpr (GATED) {
+            scaled<E, 4>(e, m, nn, N, v[0]);
+            scaled<E, 4>(e, m, N + nn, 2 * N, v[1]);
+            finish_gate<T, 4, false>(e, m, M, nn, N, true, v[0], v[1]);
+        } else if constexpr (sizeof(E) == 1) {
+            scaled<E, 4>(e, m, nn, N, v[0]);
+            Epilogue rest = e;
+            rest.bias = nullptr;
+            finish<T, kForward, 4, false, kFast<T>>(rest, m, nn, N, true, v[0]);
+        } else {
+            finish<T, kForward, 4, false>(e, m, nn, N, true, v[0]);
+        }
     }
 }
 
@@ -344,14 +350,23 @@ inline GemmArgs gemm_args(const Plan& pl, int entry, const void* q, int64_t rows
 
 template <typename E, typename T, bool GATED>
 cat_status few_rows(const Plan& pl, const void* x, const void* w, int64_t M, int64_t N, int64_t K, const Epilogue& e, char* ws, hipStream_t st) {
-    const dim3 grid((unsigned)((N + 15) / 16), (unsigned)pl.splits), block(kFewWaves * kWave);
+    const int64_t rows = pl.wide ? 32 : 16;
+    const dim3 grid((unsigned)((N + rows - 1) / rows), (unsigned)pl.splits), block(kFewWaves * kWave);
     void* parts = pl.splits > 1 || e.codes_out ? ws + pl.at_parts : nullptr;
-    if (M <= 16)
-        hipLaunchKernelGGL((k_few_rows<E, T, 1, GATED>), grid, block, 0, st, (const E*)x, (const E*)w, M, N, K, pl.k_split, parts, e);
-    else if (M <= 32)
-        hipLaunchKernelGGL((k_few_rows<E, T, 2, GATED>), grid, block, 0, st, (const E*)x, (const E*)w, M, N, K, pl.k_split, parts, e);
-    else
-        hipLaunchKernelGGL((k_few_rows<E, T, 4, GATED>), grid, block, 0, st, (const E*)x, (const E*)w, M, N, K, pl.k_split, parts, e);
+    const auto launch = [&](auto blocks, auto pieces) {
+        hipLaunchKernelGGL((k_few_rows<E, T, decltype(blocks)::value, GATED, decltype(pieces)::value>), grid, block, 0, st, (const E*)x, (const E*)w, M, N, K,
+                           pl.k_split, parts, e);
+    };
+    const std::integral_constant<int, 1> one;
+    const std::integral_constant<int, 2> two;
+    const std::integral_constant<int, 4> four;
+    if constexpr (sizeof(E) == 1 && !GATED) {
+        if (M <= 16) launch(one, one);
+        else if (M <= 32) pl.wide ? launch(two, two) : launch(two, one);
+        else pl.wide ? launch(four, two) : launch(four, one);
+    } else {
+        M <= 16 ? launch(one, one) : M <= 32 ? launch(two, one) : launch(four, one);
+    }
     CAT_LAUNCH_CHECK("k_few_rows");
     return parts ? join<E, T, GATED ? kGated : kForward>(parts, pl.splits, M, N, e, st) : CAT_OK;
 }
