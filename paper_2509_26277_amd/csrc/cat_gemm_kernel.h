@@ -26,6 +26,7 @@ namespace cat {
 
 typedef __attribute__((address_space(3))) void* lds_void;
 typedef __attribute__((address_space(3))) char* lds_char;
+typedef __attribute__((address_space(3))) volatile uint32_t* lds_words;
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
 constexpr int kStepBytes = 128;
@@ -250,10 +251,13 @@ __device__ __forceinline__ void st8(T* row, int64_t n, int64_t N, const float (&
         *(f32x4*)(row + n + 4) = f32x4{v[4], v[5], v[6], v[7]};
     }
 }
-template <typename T, int KIND, int FAST, int MT, bool WHOLE>
+// I8: of 8-bit integers, whose products leave no checkpoint.  CUT (with WHOLE): rows are whole groups of eight columns, of which some
+// lie behind the row's end.
+template <typename T, int KIND, bool I8, int MT, bool WHOLE, bool CUT = false>
 __device__ __forceinline__ void finish_rows(const Epilogue& e, f32x4 (&acc)[MT][8], int64_t m, int64_t M, int64_t n, int64_t N, int g) {
     const int64_t G = (N + kPackGroup - 1) / kPackGroup, group = n / kPackGroup;
-    if constexpr (KIND == kForward) {
+    constexpr int FAST = I8 ? kFast<T> : sizeof(T) == 2;
+    if constexpr (KIND == kForward && !I8) {
         if (e.codes_out) {
 #pragma unroll
             for (int mt = 0; mt < MT; mt++) {
@@ -303,7 +307,7 @@ __device__ __forceinline__ void finish_rows(const Epilogue& e, f32x4 (&acc)[MT][
                         const uint2 c = *(const uint2*)(e.codes_in + row * N + n + 32 * t);
                         raw[mt][t][0] = c.x, raw[mt][t][1] = c.y;
                     } else {
-                        const uint4* q = (const uint4*)((const T*)e.residual + row * N + n + 32 * t);
+                        const uint4* q = (const uint4*)((const T*)e.residual + row * N + (!CUT || n + 32 * t < N ? n + 32 * t : 0));
 #pragma unroll
                         for (int i = 0; i < kWords / 4; i++)
                             raw[mt][t][4 * i] = q[i].x, raw[mt][t][4 * i + 1] = q[i].y, raw[mt][t][4 * i + 2] = q[i].z, raw[mt][t][4 * i + 3] = q[i].w;
@@ -332,7 +336,8 @@ __device__ __forceinline__ void finish_rows(const Epilogue& e, f32x4 (&acc)[MT][
                                                     : __uint_as_float(i % 2 ? raw[mt][t][i / 2] & 0xFFFF0000u : raw[mt][t][i / 2] << 16);
             } else if constexpr (res) {
 #pragma unroll
-                for (int t = 0; t < 4; t++) ld8<T, WHOLE>((const T*)e.residual + row * N, n + 32 * t, N, more[t]);
+                for (int t = 0; t < 4; t++)
+                    if (!CUT || n + 32 * t < N) ld8<T, WHOLE>((const T*)e.residual + row * N, n + 32 * t, N, more[t]);
             }
             if constexpr (KIND == kInputGrad && ACT != CAT_ACT_NONE) {
 #pragma unroll
@@ -355,7 +360,7 @@ __device__ __forceinline__ void finish_rows(const Epilogue& e, f32x4 (&acc)[MT][
                     if constexpr (KIND == kInputGrad) v[i] *= act_grad<ACT, FAST>(more[t][i]);
                     if constexpr (res) v[i] += more[t][i];
                 }
-                st8<T, WHOLE>((T*)e.out + row * N, n + 32 * t, N, v);
+                if (!CUT || n + 32 * t < N) st8<T, WHOLE>((T*)e.out + row * N, n + 32 * t, N, v);
             }
             __builtin_amdgcn_sched_barrier(0);
         }
@@ -370,28 +375,31 @@ __device__ __forceinline__ void finish_rows(const Epilogue& e, f32x4 (&acc)[MT][
 
 // The gated product's.  Lane (r, g) holds columns n + 32 t .. + 7, t = 0, 1, of the gate in acc[mt][0..3], of the value in
 // acc[mt][4..7].
-// PACK: the largest magnitudes of a wave's 64 columns of both go to LDS (`mine`, four words a row of the tile: gate and value of the
-// wave's columns, and of the other wave's, which share a scale with them) and come back as the scales of 128.  The barrier waits for
-// LDS alone: the next tile's loads stay under way.
-template <int MT>
-__device__ __forceinline__ void gated_scales(const f32x4 (&acc)[MT][8], int64_t n, int64_t N, lds_char row0, int half, int g, PackScale (&s)[MT][2]) {
-    typedef __attribute__((address_space(3))) volatile uint32_t* words;
+// Its checkpoints: the largest magnitudes of a wave's 64 columns of both go to LDS (four words a row of the tile: gate and value of
+// one wave's columns and of the other's, which share a scale with them; gated_top) and come back as the scales of 128 (gated_scales).
+// The barrier between waits for LDS alone: the next tile's loads stay under way.
+template <int MT, bool WHOLE>
+__device__ __forceinline__ void gated_top(const f32x4 (&acc)[MT][8], int64_t n, int64_t N, lds_char row0, int half, int g) {
 #pragma unroll
     for (int mt = 0; mt < MT; mt++)
 #pragma unroll
         for (int part = 0; part < 2; part++) {
-            uint32_t a = 0;
+            float top = 0.f;  // (maximum: a NaN stays)
 #pragma unroll
             for (int nt = 0; nt < 4; nt++)
 #pragma unroll
                 for (int i = 0; i < 4; i++)
-                    if (n + 32 * (nt >> 1) + 4 * (nt & 1) + i < N) a = mag_max(a, acc[mt][part * 4 + nt][i]);
+                    if (WHOLE || n + 32 * (nt >> 1) + 4 * (nt & 1) + i < N) top = __builtin_elementwise_maximum(top, fabsf(acc[mt][part * 4 + nt][i]));
+            uint32_t a = __float_as_uint(top) & 0x7FFFFFFFu;
             const auto by16 = __builtin_amdgcn_permlane16_swap(a, a, false, false);
             a = by16[0] > by16[1] ? by16[0] : by16[1];
             const auto by32 = __builtin_amdgcn_permlane32_swap(a, a, false, false);
             a = by32[0] > by32[1] ? by32[0] : by32[1];
-            if (g == 0) ((words)(row0 + mt * 16 * 16))[half * 2 + part] = a;
+            if (g == 0) ((lds_words)(row0 + mt * 16 * 16))[half * 2 + part] = a;
         }
+}
+template <int MT>
+__device__ __forceinline__ void gated_scales(lds_char row0, PackScale (&s)[MT][2]) {
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
@@ -399,7 +407,7 @@ __device__ __forceinline__ void gated_scales(const f32x4 (&acc)[MT][8], int64_t 
     for (int mt = 0; mt < MT; mt++)
 #pragma unroll
         for (int part = 0; part < 2; part++) {
-            const uint32_t a = ((words)(row0 + mt * 16 * 16))[part], b = ((words)(row0 + mt * 16 * 16))[2 + part];
+            const uint32_t a = ((lds_words)(row0 + mt * 16 * 16))[part], b = ((lds_words)(row0 + mt * 16 * 16))[2 + part];
             s[mt][part] = pack_scale(a > b ? a : b);
         }
 }
@@ -860,7 +868,12 @@ __global__ __launch_bounds__((TM / WM) * (TN / 128) * 64, 2) void k_gemm(const G
                 PackScale scales[MT][2];
                 const bool pack = kExchange && a.e.codes_out;
                 if constexpr (kExchange) {
-                    if (pack) gated_scales<MT>(acc, nl, a.n, lds_bias + 2 * kEnd + (wm * WM + r) * 16, wn, g, scales);
+                    if (pack) {
+                        const lds_char row0 = lds_bias + 2 * kEnd + (wm * WM + r) * 16;
+                        if (nw + WO <= a.n) gated_top<MT, true>(acc, nl, a.n, row0, wn, g);
+                        else gated_top<MT, false>(acc, nl, a.n, row0, wn, g);
+                        gated_scales<MT>(row0, scales);
+                    }
                 }
                 if (nw + WO <= a.n && a.n % 8 == 0)
                     finish_gated<T, MT, true>(a.e, acc, m, a.m, nl, a.n, g, pack ? scales : nullptr);
@@ -876,11 +889,13 @@ __global__ __launch_bounds__((TM / WM) * (TN / 128) * 64, 2) void k_gemm(const G
                     finish_gate_grad<T, MT, false>(a.e, acc, m, a.m, nl, a.n, r, col_sums);
                 }
             } else {
-                constexpr int kForm = sizeof(E) == 1 ? kFast<T> : sizeof(T) == 2;
+                constexpr bool kI8 = sizeof(E) == 1;
                 if (nw + WN <= a.n && a.n % 8 == 0)
-                    finish_rows<T, KIND, kForm, MT, true>(a.e, acc, m, a.m, nl, a.n, g);
+                    finish_rows<T, KIND, kI8, MT, true>(a.e, acc, m, a.m, nl, a.n, g);
+                else if (kI8 && nw < a.n && a.n % 8 == 0)
+                    finish_rows<T, KIND, kI8, MT, true, kI8>(a.e, acc, m, a.m, nl, a.n, g);
                 else if (nw < a.n)
-                    finish_rows<T, KIND, kForm, MT, false>(a.e, acc, m, a.m, nl, a.n, g);
+                    finish_rows<T, KIND, kI8, MT, false>(a.e, acc, m, a.m, nl, a.n, g);
             }
         }
         if (t + stride >= end) break;
