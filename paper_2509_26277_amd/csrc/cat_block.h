@@ -213,16 +213,23 @@ __device__ __forceinline__ void ld_codes(const int8_t* row, int64_t j, int64_t D
 // half steps of a float SiLU at z = -80, which therefore takes the library's and the correctly rounded quotient (us, derivative
 // of 65536 x 1000: 113 -> 121).  The other float forms keep it, being no worse for it: over [-9, 9] GELU' is off by 1.9 half
 // steps of one (1.8 with an exact exponential), tanh GELU by 157 of its value (149: the rounding of its cubic argument).
-// FAST 2, the gated operators' and those of 8-bit integers': the quotient is the hardware's reciprocal, off by a step of fp32 at
-// most, where the others' is ten instructions (us, gradients of a gate 65536 x 1024 over 256, SiLU: SLOW -> QUICK).
-template <int FAST>
+// FAST 2 (bfloat16 results) and 3 (float ones), the gated operators' and those of 8-bit integers': where the hardware's exponential is
+// taken, so is its reciprocal, off by a step of fp32 at most, where the others' quotient is ten instructions (us, gate's gradients of
+// 65536 x 1024 over 256 bfloat16, GELU by tanh and its derivative among them: 176 -> 170; its u, 16384 x 4096, laid out: 77 -> 59).
+template <int HOW>  // 0: the library's exponential, correctly rounded; 1: the hardware's; 2: and its reciprocal
 __device__ __forceinline__ float logistic(float z) {
-    if constexpr (FAST == 2) return __builtin_amdgcn_rcpf(1.f + __expf(-z));
-    else if constexpr (FAST) return __fdividef(1.f, 1.f + __expf(-z));
+    if constexpr (HOW == 2) return __builtin_amdgcn_rcpf(1.f + __expf(-z));
+    else if constexpr (HOW == 1) return __fdividef(1.f, 1.f + __expf(-z));
     else return __fdiv_rn(1.f, 1.f + expf(-z));
 }
 template <typename T>
-constexpr int kFast = sizeof(T) == 2 ? 2 : 0;
+constexpr int kFast = sizeof(T) == 2 ? 2 : 3;
+template <int FAST>
+constexpr bool kHalf = FAST == 1 || FAST == 2;  // bfloat16 results
+template <int FAST>
+constexpr int kSilu = kHalf<FAST> ? FAST : 0;
+template <int FAST>
+constexpr int kTanh = FAST >= 2 ? 2 : 1;
 constexpr float kInvSqrt2 = 0.70710678118654752f, kInvSqrt2Pi = 0.39894228040143268f;
 constexpr float kTanhIn = 0.79788456080286536f, kTanhCube = 0.044715f;
 // gelu with tanh: 0.5 z (1 + tanh u) = z * logistic(2 u), u = sqrt(2 / pi) (z + 0.044715 z^3)
@@ -243,7 +250,7 @@ __device__ __forceinline__ float tail_factor(float x) {
 __device__ __forceinline__ float normal_exp(float z) { return __builtin_amdgcn_exp2f(z * z * -0.72134752044448170f); }
 // The tail by itself, Phi(-x) = 2^P(x): P a polynomial of degree 7, fitted so that x 2^P(x) is off by 2.4e-7 at most, and 2^P(x) by 4.4e-5
 // of its value up to x = 7 (behind that Phi is below 2e-12, and P falls on).  14 instructions' time for GELU where exponential, reciprocal
-// and tail_factor take 24 (us, 16384 x 8192 over 2048 8-bit integers: 285 -> GELUUS).
+// and tail_factor take 24 (us, 16384 x 8192 over 2048 8-bit integers: 285 -> 264).
 __device__ __forceinline__ float tail(float x) {
     float p = fmaf(x, -1.592344006e-6f, 5.686387885e-5f);
     p = fmaf(x, p, -8.961785352e-4f);
@@ -260,15 +267,15 @@ __device__ __forceinline__ float act_value(float z) {
     } else if constexpr (ACT == CAT_ACT_GELU && FAST == 2) {  // (as below; minimum and maximum hand a NaN on)
         const float x = fabsf(__builtin_elementwise_minimum(z, 1e30f));
         return fmaf(-x, tail(x), __builtin_elementwise_maximum(z, 0.f));
-    } else if constexpr (ACT == CAT_ACT_GELU && FAST) {  // z - z Phi(-z), or z Phi(z)
+    } else if constexpr (ACT == CAT_ACT_GELU && kHalf<FAST>) {  // z - z Phi(-z), or z Phi(z)
         const float x = fabsf(fminf(z, 1e30f));           // (no inf * 0 for +inf)
         return fmaf(-x, normal_exp(z) * tail_factor(x), fmaxf(z, 0.f));
     } else if constexpr (ACT == CAT_ACT_GELU) {
         return 0.5f * z * (1.f + erff(z * kInvSqrt2));
     } else if constexpr (ACT == CAT_ACT_GELU_TANH) {
-        return z * logistic<(FAST > 1 ? FAST : 1)>(tanh_arg2(z));
+        return z * logistic<kTanh<FAST>>(tanh_arg2(z));
     } else if constexpr (ACT == CAT_ACT_SILU) {
-        return z * logistic<FAST>(z);
+        return z * logistic<kSilu<FAST>>(z);
     } else {
         return z;
     }
@@ -277,17 +284,17 @@ template <int ACT, int FAST>
 __device__ __forceinline__ float act_grad(float z) {
     if constexpr (ACT == CAT_ACT_RELU) {
         return z > 0.f ? 1.f : (z != z ? z : 0.f);
-    } else if constexpr (ACT == CAT_ACT_GELU && FAST) {  // Phi + z phi: s below zero, 1 - s above
+    } else if constexpr (ACT == CAT_ACT_GELU && kHalf<FAST>) {  // Phi + z phi: s below zero, 1 - s above
         const float x = fminf(fabsf(z), 1e30f), s = normal_exp(z) * fmaf(-kInvSqrt2Pi, x, tail_factor(x));
         return z > 0.f ? 1.f - s : s;
     } else if constexpr (ACT == CAT_ACT_GELU) {
         return fmaf(z * kInvSqrt2Pi, __expf(-0.5f * z * z), 0.5f * (1.f + erff(z * kInvSqrt2)));
     } else if constexpr (ACT == CAT_ACT_GELU_TANH) {
         // (beyond |z| = 32 the factor p (1 - p) is zero in fp32, and z * z must not turn it into 0 * inf)
-        const float p = logistic<(FAST > 1 ? FAST : 1)>(tanh_arg2(z)), c = fminf(fmaxf(z, -32.f), 32.f);
+        const float p = logistic<kTanh<FAST>>(tanh_arg2(z)), c = fminf(fmaxf(z, -32.f), 32.f);
         return fmaf(c * p * (1.f - p), 2.f * kTanhIn * fmaf(3.f * kTanhCube * c, c, 1.f), p);
     } else if constexpr (ACT == CAT_ACT_SILU) {
-        const float p = logistic<FAST>(z);
+        const float p = logistic<kSilu<FAST>>(z);
         return p * fmaf(z, 1.f - p, 1.f);
     } else {
         return 1.f;
@@ -297,15 +304,15 @@ __device__ __forceinline__ float act_grad(float z) {
 template <int ACT, int FAST>
 __device__ __forceinline__ void act_both(float z, float& value, float& grad) {
     if constexpr (ACT == CAT_ACT_SILU) {
-        const float p = logistic<FAST>(z);
+        const float p = logistic<kSilu<FAST>>(z);
         value = z * p;
         grad = p * fmaf(z, 1.f - p, 1.f);
-    } else if constexpr (ACT == CAT_ACT_GELU && FAST) {
+    } else if constexpr (ACT == CAT_ACT_GELU && kHalf<FAST>) {
         const float x = fminf(fabsf(z), 1e30f), e = normal_exp(z), g = tail_factor(x), s = e * fmaf(-kInvSqrt2Pi, x, g);
         value = fmaf(-x, e * g, fmaxf(z, 0.f));
         grad = z > 0.f ? 1.f - s : s;
     } else if constexpr (ACT == CAT_ACT_GELU_TANH) {
-        const float p = logistic<(FAST > 1 ? FAST : 1)>(tanh_arg2(z)), c = fminf(fmaxf(z, -32.f), 32.f);
+        const float p = logistic<kTanh<FAST>>(tanh_arg2(z)), c = fminf(fmaxf(z, -32.f), 32.f);
         value = z * p;
         grad = fmaf(c * p * (1.f - p), 2.f * kTanhIn * fmaf(3.f * kTanhCube * c, c, 1.f), p);
     } else {

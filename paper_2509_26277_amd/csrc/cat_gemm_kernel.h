@@ -480,28 +480,12 @@ __device__ __forceinline__ float sums_by_lane(float (&v)[16], int r) {
     return v[0];
 }
 // The gate's gradients: lane (r, g) as in finish_rows.  sums: this wave's row of col_sums.  Two pairs of tiles at a time for all rows,
-// so that the sums over rows are 32 registers; a row's codes are under way while the one before it is worked on.
-template <typename T, int MT, bool WHOLE>
+// so that the sums over rows are 32 registers.
+template <typename T, int MT>
 __device__ __forceinline__ void finish_gate_grad(const Epilogue& e, f32x4 (&acc)[MT][8], int64_t m, int64_t M, int64_t n, int64_t N, int r, float* sums) {
     const int64_t G = (N + kPackGroup - 1) / kPackGroup, group = n / kPackGroup;
-    float steps[MT][2];
-#pragma unroll
-    for (int mt = 0; mt < MT; mt++) {
-        const int64_t row = m + 16 * mt < M ? m + 16 * mt : M - 1;
-        steps[mt][0] = e.scales_in[row * G + group], steps[mt][1] = e.scales_in[(M + row) * G + group];
-    }
     with_act(e.act, [&](auto which) {
         constexpr int ACT = decltype(which)::value;
-        uint2 held[2][2][2];
-        const auto request = [&](int at, uint2(&to)[2][2]) {  // at: half * MT + row
-            if constexpr (WHOLE) {
-                const int64_t row = m + 16 * (at % MT) < M ? m + 16 * (at % MT) : M - 1;
-                const int8_t *gate = e.codes_in + row * N + n + 64 * (at / MT), *value = gate + M * N;
-#pragma unroll
-                for (int t = 0; t < 2; t++) to[t][0] = *(const uint2*)(gate + 32 * t), to[t][1] = *(const uint2*)(value + 32 * t);
-            }
-        };
-        request(0, held[0]);
 #pragma unroll
         for (int half = 0; half < 2; half++) {
             float s[2][16];
@@ -509,38 +493,26 @@ __device__ __forceinline__ void finish_gate_grad(const Epilogue& e, f32x4 (&acc)
             for (int i = 0; i < 32; i++) s[i / 16][i % 16] = 0.f;
 #pragma unroll
             for (int mt = 0; mt < MT; mt++) {
-                const int step = half * MT + mt;
-                if (step + 1 < 2 * MT) request(step + 1, held[(step + 1) & 1]);
-                const bool mine = m + 16 * mt < M;
-                const int64_t row = mine ? m + 16 * mt : M - 1;
+                const int64_t row = m + 16 * mt;
                 T* out = (T*)e.out + row * 2 * N;
 #pragma unroll
                 for (int t = 0; t < 2; t++) {
                     const int64_t at = n + 64 * half + 32 * t;
-                    if (mine && (WHOLE || at < N)) {
+                    if (row < M && at < N) {
                         float gate[8], value[8];
-                        if constexpr (WHOLE) {
-                            const uint2 a = held[step & 1][t][0], b = held[step & 1][t][1];
-#pragma unroll
-                            for (int i = 0; i < 8; i++) {
-                                gate[i] = code_value(i < 4 ? a.x : a.y, i % 4) * steps[mt][0];
-                                value[i] = code_value(i < 4 ? b.x : b.y, i % 4) * steps[mt][1];
-                            }
-                        } else {
-                            ld_codes<8>(e.codes_in + row * N, at, N, steps[mt][0], gate);
-                            ld_codes<8>(e.codes_in + (M + row) * N, at, N, steps[mt][1], value);
-                        }
+                        ld_codes<8>(e.codes_in + row * N, at, N, e.scales_in[row * G + group], gate);
+                        ld_codes<8>(e.codes_in + (M + row) * N, at, N, e.scales_in[(M + row) * G + group], value);
 #pragma unroll
                         for (int i = 0; i < 8; i++) {
-                            const float d = acc[mt][4 * half + 2 * t + (i >> 2)][i & 3], z = gate[i];
-                            float a, da;
-                            act_both<ACT, kFast<T>>(z, a, da);
-                            gate[i] = d * value[i] * da;
-                            value[i] = d * a;
+                            const float d = acc[mt][4 * half + 2 * t + (i >> 2)][i & 3];
+                            float u, du;
+                            act_both<ACT, kFast<T>>(gate[i], u, du);
+                            gate[i] = d * value[i] * du;
+                            value[i] = d * u;
                             s[t][i] += gate[i], s[t][8 + i] += value[i];
                         }
-                        st8<T, WHOLE>(out, at, N, gate);
-                        st8<T, WHOLE>(out + N, at, N, value);
+                        st_entries<T, 8>(out, at, N, gate);
+                        st_entries<T, 8>(out + N, at, N, value);
                     }
                     __builtin_amdgcn_sched_barrier(0);
                 }
@@ -550,7 +522,7 @@ __device__ __forceinline__ void finish_gate_grad(const Epilogue& e, f32x4 (&acc)
                 for (int t = 0; t < 2; t++) {
                     const float total = sums_by_lane(s[t], r);
                     const int64_t c = n + 64 * half + 32 * t + (r & 7);
-                    if (WHOLE || c < N) sums[(r >> 3) * N + c] = total;
+                    if (c < N) sums[(r >> 3) * N + c] = total;
                 }
             }
             __builtin_amdgcn_sched_barrier(0);
@@ -558,11 +530,11 @@ __device__ __forceinline__ void finish_gate_grad(const Epilogue& e, f32x4 (&acc)
     });
 }
 
-// The same for bfloat16 rows of whole groups of eight columns.  Nothing is stored before the last codes have come: loads and stores
-// complete in the order of their issue, and a load behind stores would be waited for as long as those (us, 65536 x 1024 over 256
-// without sums: 163; without loads 102, without stores 93).  What is stored waits in the sums' registers, both gradients of an entry
-// in one.
-template <int ACT, int MT>
+// The same for rows of whole groups of eight columns, a row's codes under way while the one before it is worked on.  Nothing is stored
+// before the last codes have come: loads and stores complete in the order of their issue, and a load behind stores would be waited for
+// as long as those (us, 65536 x 1024 over 256 bfloat16 without sums: 163, now 136; without loads 102, without stores 93).  What is
+// stored waits in the sums' registers, both gradients of an entry in one where they are bfloat16.
+template <typename T, int ACT, int MT>
 __device__ __forceinline__ void finish_gate_grad8(const Epilogue& e, f32x4 (&acc)[MT][8], int64_t m, int64_t M, int64_t n, int64_t N, int r, float* sums) {
     const int64_t G = (N + kPackGroup - 1) / kPackGroup, group = n / kPackGroup;
     float steps[MT][2];
@@ -571,6 +543,7 @@ __device__ __forceinline__ void finish_gate_grad8(const Epilogue& e, f32x4 (&acc
         const int64_t row = m + 16 * mt < M ? m + 16 * mt : M - 1;
         steps[mt][0] = e.scales_in[row * G + group], steps[mt][1] = e.scales_in[(M + row) * G + group];
     }
+    f32x4 second[sizeof(T) == 4 ? MT : 1][8];  // float: the value's gradients
     uint2 held[2][2][2];
     const auto request = [&](int at, uint2(&to)[2][2]) {  // at: half * MT + row; columns behind the last: those of the row's first group
         const int64_t row = m + 16 * (at % MT) < M ? m + 16 * (at % MT) : M - 1;
@@ -601,12 +574,18 @@ __device__ __forceinline__ void finish_gate_grad8(const Epilogue& e, f32x4 (&acc
                         const float d = acc[mt][nt][i & 3];
                         const float gate = code_value(i < 4 ? a.x : a.y, i % 4) * steps[mt][0], value = code_value(i < 4 ? b.x : b.y, i % 4) * steps[mt][1];
                         float u, du;
-                        act_both<ACT, 2>(gate, u, du);
-                        const float dg = d * value * du, dv = d * u;
+                        act_both<ACT, kFast<T>>(gate, u, du);
+                        float dg = d * value * du, dv = d * u;
                         s[t][i] += dg, s[t][8 + i] += dv;
-                        uint32_t both = pack_bf16(dg, dv);
-                        asm volatile("" : "+v"(both));  // (here and now: left to the compiler, it is done where it is stored, from all it takes)
-                        acc[mt][nt][i & 3] = __uint_as_float(both);
+                        // (here and now: left to the compiler, it is done where it is stored, from all it takes)
+                        if constexpr (sizeof(T) == 2) {
+                            uint32_t both = pack_bf16(dg, dv);
+                            asm volatile("" : "+v"(both));
+                            acc[mt][nt][i & 3] = __uint_as_float(both);
+                        } else {
+                            asm volatile("" : "+v"(dg), "+v"(dv));
+                            acc[mt][nt][i & 3] = dg, second[mt][nt][i & 3] = dv;
+                        }
                     }
                 }
                 __builtin_amdgcn_sched_barrier(0);
@@ -626,18 +605,25 @@ __device__ __forceinline__ void finish_gate_grad8(const Epilogue& e, f32x4 (&acc
     for (int mt = 0; mt < MT; mt++) {
         const int64_t row = m + 16 * mt;
         if (row >= M) continue;
-        bf16_t* out = (bf16_t*)e.out + row * 2 * N + n;
+        T* out = (T*)e.out + row * 2 * N + n;
 #pragma unroll
         for (int t = 0; t < 4; t++) {
-            uint32_t gate[4], value[4];
+            if (n + 32 * t >= N) continue;
+            if constexpr (sizeof(T) == 2) {
+                uint32_t gate[4], value[4];
 #pragma unroll
-            for (int i = 0; i < 4; i++) {
-                const uint32_t lo = __float_as_uint(acc[mt][2 * t + (i >> 1)][2 * (i & 1)]), hi = __float_as_uint(acc[mt][2 * t + (i >> 1)][2 * (i & 1) + 1]);
-                gate[i] = __builtin_amdgcn_perm(hi, lo, 0x05040100u), value[i] = __builtin_amdgcn_perm(hi, lo, 0x07060302u);
-            }
-            if (n + 32 * t < N) {
+                for (int i = 0; i < 4; i++) {
+                    const uint32_t lo = __float_as_uint(acc[mt][2 * t + (i >> 1)][2 * (i & 1)]), hi = __float_as_uint(acc[mt][2 * t + (i >> 1)][2 * (i & 1) + 1]);
+                    gate[i] = __builtin_amdgcn_perm(hi, lo, 0x05040100u), value[i] = __builtin_amdgcn_perm(hi, lo, 0x07060302u);
+                }
                 *(uint4*)(out + 32 * t) = make_uint4(gate[0], gate[1], gate[2], gate[3]);
                 *(uint4*)(out + N + 32 * t) = make_uint4(value[0], value[1], value[2], value[3]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 2; i++) {
+                    *(f32x4*)(out + 32 * t + 4 * i) = acc[mt][2 * t + i];
+                    *(f32x4*)(out + N + 32 * t + 4 * i) = second[mt][2 * t + i];
+                }
             }
         }
         __builtin_amdgcn_sched_barrier(0);
@@ -666,8 +652,7 @@ __global__ __launch_bounds__((TM / WM) * (TN / 128) * 64, 2) void k_gemm(const G
 
     // Workgroups go to the eight XCDs in turn; each XCD takes a run of neighbouring tiles, eight columns of them at a time, so
     // that what its L2 holds of either operand serves many of them.  With shares of k the run goes through the tiles of a share and
-    // then of the next one: an XCD reads its share of k and not all of it (us, weight gradient 1024 x 4096 over 16384 rows in four
-    // shares: 170 -> SHARES).
+    // then of the next one: an XCD reads its share of k and not all of it.
     const uint32_t tm = (uint32_t)((a.m + TM - 1) / TM), tn = (uint32_t)((a.n + TO - 1) / TO), tiles = tm * tn;
     const uint32_t xcd = blockIdx.x & 7, all = tiles * (uint32_t)a.splits, share = all / 8, more = all % 8;
     uint32_t stride = (gridDim.x - xcd + 7) / 8, end = (xcd + 1) * share + (xcd + 1 < more ? xcd + 1 : more);
@@ -882,11 +867,9 @@ __global__ __launch_bounds__((TM / WM) * (TN / 128) * 64, 2) void k_gemm(const G
             } else if constexpr (KIND == kGatedGrad) {
                 float* col_sums = a.e.col_sums ? a.e.col_sums + ((int64_t)tile_m * (TM / WM) + wm) * 2 * a.n : nullptr;
                 if constexpr (ACT >= 0) {
-                    if (nw < a.n) finish_gate_grad8<ACT, MT>(a.e, acc, m, a.m, nl, a.n, r, col_sums);
-                } else if (sizeof(T) == 4 && nw + WO <= a.n && a.n % 8 == 0) {
-                    if constexpr (sizeof(T) == 4) finish_gate_grad<T, MT, true>(a.e, acc, m, a.m, nl, a.n, r, col_sums);
-                } else if (nw < a.n) {
-                    finish_gate_grad<T, MT, false>(a.e, acc, m, a.m, nl, a.n, r, col_sums);
+                    if (nw < a.n) finish_gate_grad8<T, ACT, MT>(a.e, acc, m, a.m, nl, a.n, r, col_sums);
+                } else {
+                    if (nw < a.n) finish_gate_grad<T, MT>(a.e, acc, m, a.m, nl, a.n, r, col_sums);
                 }
             } else {
                 constexpr bool kI8 = sizeof(E) == 1;
@@ -915,6 +898,20 @@ cat_status launch_gemm_tiles(const GemmArgs& a, hipStream_t st) {
     hipLaunchKernelGGL((k_gemm<E, T, KIND, TM, TN, WM, ACT>), dim3((unsigned)(a.splits > 1 ? tiles * a.splits : tiles < most ? tiles : most)), dim3((TM / WM) * (TN / 128) * 64), 0, st, a);
     CAT_LAUNCH_CHECK("k_gemm");
     return CAT_OK;
+}
+
+// the gate's gradients: a kernel for each activation where rows are whole groups of eight columns, one for all where they are not (or
+// where the joining kernel works them out)
+template <typename T, int EDGE, int WM>
+cat_status launch_gate_grad(const GemmArgs& a, hipStream_t st) {
+    if (a.n % 8 != 0 || a.parts) return launch_gemm_tiles<T, T, kGatedGrad, EDGE, EDGE, WM>(a, st);
+    switch (a.e.act) {
+        case CAT_ACT_NONE: return launch_gemm_tiles<T, T, kGatedGrad, EDGE, EDGE, WM, CAT_ACT_NONE>(a, st);
+        case CAT_ACT_RELU: return launch_gemm_tiles<T, T, kGatedGrad, EDGE, EDGE, WM, CAT_ACT_RELU>(a, st);
+        case CAT_ACT_GELU: return launch_gemm_tiles<T, T, kGatedGrad, EDGE, EDGE, WM, CAT_ACT_GELU>(a, st);
+        case CAT_ACT_GELU_TANH: return launch_gemm_tiles<T, T, kGatedGrad, EDGE, EDGE, WM, CAT_ACT_GELU_TANH>(a, st);
+        default: return launch_gemm_tiles<T, T, kGatedGrad, EDGE, EDGE, WM, CAT_ACT_SILU>(a, st);
+    }
 }
 
 }  // namespace cat

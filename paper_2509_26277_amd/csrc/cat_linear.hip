@@ -74,7 +74,7 @@ double choose_tiles(GemmKind kind, int64_t m, int64_t n, int64_t steps, int entr
 }  // namespace
 
 // The launch of few rows takes 5 us and what its bytes of w take at 3.5 TB/s.  (us: gated float 4099 x 1001 over 513, 528 tiles where the
-// card holds 512: 117 in one, TAILUS with three rows apart.)
+// card holds 512: 117 in one, 93 with three rows apart.)
 int64_t tail_rows(GemmKind kind, int64_t m, int64_t n, int64_t k, int entry) {
     const int64_t step = 128 / entry, steps = (k + step - 1) / step, width = kind == kGated ? 2 * n : n;
     bool large;
@@ -132,7 +132,7 @@ Plan plan(GemmKind kind, int64_t m, int64_t n, int64_t k, int64_t rows_q, int64_
     if (pl.lay_p) at += up256((size_t)rows_p * pl.ldp * entry);
     pl.at_parts = at;
     // (few rows: the checkpoint's groups of 128 columns are found by the joining kernel, whatever the number of shares)
-    if (pl.joined || pl.few) at += up256((size_t)pl.splits * m * (kind == kGated ? 2 * n : n) * 4);
+    if (pl.joined || (pl.few && (own || pack || pl.splits > 1))) at += up256((size_t)pl.splits * m * (kind == kGated ? 2 * n : n) * 4);
     pl.at_sums = at;
     if (kind == kWeightGrad) {  // sums over the rows of dy (k rows, m columns)
         const int64_t v = 16 / entry, gx = (m + 64 * v - 1) / (64 * v);

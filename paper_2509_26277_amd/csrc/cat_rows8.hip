@@ -173,7 +173,7 @@ __global__ __launch_bounds__(kNormThreads) void k_rows8_long(const T* __restrict
 
 // How many threads share a row: four 16-byte groups each (three, where those are enough), so that a wave has up to 4 KB of rows under
 // way and few lanes to reduce over; 8 threads of the shortest rows, and more than a wave's from 257 groups on, as in layer norm.
-// (us, 65536 x 512 bf16 through the norm: 36 with a wave a row and a group a lane, NORMUS so; 65536 x 512 fp32 47 and ROWUS.)
+// (us, 65536 x 512 bf16 through the norm: 36 with a wave a row and a group a lane, 26 so; 65536 x 512 fp32 47 and 26.)
 template <typename T>
 NormShape rows8_shape(int64_t D) {
     const int64_t n = (D + kVec<T> - 1) / kVec<T>;
