@@ -668,9 +668,13 @@ cat_status cat_activation_backward(const void *dy, const int8_t *codes, const fl
  *               x * (127 / a), ties to even, a the row's largest magnitude, and stands for code * s, s = a / 127.  Roundings, rows
  *               with a < 2^-100 (zeros), NaN and infinities (a row of NaN) as a group of cat_pack8 has them.  A weight goes
  *               through it once, its rows being output channels.
+ *               ld >= D: entries from a row of codes to the next; what lies between is left as it was.
  * cat_layer_norm_quantize  the same of cat_layer_norm's y, before its rounding to dt.
  * cat_linear8   z = (sum over k of x w) * x_scales * w_scales + bias, y = act(z) + residual (M x N of dt, nullable).  x: M x K, w:
  *               N x K, any 8-bit integers (-128 too); the sums are exact, K at most 131071; x_scales: M floats, w_scales: N.
+ *               ldx, ldw: entries from a row of x, of w, to the next: K, or a larger multiple of 16, in which case the last row may be
+ *               read up to the next multiple of 16 too.  What lies behind K does not count.  Where K is no multiple of 16, w is laid
+ *               out anew in the workspace, and x unless ldx is one: rows that cat_quantize_rows left 16 bytes' multiples apart are not.
  * cat_gated_linear   g and v the products of x (M x K) with the gate's and the value's rows of w, plus bias; y = act(g) * v (M x F).
  *               codes, scales: both or neither, the checkpoints of g and of v (of their fp32 values), one behind the other: 2 x
  *               M x F int8 and 2 x M x ceil(F / 128) floats, each half as cat_pack8 gives it.
@@ -682,20 +686,21 @@ cat_status cat_activation_backward(const void *dy, const int8_t *codes, const fl
  *               rows act(g) * v is rounded to bfloat16, as cat_linear_backward_weight has it.
  * One size of workspace covers both gradients, and cat_gated_linear with and without checkpoints; F is below 2^23 bytes of dt.
  * CAT_ERR_UNSUPPORTED also for K of more than 131071 8-bit integers. */
-cat_status cat_quantize_rows(const void *x, int64_t N, int64_t D, cat_dtype dt, int8_t *codes, float *scales, void *hip_stream);
+cat_status cat_quantize_rows(const void *x, int64_t N, int64_t D, cat_dtype dt, int8_t *codes, int64_t ld, float *scales,
+                             void *hip_stream);
 cat_status cat_layer_norm_quantize(const void *x, int64_t N, int64_t D, cat_dtype dt, const float *weight, const float *bias,
-                                   float eps, int8_t *codes, float *scales, void *hip_stream);
+                                   float eps, int8_t *codes, int64_t ld, float *scales, void *hip_stream);
 size_t cat_linear8_workspace_bytes(int64_t M, int64_t N, int64_t K);
-cat_status cat_linear8(const int8_t *x, const float *x_scales, const int8_t *w, const float *w_scales, const float *bias,
-                       const void *residual, int64_t M, int64_t N, int64_t K, cat_dtype dt, cat_activation act, void *y,
-                       void *workspace, size_t workspace_bytes, void *hip_stream);
+cat_status cat_linear8(const int8_t *x, int64_t ldx, const float *x_scales, const int8_t *w, int64_t ldw,
+                       const float *w_scales, const float *bias, const void *residual, int64_t M, int64_t N, int64_t K,
+                       cat_dtype dt, cat_activation act, void *y, void *workspace, size_t workspace_bytes, void *hip_stream);
 size_t cat_gated_linear_workspace_bytes(int64_t M, int64_t F, int64_t K, cat_dtype dt);
 cat_status cat_gated_linear(const void *x, const void *w, const float *bias, int64_t M, int64_t F, int64_t K, cat_dtype dt,
                             cat_activation act, void *y, int8_t *codes, float *scales, void *workspace,
                             size_t workspace_bytes, void *hip_stream);
 size_t cat_gated_linear8_workspace_bytes(int64_t M, int64_t F, int64_t K);
-cat_status cat_gated_linear8(const int8_t *x, const float *x_scales, const int8_t *w, const float *w_scales,
-                             const float *bias, int64_t M, int64_t F, int64_t K, cat_dtype dt, cat_activation act, void *y,
+cat_status cat_gated_linear8(const int8_t *x, int64_t ldx, const float *x_scales, const int8_t *w, int64_t ldw,
+                             const float *w_scales, const float *bias, int64_t M, int64_t F, int64_t K, cat_dtype dt, cat_activation act, void *y,
                              void *workspace, size_t workspace_bytes, void *hip_stream);
 size_t cat_gated_backward_workspace_bytes(int64_t M, int64_t N, int64_t F, cat_dtype dt);
 cat_status cat_gated_backward_input(const void *dy, const void *w, const int8_t *codes, const float *scales, int64_t M,

@@ -185,13 +185,13 @@ def load_library():
     lib.cat_linear_backward_weight.restype = c.c_int
     lib.cat_activation_backward.argtypes = [vp, vp, vp, i64, i64, dt, c.c_int, vp, vp]
     lib.cat_activation_backward.restype = c.c_int
-    lib.cat_quantize_rows.argtypes = [vp, i64, i64, dt, vp, vp, vp]
+    lib.cat_quantize_rows.argtypes = [vp, i64, i64, dt, vp, i64, vp, vp]
     lib.cat_quantize_rows.restype = c.c_int
-    lib.cat_layer_norm_quantize.argtypes = [vp, i64, i64, dt, vp, vp, f32, vp, vp, vp]
+    lib.cat_layer_norm_quantize.argtypes = [vp, i64, i64, dt, vp, vp, f32, vp, i64, vp, vp]
     lib.cat_layer_norm_quantize.restype = c.c_int
     lib.cat_linear8_workspace_bytes.argtypes = [i64, i64, i64]
     lib.cat_linear8_workspace_bytes.restype = sz
-    lib.cat_linear8.argtypes = [vp, vp, vp, vp, vp, vp, i64, i64, i64, dt, c.c_int, vp, vp, sz, vp]
+    lib.cat_linear8.argtypes = [vp, i64, vp, vp, i64, vp, vp, vp, i64, i64, i64, dt, c.c_int, vp, vp, sz, vp]
     lib.cat_linear8.restype = c.c_int
     lib.cat_gated_linear_workspace_bytes.argtypes = [i64, i64, i64, dt]
     lib.cat_gated_linear_workspace_bytes.restype = sz
@@ -199,7 +199,7 @@ def load_library():
     lib.cat_gated_linear.restype = c.c_int
     lib.cat_gated_linear8_workspace_bytes.argtypes = [i64, i64, i64]
     lib.cat_gated_linear8_workspace_bytes.restype = sz
-    lib.cat_gated_linear8.argtypes = [vp, vp, vp, vp, vp, i64, i64, i64, dt, c.c_int, vp, vp, sz, vp]
+    lib.cat_gated_linear8.argtypes = [vp, i64, vp, vp, i64, vp, vp, i64, i64, i64, dt, c.c_int, vp, vp, sz, vp]
     lib.cat_gated_linear8.restype = c.c_int
     lib.cat_gated_backward_workspace_bytes.argtypes = [i64, i64, i64, dt]
     lib.cat_gated_backward_workspace_bytes.restype = sz
@@ -937,41 +937,62 @@ def _room(here, workspace, nbytes, device):
     return workspace
 
 
+def _empty_codes(N, D, device):
+    """Codes whose rows start on 16-byte boundaries, as the products take them without laying them out anew (a view, unless D is a
+    multiple of 16), the entries from one row to the next, and their scales."""
+    ld = (D + 15) // 16 * 16
+    codes = torch.empty((N, ld), dtype=torch.int8, device=device)
+    return codes if ld == D else codes[:, :D], ld, torch.empty((N,), dtype=torch.float32, device=device)
+
+
+def _codes(here, t, rows, K, name):
+    """_at of a matrix of codes, and the entries from one row to the next: contiguous, or rows on 16-byte boundaries whose last one has
+    memory up to the next."""
+    if t.is_contiguous():
+        return _at(here, t, torch.int8, (rows, K), name), K
+    ld = t.stride(0)
+    if (t.get_device() != here or t.dtype != torch.int8 or t.shape != (rows, K) or t.stride(1) != 1 or ld < K or ld % 16
+            or t.untyped_storage().nbytes() < t.storage_offset() + (rows - 1) * ld + (K + 15) // 16 * 16):
+        raise ValueError(f"{name} must be a matrix of {rows} x {K} int8 on cuda:{here}, contiguous or with rows on 16-byte boundaries")
+    return t.data_ptr(), ld
+
+
 def cat_quantize_rows(x):
     """Rows to 8-bit integers with a scale a row (cat_quantize_rows): (codes, scales), codes of x's shape, row m standing for
-    ``codes[m] * scales[m]``.  A weight (its rows output channels) goes through it once."""
+    ``codes[m] * scales[m]``; rows of codes start on 16-byte boundaries.  A weight (its rows output channels) goes through it once."""
     N, D, dt = _rows(x, "x")
     here = _here(x, "x")
     px = _at(here, x, x.dtype, (N, D), "x")
-    codes, scales = torch.empty((N, D), dtype=torch.int8, device=x.device), torch.empty((N,), dtype=torch.float32, device=x.device)
-    _check(load_library().cat_quantize_rows(px, N, D, dt, codes.data_ptr(), scales.data_ptr(), _stream()))
+    codes, ld, scales = _empty_codes(N, D, x.device)
+    _check(load_library().cat_quantize_rows(px, N, D, dt, codes.data_ptr(), ld, scales.data_ptr(), _stream()))
     return codes, scales
 
 
 def cat_layer_norm_quantize(x, weight=None, bias=None, eps=1e-5):
-    """Layer norm of every row straight to 8-bit integers with a scale a row (cat_layer_norm_quantize): (codes, scales)."""
+    """Layer norm of every row straight to 8-bit integers with a scale a row (cat_layer_norm_quantize): (codes, scales), as
+    cat_quantize_rows gives them."""
     N, D, dt = _rows(x, "x")
     here = _here(x, "x")
     px, pw, pb = _at(here, x, x.dtype, (N, D), "x"), _at(here, weight, torch.float32, (D,), "weight"), _at(here, bias, torch.float32, (D,), "bias")
-    codes, scales = torch.empty((N, D), dtype=torch.int8, device=x.device), torch.empty((N,), dtype=torch.float32, device=x.device)
-    _check(load_library().cat_layer_norm_quantize(px, N, D, dt, pw, pb, float(eps), codes.data_ptr(), scales.data_ptr(), _stream()))
+    codes, ld, scales = _empty_codes(N, D, x.device)
+    _check(load_library().cat_layer_norm_quantize(px, N, D, dt, pw, pb, float(eps), codes.data_ptr(), ld, scales.data_ptr(), _stream()))
     return codes, scales
 
 
 def cat_linear8(x, x_scales, w, w_scales, bias=None, act="none", residual=None, dtype=torch.bfloat16, out=None, workspace=None):
-    """act((x w^T) * x_scales * w_scales + bias) + residual of 8-bit integers x (M x K) and w (N x K) (cat_linear8), scales and
-    bias float32, residual and result (M x N) of ``dtype``, float32 or bfloat16."""
+    """act((x w^T) * x_scales * w_scales + bias) + residual of 8-bit integers x (M x K) and w (N x K) (cat_linear8), contiguous or
+    with rows on 16-byte boundaries, scales and bias float32, residual and result (M x N) of ``dtype``, float32 or bfloat16."""
     lib = load_library()
     (M, K), N, dt = _two(x, "x"), _two(w, "w")[0], _out_type(dtype)
     here = _here(x, "x")
-    px, pw = _at(here, x, torch.int8, (M, K), "x"), _at(here, w, torch.int8, (N, K), "w")
+    (px, ldx), (pw, ldw) = _codes(here, x, M, K, "x"), _codes(here, w, N, K, "w")
     ps, pt = _at(here, x_scales, torch.float32, (M,), "x_scales"), _at(here, w_scales, torch.float32, (N,), "w_scales")
     pb, pr = _at(here, bias, torch.float32, (N,), "bias"), _at(here, residual, dtype, (M, N), "residual")
     act = _act(act)
     if out is None:
         out = torch.empty((M, N), dtype=dtype, device=x.device)
     workspace = _room(here, workspace, lib.cat_linear8_workspace_bytes(M, N, K), x.device)
-    _check(lib.cat_linear8(px, ps, pw, pt, pb, pr, M, N, K, dt, act, _at(here, out, dtype, (M, N), "out"), workspace.data_ptr(), workspace.numel(),
+    _check(lib.cat_linear8(px, ldx, ps, pw, ldw, pt, pb, pr, M, N, K, dt, act, _at(here, out, dtype, (M, N), "out"), workspace.data_ptr(), workspace.numel(),
                            _stream()))
     return out
 
@@ -1010,14 +1031,14 @@ def cat_gated_linear8(x, x_scales, w, w_scales, bias=None, act="silu", dtype=tor
     lib = load_library()
     (M, K), F, dt = _two(x, "x"), _halves(w, "w")[0], _out_type(dtype)
     here = _here(x, "x")
-    px, pw = _at(here, x, torch.int8, (M, K), "x"), _at(here, w, torch.int8, (2 * F, K), "w")
+    (px, ldx), (pw, ldw) = _codes(here, x, M, K, "x"), _codes(here, w, 2 * F, K, "w")
     ps, pt = _at(here, x_scales, torch.float32, (M,), "x_scales"), _at(here, w_scales, torch.float32, (2 * F,), "w_scales")
     pb = _at(here, bias, torch.float32, (2 * F,), "bias")
     act = _act(act)
     if out is None:
         out = torch.empty((M, F), dtype=dtype, device=x.device)
     workspace = _room(here, workspace, lib.cat_gated_linear8_workspace_bytes(M, F, K), x.device)
-    _check(lib.cat_gated_linear8(px, ps, pw, pt, pb, M, F, K, dt, act, _at(here, out, dtype, (M, F), "out"), workspace.data_ptr(), workspace.numel(),
+    _check(lib.cat_gated_linear8(px, ldx, ps, pw, ldw, pt, pb, M, F, K, dt, act, _at(here, out, dtype, (M, F), "out"), workspace.data_ptr(), workspace.numel(),
                                  _stream()))
     return out
 

@@ -102,8 +102,8 @@ cat_status cat_gated_linear(const void* x, const void* w, const float* bias, int
     Epilogue e = {};
     e.out = y, e.bias = bias, e.codes_out = codes, e.scales_out = scales, e.act = (int)act;
     if (pl.few)
-        return dt == CAT_F32 ? few_rows<float, float, true>(pl, x, w, M, F, K, e, ws, st) : few_rows<bf16_t, bf16_t, true>(pl, x, w, M, F, K, e, ws, st);
-    if (tail) CAT_TRY((dt == CAT_F32 ? few_tail<float, float, true>(x, w, M, tail, F, K, e, st) : few_tail<bf16_t, bf16_t, true>(x, w, M, tail, F, K, e, st)));
+        return dt == CAT_F32 ? few_rows<float, float, true>(pl, x, K, w, K, M, F, K, e, ws, st) : few_rows<bf16_t, bf16_t, true>(pl, x, K, w, K, M, F, K, e, ws, st);
+    if (tail) CAT_TRY((dt == CAT_F32 ? few_tail<float, float, true>(x, K, w, K, M, tail, F, K, e, st) : few_tail<bf16_t, bf16_t, true>(x, K, w, K, M, tail, F, K, e, st)));
     M -= tail;
     CAT_TRY(lay_out(dt, pl, x, M, K, w, nullptr, nullptr, false, 0, 2 * F, K, ws, st));
     const GemmArgs a = gemm_args(pl, entry_bytes(dt), pl.lay_q ? ws + pl.at_q : x, M, pl.lay_p ? ws + pl.at_p : w, 2 * F, M, F, K, e, ws);

@@ -252,7 +252,7 @@ cat_status cat_linear(const void* x, const void* w, const float* bias, const voi
     hipStream_t st = (hipStream_t)hip_stream;
     char* ws = (char*)workspace;
     const Epilogue e = {y, bias, residual, codes, scales, nullptr, nullptr, (int)act};
-    if (pl.few) return dt == CAT_F32 ? few_rows<float, float, false>(pl, x, w, M, N, K, e, ws, st) : few_rows<bf16_t, bf16_t, false>(pl, x, w, M, N, K, e, ws, st);
+    if (pl.few) return dt == CAT_F32 ? few_rows<float, float, false>(pl, x, K, w, K, M, N, K, e, ws, st) : few_rows<bf16_t, bf16_t, false>(pl, x, K, w, K, M, N, K, e, ws, st);
     CAT_TRY(lay_out(dt, pl, x, M, K, w, nullptr, nullptr, false, 0, N, K, ws, st));
     return multiply_tiles(kForward, pl, dt, pl.lay_q ? ws + pl.at_q : x, M, pl.lay_p ? ws + pl.at_p : w, N, M, N, K, e, ws, st);
 }

@@ -21,10 +21,15 @@ __global__ __launch_bounds__(256) void k_lay_out8(const Layout<int8_t> first, co
     const int64_t per = a.ld / 16, n = a.rows * per;
     for (int64_t t = block * 256 + threadIdx.x; t < n; t += (int64_t)a.blocks * 256) {
         const int64_t row = n < (1ll << 32) ? (uint32_t)t / (uint32_t)per : t / per, j = (t - row * per) * 16;
-        *(f32x4*)(a.dst + row * a.ld + j) = few_load(a.src + row * a.cols, j, a.cols);
+        *(f32x4*)(a.dst + row * a.ld + j) = few_load(a.src + row * a.from, j, a.cols);
     }
 }
 
+// ld: from a row of codes to the next
+cat_status check_ld(const char* who, const char* name, int64_t ld, int64_t K) {
+    if (ld == K || (ld > K && ld % 16 == 0 && ld <= kGemmMaxRowBytes)) return CAT_OK;
+    return set_error(CAT_ERR_INVALID_ARG, "%s: rows of %s of %lld entries lie %lld apart: as many, or a larger multiple of 16", who, name, (long long)K, (long long)ld);
+}
 cat_status check8(const char* who, int64_t M, int64_t N, int64_t K, cat_dtype dt, int act) {
     CAT_TRY(check_linear(who, M, N, 1, dt));
     CAT_TRY(check_rows(who, M, K, dt));
@@ -34,29 +39,38 @@ cat_status check8(const char* who, int64_t M, int64_t N, int64_t K, cat_dtype dt
     return CAT_OK;
 }
 int64_t tail8(bool gated, int64_t M, int64_t N, int64_t K) { return tail_rows(gated ? kGated : kForward, M, N, K, 1); }
-Plan plan8(bool gated, int64_t M, int64_t N, int64_t K) {  // (of the rows before the tail)
-    return plan(gated ? kGated : kForward, M, N, K, M, K, gated ? 2 * N : N, K, 1, false);
+// Of the rows before the tail.  Rows of x that start on 16-byte boundaries are used where they are, whatever their last 16 bytes hold
+// behind K: w's hold zeros there, being laid out anew unless K is a multiple of 16.
+Plan plan8(bool gated, int64_t M, int64_t N, int64_t K, int64_t ldx, int64_t ldw) {
+    return plan(gated ? kGated : kForward, M, N, K, M, ldx, gated ? 2 * N : N, K % 16 ? K : ldw, 1, false);
 }
-size_t workspace8(bool gated, int64_t M, int64_t N, int64_t K) { return plan8(gated, M - tail8(gated, M, N, K), N, K).total; }
+size_t workspace8(bool gated, int64_t M, int64_t N, int64_t K) { return plan8(gated, M - tail8(gated, M, N, K), N, K, K, K).total; }
 
 template <typename T, bool GATED>
-cat_status product8(const Plan& pl, const int8_t* x, const int8_t* w, int64_t M, int64_t N, int64_t K, const Epilogue& e, char* ws, hipStream_t st) {
+cat_status product8(const Plan& pl, const int8_t* x, int64_t ldx, const int8_t* w, int64_t ldw, int64_t M, int64_t N, int64_t K, const Epilogue& e, char* ws,
+                    hipStream_t st) {
     constexpr GemmKind kind = GATED ? kGated : kForward;
-    if (pl.few) return few_rows<int8_t, T, GATED>(pl, x, w, M, N, K, e, ws, st);
+    if (pl.few) return few_rows<int8_t, T, GATED>(pl, x, ldx, w, ldw, M, N, K, e, ws, st);
     const int64_t rows_w = GATED ? 2 * N : N;
-    if (pl.lay_q) {  // (rows of one length: both operands or neither)
-        const Layout<int8_t> lq = layout_of<int8_t>(x, nullptr, nullptr, M, K, pl.ldq, ws + pl.at_q), lp = layout_of<int8_t>(w, nullptr, nullptr, rows_w, K, pl.ldp, ws + pl.at_p);
-        hipLaunchKernelGGL(k_lay_out8, dim3(lq.blocks + lp.blocks), dim3(256), 0, st, lq, lp);
+    Layout<int8_t> lq = layout_of<int8_t>(x, nullptr, nullptr, M, K, pl.ldq, ws + pl.at_q), lp = layout_of<int8_t>(w, nullptr, nullptr, rows_w, K, pl.ldp, ws + pl.at_p);
+    lq.from = ldx, lp.from = ldw;
+    if (pl.lay_p) {  // (and x with it, or not)
+        const Layout<int8_t> none = {};
+        hipLaunchKernelGGL(k_lay_out8, dim3(lp.blocks + (pl.lay_q ? lq.blocks : 0)), dim3(256), 0, st, lp, pl.lay_q ? lq : none);
         CAT_LAUNCH_CHECK("k_lay_out8");
     }
-    const GemmArgs a = gemm_args(pl, 1, pl.lay_q ? ws + pl.at_q : (const char*)x, M, pl.lay_p ? ws + pl.at_p : (const char*)w, rows_w, M, N, K, e, ws);
+    GemmArgs a = gemm_args(pl, 1, pl.lay_q ? ws + pl.at_q : (const char*)x, M, pl.lay_p ? ws + pl.at_p : (const char*)w, rows_w, M, N, K, e, ws);
+    if (!pl.lay_q) a.q_bytes = (M - 1) * pl.ldq + whole(K, 1);
+    if (!pl.lay_p) a.p_bytes = (rows_w - 1) * pl.ldp + K;
     CAT_TRY(launch_gemm_i8(kind, pl.large, sizeof(T) == 4 ? CAT_F32 : CAT_BF16, a, st));
     return pl.joined ? join<int8_t, T, kind>(a.parts, pl.splits, M, N, e, st) : CAT_OK;
 }
 template <bool GATED>
-cat_status product8(const char* who, const int8_t* x, const float* x_scales, const int8_t* w, const float* w_scales, const float* bias, const void* residual,
-                    int64_t M, int64_t N, int64_t K, cat_dtype dt, int act, void* y, void* workspace, size_t workspace_bytes, void* hip_stream) {
+cat_status product8(const char* who, const int8_t* x, int64_t ldx, const float* x_scales, const int8_t* w, int64_t ldw, const float* w_scales,
+                    const float* bias, const void* residual, int64_t M, int64_t N, int64_t K, cat_dtype dt, int act, void* y, void* workspace, size_t workspace_bytes, void* hip_stream) {
     CAT_TRY(check8(who, M, N, K, dt, act));
+    CAT_TRY(check_ld(who, "x", ldx, K));
+    CAT_TRY(check_ld(who, "w", ldw, K));
     CAT_TRY(check_ptr(who, "x", x, M > 0));
     CAT_TRY(check_ptr(who, "x_scales", x_scales, M > 0));
     CAT_TRY(check_ptr(who, "w", w, true));
@@ -67,15 +81,15 @@ cat_status product8(const char* who, const int8_t* x, const float* x_scales, con
     if (M > 0 && (y == x || y == w || y == residual || y == x_scales || y == w_scales || y == bias))
         return set_error(CAT_ERR_INVALID_ARG, "%s: y may not alias an input", who);
     const int64_t tail = tail8(GATED, M, N, K);
-    const Plan pl = plan8(GATED, M - tail, N, K);
+    const Plan pl = plan8(GATED, M - tail, N, K, ldx, ldw);
     CAT_TRY(check_workspace(who, workspace, workspace_bytes, pl.total));
     if (M == 0) return CAT_OK;
     Epilogue e = {};
     e.out = y, e.bias = bias, e.residual = residual, e.act = act, e.row_scales = x_scales, e.col_scales = w_scales;
     hipStream_t st = (hipStream_t)hip_stream;
-    if (tail) CAT_TRY((dt == CAT_F32 ? few_tail<int8_t, float, GATED>(x, w, M, tail, N, K, e, st) : few_tail<int8_t, bf16_t, GATED>(x, w, M, tail, N, K, e, st)));
-    return dt == CAT_F32 ? product8<float, GATED>(pl, x, w, M - tail, N, K, e, (char*)workspace, st)
-                         : product8<bf16_t, GATED>(pl, x, w, M - tail, N, K, e, (char*)workspace, st);
+    if (tail) CAT_TRY((dt == CAT_F32 ? few_tail<int8_t, float, GATED>(x, ldx, w, ldw, M, tail, N, K, e, st) : few_tail<int8_t, bf16_t, GATED>(x, ldx, w, ldw, M, tail, N, K, e, st)));
+    return dt == CAT_F32 ? product8<float, GATED>(pl, x, ldx, w, ldw, M - tail, N, K, e, (char*)workspace, st)
+                         : product8<bf16_t, GATED>(pl, x, ldx, w, ldw, M - tail, N, K, e, (char*)workspace, st);
 }
 
 }  // namespace
@@ -88,17 +102,17 @@ extern "C" {
 size_t cat_linear8_workspace_bytes(int64_t M, int64_t N, int64_t K) {
     return check8("cat_linear8_workspace_bytes", M, N, K, CAT_F32, 0) == CAT_OK ? workspace8(false, M, N, K) : 0;
 }
-cat_status cat_linear8(const int8_t* x, const float* x_scales, const int8_t* w, const float* w_scales, const float* bias, const void* residual, int64_t M,
+cat_status cat_linear8(const int8_t* x, int64_t ldx, const float* x_scales, const int8_t* w, int64_t ldw, const float* w_scales, const float* bias, const void* residual, int64_t M,
                        int64_t N, int64_t K, cat_dtype dt, cat_activation act, void* y, void* workspace, size_t workspace_bytes, void* hip_stream) {
-    return product8<false>("cat_linear8", x, x_scales, w, w_scales, bias, residual, M, N, K, dt, (int)act, y, workspace, workspace_bytes, hip_stream);
+    return product8<false>("cat_linear8", x, ldx, x_scales, w, ldw, w_scales, bias, residual, M, N, K, dt, (int)act, y, workspace, workspace_bytes, hip_stream);
 }
 
 size_t cat_gated_linear8_workspace_bytes(int64_t M, int64_t F, int64_t K) {
     return check8("cat_gated_linear8_workspace_bytes", M, F, K, CAT_F32, 0) == CAT_OK ? workspace8(true, M, F, K) : 0;
 }
-cat_status cat_gated_linear8(const int8_t* x, const float* x_scales, const int8_t* w, const float* w_scales, const float* bias, int64_t M, int64_t F,
+cat_status cat_gated_linear8(const int8_t* x, int64_t ldx, const float* x_scales, const int8_t* w, int64_t ldw, const float* w_scales, const float* bias, int64_t M, int64_t F,
                              int64_t K, cat_dtype dt, cat_activation act, void* y, void* workspace, size_t workspace_bytes, void* hip_stream) {
-    return product8<true>("cat_gated_linear8", x, x_scales, w, w_scales, bias, nullptr, M, F, K, dt, (int)act, y, workspace, workspace_bytes, hip_stream);
+    return product8<true>("cat_gated_linear8", x, ldx, x_scales, w, ldw, w_scales, bias, nullptr, M, F, K, dt, (int)act, y, workspace, workspace_bytes, hip_stream);
 }
 
 }  // extern "C"

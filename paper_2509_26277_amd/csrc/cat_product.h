@@ -127,8 +127,8 @@ __device__ __forceinline__ Sums<E> few_multiply(f32x4 a, f32x4 b, Sums<E> c) {
     }
 }
 template <typename E, typename T, int MB, bool GATED, int R>
-__global__ __launch_bounds__(kFewWaves * kWave) void k_few_rows(const E* __restrict__ x, const E* __restrict__ w, int64_t M, int64_t N, int64_t K,
-                                                                int64_t k_split, void* __restrict__ parts, const Epilogue e) {
+__global__ __launch_bounds__(kFewWaves * kWave) void k_few_rows(const E* __restrict__ x, const E* __restrict__ w, int64_t ldx, int64_t ldw, int64_t M, int64_t N,
+                                                                int64_t K, int64_t k_split, void* __restrict__ parts, const Epilogue e) {
     constexpr int kStep = 4 * kVec<E>, U = MB == 1 ? 8 : 4, P = GATED ? 2 : 1, Q = P * R;
     __shared__ Sums<E> sums[kFewWaves][Q * MB][kWave];
     const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave, r = lane & 15, g = lane >> 4;
@@ -137,10 +137,10 @@ __global__ __launch_bounds__(kFewWaves * kWave) void k_few_rows(const E* __restr
 #pragma unroll
     for (int q = 0; q < Q; q++) {
         const int64_t n = n0 + q % R * 16 + r;
-        wr[q] = w + (q / R * N + (n < N ? n : N - 1)) * K;
+        wr[q] = w + (q / R * N + (n < N ? n : N - 1)) * ldw;
     }
 #pragma unroll
-    for (int b = 0; b < MB; b++) xr[b] = x + (b * 16 + r < M ? b * 16 + r : M - 1) * K;
+    for (int b = 0; b < MB; b++) xr[b] = x + (b * 16 + r < M ? b * 16 + r : M - 1) * ldx;
     Sums<E> acc[Q][MB];
 #pragma unroll
     for (int i = 0; i < Q * MB; i++) acc[i / MB][i % MB] = Sums<E>{0, 0, 0, 0};
@@ -265,7 +265,7 @@ struct Layout {
     const T* src;
     const int8_t* codes;  // instead of src: a checkpoint, through act; gated: times the one behind it
     const float* scales;
-    int64_t rows, cols, ld;
+    int64_t rows, cols, from, ld;  // from, ld: from a row of src, of dst, to the next
     T* dst;
     unsigned blocks;
 };
@@ -293,14 +293,14 @@ __global__ __launch_bounds__(256) void k_lay_out(const Layout<T> first, const La
                 for (int e = 0; e < V; e++) v[e] *= value[e];
             }
         } else {
-            ld_group_to(a.src + row * a.cols, j, a.cols, v);
+            ld_group_to(a.src + row * a.from, j, a.cols, v);
         }
         st_group(a.dst + row * a.ld + j, v);
     }
 }
 template <typename T>
 Layout<T> layout_of(const void* src, const int8_t* codes, const float* scales, int64_t rows, int64_t cols, int64_t ld, void* dst) {
-    return {(const T*)src, codes, scales, rows, cols, ld, (T*)dst, blocks_of(rows * (ld / kVec<T>))};
+    return {(const T*)src, codes, scales, rows, cols, cols, ld, (T*)dst, blocks_of(rows * (ld / kVec<T>))};
 }
 // q and p as the plan has them, those that lie otherwise; p from a checkpoint if codes are given
 template <typename T>
@@ -349,13 +349,14 @@ inline GemmArgs gemm_args(const Plan& pl, int entry, const void* q, int64_t rows
 }
 
 template <typename E, typename T, bool GATED>
-cat_status few_rows(const Plan& pl, const void* x, const void* w, int64_t M, int64_t N, int64_t K, const Epilogue& e, char* ws, hipStream_t st) {
+cat_status few_rows(const Plan& pl, const void* x, int64_t ldx, const void* w, int64_t ldw, int64_t M, int64_t N, int64_t K, const Epilogue& e, char* ws,
+                    hipStream_t st) {
     const int64_t rows = pl.wide ? 32 : 16;
     const dim3 grid((unsigned)((N + rows - 1) / rows), (unsigned)pl.splits), block(kFewWaves * kWave);
     void* parts = pl.splits > 1 || e.codes_out ? ws + pl.at_parts : nullptr;
     const auto launch = [&](auto blocks, auto pieces) {
-        hipLaunchKernelGGL((k_few_rows<E, T, decltype(blocks)::value, GATED, decltype(pieces)::value>), grid, block, 0, st, (const E*)x, (const E*)w, M, N, K,
-                           pl.k_split, parts, e);
+        hipLaunchKernelGGL((k_few_rows<E, T, decltype(blocks)::value, GATED, decltype(pieces)::value>), grid, block, 0, st, (const E*)x, (const E*)w, ldx, ldw, M,
+                           N, K, pl.k_split, parts, e);
     };
     const std::integral_constant<int, 1> one;
     const std::integral_constant<int, 2> two;
@@ -372,14 +373,14 @@ cat_status few_rows(const Plan& pl, const void* x, const void* w, int64_t M, int
 }
 // the last `tail` of M rows (tail_rows), in one launch
 template <typename E, typename T, bool GATED>
-cat_status few_tail(const void* x, const void* w, int64_t M, int64_t tail, int64_t N, int64_t K, Epilogue e, hipStream_t st) {
+cat_status few_tail(const void* x, int64_t ldx, const void* w, int64_t ldw, int64_t M, int64_t tail, int64_t N, int64_t K, Epilogue e, hipStream_t st) {
     const int64_t m0 = M - tail;
     e.out = (T*)e.out + m0 * N;
     if (e.residual) e.residual = (const T*)e.residual + m0 * N;
     if (e.row_scales) e.row_scales += m0;
     Plan pl = {};
     pl.splits = 1, pl.k_split = K;
-    return few_rows<E, T, GATED>(pl, (const E*)x + m0 * K, w, tail, N, K, e, nullptr, st);
+    return few_rows<E, T, GATED>(pl, (const E*)x + m0 * ldx, ldx, w, ldw, tail, N, K, e, nullptr, st);
 }
 
 }  // namespace

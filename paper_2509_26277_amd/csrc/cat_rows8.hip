@@ -29,7 +29,7 @@ __device__ __forceinline__ uint32_t row_max(uint32_t a, float (*slots)[2][8], in
 template <typename T, int TPR, int VPL, bool NORM>
 __global__ __launch_bounds__(kThreads<TPR>) void k_rows8(const T* __restrict__ x, int64_t N, int64_t D, const float* __restrict__ weight,
                                                          const float* __restrict__ bias, float eps, int8_t* __restrict__ codes,
-                                                         float* __restrict__ scales) {
+                                                         int64_t ld, float* __restrict__ scales) {
     constexpr int V = kVec<T>, RPB = kThreads<TPR> / TPR;
     __shared__ float slots[2][2][8];
     int slot = 0;
@@ -107,7 +107,7 @@ __global__ __launch_bounds__(kThreads<TPR>) void k_rows8(const T* __restrict__ x
 #pragma unroll
         for (int k = 0; k < VPL; k++) {
             const int64_t j = ((int64_t)k * TPR + sub) * V;
-            if (j < D) st_codes<V>(codes + row * D, j, D, h[k], s.up);
+            if (j < D) st_codes<V>(codes + row * ld, j, D, h[k], s.up);
         }
     }
 }
@@ -115,7 +115,7 @@ __global__ __launch_bounds__(kThreads<TPR>) void k_rows8(const T* __restrict__ x
 template <typename T, bool NORM>
 __global__ __launch_bounds__(kNormThreads) void k_rows8_long(const T* __restrict__ x, int64_t N, int64_t D, const float* __restrict__ weight,
                                                              const float* __restrict__ bias, float eps, int8_t* __restrict__ codes,
-                                                             float* __restrict__ scales) {
+                                                             int64_t ld, float* __restrict__ scales) {
     constexpr int V = kVec<T>;
     __shared__ float slots[2][2][8];
     int slot = 0;
@@ -166,7 +166,7 @@ __global__ __launch_bounds__(kNormThreads) void k_rows8_long(const T* __restrict
         for (int64_t j = (int64_t)threadIdx.x * V; j < D; j += kNormThreads * V) {
             float v[V];
             values(j, v);
-            st_codes<V>(codes + row * D, j, D, v, s.up);
+            st_codes<V>(codes + row * ld, j, D, v, s.up);
         }
     }
 }
@@ -183,13 +183,13 @@ NormShape rows8_shape(int64_t D) {
 }
 constexpr int kRows8Groups = 1024;  // workgroups; further rows by stride
 template <typename T, bool NORM>
-cat_status launch_rows8(const T* x, int64_t N, int64_t D, const float* weight, const float* bias, float eps, int8_t* codes, float* scales, hipStream_t st) {
+cat_status launch_rows8(const T* x, int64_t N, int64_t D, const float* weight, const float* bias, float eps, int8_t* codes, int64_t ld, float* scales, hipStream_t st) {
     const NormShape s = rows8_shape<T>(D);
     const int64_t rpb = s.tpr && s.tpr < kNormThreads ? kNormThreads / s.tpr : 1, blocks = (N + rpb - 1) / rpb;
     const dim3 grid((unsigned)(blocks < kRows8Groups ? blocks : kRows8Groups));
 #define CAT_X(TPR, VPL)               \
     if (s.tpr == TPR && s.vpl == VPL) \
-        hipLaunchKernelGGL((k_rows8<T, TPR, VPL, NORM>), grid, dim3(kThreads<TPR>), 0, st, x, N, D, weight, bias, eps, codes, scales);
+        hipLaunchKernelGGL((k_rows8<T, TPR, VPL, NORM>), grid, dim3(kThreads<TPR>), 0, st, x, N, D, weight, bias, eps, codes, ld, scales);
     CAT_X(8, 1) CAT_X(8, 2) CAT_X(8, 3) CAT_X(8, 4) CAT_X(16, 3) CAT_X(16, 4) CAT_X(32, 3) CAT_X(32, 4) CAT_X(64, 3) CAT_X(64, 4) CAT_X(256, 4)
     if constexpr (sizeof(T) == 4) {
         CAT_X(64, 8) CAT_X(256, 8)
@@ -197,13 +197,14 @@ cat_status launch_rows8(const T* x, int64_t N, int64_t D, const float* weight, c
         CAT_X(256, 2)
     }
 #undef CAT_X
-    if (!s.tpr) hipLaunchKernelGGL((k_rows8_long<T, NORM>), grid, dim3(kNormThreads), 0, st, x, N, D, weight, bias, eps, codes, scales);
+    if (!s.tpr) hipLaunchKernelGGL((k_rows8_long<T, NORM>), grid, dim3(kNormThreads), 0, st, x, N, D, weight, bias, eps, codes, ld, scales);
     CAT_LAUNCH_CHECK("k_rows8");
     return CAT_OK;
 }
 
-cat_status check_rows8(const char* who, const void* x, int64_t N, int64_t D, cat_dtype dt, const int8_t* codes, const float* scales) {
+cat_status check_rows8(const char* who, const void* x, int64_t N, int64_t D, cat_dtype dt, const int8_t* codes, int64_t ld, const float* scales) {
     CAT_TRY(check_rows(who, N, D, dt));
+    if (ld < D || ld >= (1ll << 31)) return set_error(CAT_ERR_INVALID_ARG, "%s: rows of %lld codes lie %lld apart", who, (long long)D, (long long)ld);
     CAT_TRY(check_ptr(who, "x", x, N > 0));
     CAT_TRY(check_ptr(who, "codes", codes, N > 0));
     CAT_TRY(check_ptr(who, "scales", scales, N > 0));
@@ -218,25 +219,25 @@ using namespace cat;
 
 extern "C" {
 
-cat_status cat_quantize_rows(const void* x, int64_t N, int64_t D, cat_dtype dt, int8_t* codes, float* scales, void* hip_stream) {
-    CAT_TRY(check_rows8("cat_quantize_rows", x, N, D, dt, codes, scales));
+cat_status cat_quantize_rows(const void* x, int64_t N, int64_t D, cat_dtype dt, int8_t* codes, int64_t ld, float* scales, void* hip_stream) {
+    CAT_TRY(check_rows8("cat_quantize_rows", x, N, D, dt, codes, ld, scales));
     if (N == 0) return CAT_OK;
     hipStream_t st = (hipStream_t)hip_stream;
-    return dt == CAT_F32 ? launch_rows8<float, false>((const float*)x, N, D, nullptr, nullptr, 0.f, codes, scales, st)
-                         : launch_rows8<bf16_t, false>((const bf16_t*)x, N, D, nullptr, nullptr, 0.f, codes, scales, st);
+    return dt == CAT_F32 ? launch_rows8<float, false>((const float*)x, N, D, nullptr, nullptr, 0.f, codes, ld, scales, st)
+                         : launch_rows8<bf16_t, false>((const bf16_t*)x, N, D, nullptr, nullptr, 0.f, codes, ld, scales, st);
 }
 
 cat_status cat_layer_norm_quantize(const void* x, int64_t N, int64_t D, cat_dtype dt, const float* weight, const float* bias, float eps, int8_t* codes,
-                                   float* scales, void* hip_stream) {
+                                   int64_t ld, float* scales, void* hip_stream) {
     const char* who = "cat_layer_norm_quantize";
-    CAT_TRY(check_rows8(who, x, N, D, dt, codes, scales));
+    CAT_TRY(check_rows8(who, x, N, D, dt, codes, ld, scales));
     CAT_TRY(check_ptr(who, "weight", weight, false));
     CAT_TRY(check_ptr(who, "bias", bias, false));
     if (!(eps >= 0.f) || isinf(eps)) return set_error(CAT_ERR_INVALID_ARG, "%s: eps = %g is not finite and >= 0", who, (double)eps);
     if (N == 0) return CAT_OK;
     hipStream_t st = (hipStream_t)hip_stream;
-    return dt == CAT_F32 ? launch_rows8<float, true>((const float*)x, N, D, weight, bias, eps, codes, scales, st)
-                         : launch_rows8<bf16_t, true>((const bf16_t*)x, N, D, weight, bias, eps, codes, scales, st);
+    return dt == CAT_F32 ? launch_rows8<float, true>((const float*)x, N, D, weight, bias, eps, codes, ld, scales, st)
+                         : launch_rows8<bf16_t, true>((const bf16_t*)x, N, D, weight, bias, eps, codes, ld, scales, st);
 }
 
 }  // extern "C"

@@ -30,19 +30,19 @@ WS = dict(ws=FAKE, ws_bytes=1 << 40, stream=None)
 
 
 def _quantize(lib, **kw):
-    return _call(lib.cat_quantize_rows, dict(x=A, N=4, D=8, dt=0, codes=B, scales=C, stream=None), **kw)
+    return _call(lib.cat_quantize_rows, dict(x=A, N=4, D=8, dt=0, codes=B, ld=8, scales=C, stream=None), **kw)
 
 
 def _norm_quantize(lib, **kw):
-    return _call(lib.cat_layer_norm_quantize, dict(x=A, N=4, D=8, dt=0, weight=None, bias=None, eps=1e-5, codes=B, scales=C, stream=None), **kw)
+    return _call(lib.cat_layer_norm_quantize, dict(x=A, N=4, D=8, dt=0, weight=None, bias=None, eps=1e-5, codes=B, ld=8, scales=C, stream=None), **kw)
 
 
 def _linear8(lib, **kw):
-    return _call(lib.cat_linear8, dict(x=A, xs=B, w=C, w_scales=D, bias=None, res=None, M=4, N=8, K=16, dt=1, act=0, y=E, **WS), **kw)
+    return _call(lib.cat_linear8, dict(x=A, ldx=16, xs=B, w=C, ldw=16, w_scales=D, bias=None, res=None, M=4, N=8, K=16, dt=1, act=0, y=E, **WS), **kw)
 
 
 def _gated8(lib, **kw):
-    return _call(lib.cat_gated_linear8, dict(x=A, xs=B, w=C, w_scales=D, bias=None, M=4, N=8, K=16, dt=1, act=0, y=E, **WS), **kw)
+    return _call(lib.cat_gated_linear8, dict(x=A, ldx=16, xs=B, w=C, ldw=16, w_scales=D, bias=None, M=4, N=8, K=16, dt=1, act=0, y=E, **WS), **kw)
 
 
 def _gated(lib, **kw):
@@ -97,7 +97,7 @@ def test_shapes_of_products(lib, call):
 
 def test_long_sums(lib):
     for call in (_linear8, _gated8):
-        assert call(lib, K=131072) == UNSUPPORTED and b"131071" in lib.cat_last_error()
+        assert call(lib, K=131072, ldx=131072, ldw=131072) == UNSUPPORTED and b"131071" in lib.cat_last_error()
     for call in (_gated, _input, _weight):
         assert call(lib, K=(1 << 22) + 8) == UNSUPPORTED
 
@@ -106,6 +106,19 @@ def test_long_sums(lib):
 def test_activations(lib, call):
     for act in (-1, 5, 99):
         assert call(lib, act=act) == INVALID and b"activation" in lib.cat_last_error()
+
+
+def test_distances_of_rows(lib):
+    for call in ROWS:
+        for ld in (7, 0, -8, 1 << 31):
+            assert call(lib, ld=ld) == INVALID and b"apart" in lib.cat_last_error()
+        assert call(lib, N=0, ld=8) == 0 and call(lib, N=0, ld=9) == 0
+    for call in (_linear8, _gated8):
+        for name in ("ldx", "ldw"):
+            for ld in (0, 15, 17, 24, 40, (1 << 23) + 16):
+                assert call(lib, **{name: ld}) == INVALID and b"apart" in lib.cat_last_error()
+            assert call(lib, M=0, **{name: 32}) == 0
+        assert call(lib, M=0, K=13, ldx=13, ldw=16) == 0 and call(lib, M=0, K=13, ldx=14, ldw=16) == INVALID
 
 
 def test_codes_and_scales_come_together(lib):

@@ -132,6 +132,38 @@ def test_many_tiles(M, N, K, dtype):
                half_step(t) * want.abs() * (1 + U32) + U32 * want.abs() + ue * (v.abs() + ve) + u.abs() * ve, "gated")
 
 
+def _apart(codes, ld):
+    """The same codes in rows ld entries apart, everything between and behind them as large as it can be."""
+    buf = torch.full((codes.shape[0], ld), -128, dtype=torch.int8, device="cuda")
+    buf[:, :codes.shape[1]] = codes
+    return buf[:, :codes.shape[1]]
+
+
+@pytest.mark.parametrize("M,N,K", [(1, 40, 33), (5, 100, 1030), (40, 4100, 4097), (70, 96, 1), (130, 258, 1030), (300, 130, 144), (200, 300, 4001), (2304, 2050, 133)])
+def test_rows_that_lie_apart(M, N, K):
+    """Rows on 16-byte boundaries, whatever lies between them; as one operand's, the other's, both's: the same bits."""
+    x, xs, w, ws = _operands(M, N, K)
+    for call in (cat_linear8, cat_gated_linear8):
+        want = call(x, xs, w, ws, act="silu")
+        for ld in ((K + 15) // 16 * 16, (K + 15) // 16 * 16 + 48):
+            far_x, far_w = _apart(x, ld), _apart(w, ld)
+            for a, b in ((far_x, w), (x, far_w), (far_x, far_w)):
+                assert torch.equal(call(a, xs, b, ws, act="silu"), want), ld
+    wide = _apart(x, (K + 15) // 16 * 16 + 16)
+    for bad in (torch.empty((M + 1, K + 1), dtype=torch.int8, device="cuda")[1:, :K] if M > 1 else None,  # rows on any byte
+                torch.empty((K, M), dtype=torch.int8, device="cuda").t() if M > 1 and K > 1 else None):
+        if bad is not None and not bad.is_contiguous() and bad.stride(0) % 16:
+            with pytest.raises(ValueError):
+                cat_linear8(bad, xs, w, ws)
+    assert torch.equal(cat_linear8(wide, xs, w, ws), cat_linear8(x, xs, w, ws))
+
+
+def test_a_view_whose_last_row_ends_with_its_memory_is_refused():
+    view = torch.zeros(63 * 48 + 45, dtype=torch.int8, device="cuda").as_strided((64, 45), (48, 1))  # 48 entries of its last row are not there
+    with pytest.raises(ValueError):
+        cat_linear8(view, torch.ones(64, device="cuda"), torch.zeros(8, 45, dtype=torch.int8, device="cuda"), torch.ones(8, device="cuda"))
+
+
 @pytest.mark.parametrize("M", [5, 200])
 def test_nan_and_infinity_go_where_the_formula_takes_them(M):
     x, xs, w, ws = _operands(M, 150, 200)

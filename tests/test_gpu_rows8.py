@@ -2,7 +2,7 @@
 import pytest
 import torch
 
-from paper_2509_26277_amd import cat_layer_norm_quantize, cat_pack8, cat_quantize_rows
+from paper_2509_26277_amd import binding, cat_layer_norm_quantize, cat_pack8, cat_quantize_rows
 
 from block_util import TYPES, U32, assert_close, norm_ref
 
@@ -56,6 +56,19 @@ def test_more_rows_than_workgroups():
         codes, scales = cat_quantize_rows(x)
         want_c, want_s = _reference(x)
         assert torch.equal(scales.cpu(), want_s) and torch.equal(codes.cpu(), want_c)
+
+
+def test_rows_lie_on_16_byte_boundaries_and_nothing_else_is_written():
+    lib = binding.load_library()
+    for D in (1, 13, 130, 3001, 9001):
+        x = _rows(21, D, "bf16", D)
+        codes, scales = cat_quantize_rows(x)
+        assert codes.shape == (21, D) and codes.stride(0) % 16 == 0
+        for ld in (D, D + 3, (D + 15) // 16 * 16 + 16):
+            buf, s = torch.full((23, ld), 77, dtype=torch.int8, device="cuda"), torch.empty(21, device="cuda")
+            assert lib.cat_quantize_rows(x.data_ptr(), 21, D, 1, buf.data_ptr(), ld, s.data_ptr(), binding._stream()) == 0
+            assert torch.equal(buf[:21, :D], codes) and torch.equal(s, scales)
+            assert bool((buf[21:] == 77).all()) and bool((buf[:, D:] == 77).all())
 
 
 def test_ties_go_to_the_even_code_and_the_largest_float_stays_finite():
