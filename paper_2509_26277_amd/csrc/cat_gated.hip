@@ -138,7 +138,7 @@ cat_status cat_gated_backward_input(const void* dy, const void* w, const int8_t*
     e.out = dz, e.codes_in = codes, e.scales_in = scales, e.act = (int)act, e.col_sums = dbias ? (float*)(ws + pl.at_sums) : nullptr;
     CAT_TRY(lay_out(dt, pl, dy, M, N, w, nullptr, nullptr, false, 0, N, F, ws, st));
     const GemmArgs a = gemm_args(pl, entry_bytes(dt), pl.lay_q ? ws + pl.at_q : dy, M, pl.lay_p ? ws + pl.at_p : w, N, M, F, N, e, ws);
-    CAT_TRY(dt == CAT_F32 ? launch_gemm_f32(kGatedGrad, a, st) : launch_gemm_bf16(kGatedGrad, pl.large, a, st));
+    CAT_TRY(dt == CAT_F32 ? launch_gate_grad_f32(a, st) : launch_gate_grad_bf16(pl.large, a, st));
     if (pl.joined) {
         const dim3 grid((unsigned)((F + kPackGroup - 1) / kPackGroup), (unsigned)pl.sum_parts);
         if (dt == CAT_F32)

@@ -138,9 +138,12 @@ __device__ __forceinline__ void finish(const Epilogue& e, int64_t m, int64_t n, 
     st_entries<T, E>((T*)e.out + at, n, N, v);
 }
 
-// launchers of the tile kernels, one translation unit a type; `large`: tiles of 256 x 256 (not float)
+// launchers of the tile kernels, one translation unit a type, the gate's gradients, which are many, in others (and not in
+// launch_gemm_*); `large`: tiles of 256 x 256 (not float)
 cat_status launch_gemm_f32(GemmKind kind, const GemmArgs& a, hipStream_t st);
 cat_status launch_gemm_bf16(GemmKind kind, bool large, const GemmArgs& a, hipStream_t st);
+cat_status launch_gate_grad_f32(const GemmArgs& a, hipStream_t st);
+cat_status launch_gate_grad_bf16(bool large, const GemmArgs& a, hipStream_t st);
 cat_status launch_gemm_i8(GemmKind kind, bool large, cat_dtype out, const GemmArgs& a, hipStream_t st);
 
 }  // namespace cat

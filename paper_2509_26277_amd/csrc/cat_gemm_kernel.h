@@ -479,63 +479,15 @@ __device__ __forceinline__ float sums_by_lane(float (&v)[16], int r) {
     halve(std::integral_constant<int, 2>()), halve(std::integral_constant<int, 1>());
     return v[0];
 }
-// The gate's gradients: lane (r, g) as in finish_rows.  sums: this wave's row of col_sums.  Two pairs of tiles at a time for all rows,
-// so that the sums over rows are 32 registers.
-template <typename T, int MT>
+// The gate's gradients, of rows of at least eight columns: lane (r, g) as in finish_rows; sums: this wave's row of col_sums.  Two pairs
+// of tiles at a time for all rows, so that the sums over rows are 32 registers, a row's codes under way while the one before it is
+// worked on.  Nothing is stored before the last codes have come: loads and stores complete in the order of their issue, and a load
+// behind stores would be waited for as long as those (us, 65536 x 1024 over 256 bfloat16 without sums: 163, now 136; without loads 102,
+// without stores 93).  What is stored waits in the sums' registers, both gradients of an entry in one where they are bfloat16.
+// ALIGNED: rows are whole groups of eight columns.  Otherwise the codes of a row's last group come with those before them, from its last
+// eight (us, 16384 x 4097 over 1024 bfloat16: 380 with loads and stores entry by entry there, 310 so).
+template <typename T, int ACT, int MT, bool ALIGNED>
 __device__ __forceinline__ void finish_gate_grad(const Epilogue& e, f32x4 (&acc)[MT][8], int64_t m, int64_t M, int64_t n, int64_t N, int r, float* sums) {
-    const int64_t G = (N + kPackGroup - 1) / kPackGroup, group = n / kPackGroup;
-    with_act(e.act, [&](auto which) {
-        constexpr int ACT = decltype(which)::value;
-#pragma unroll
-        for (int half = 0; half < 2; half++) {
-            float s[2][16];
-#pragma unroll
-            for (int i = 0; i < 32; i++) s[i / 16][i % 16] = 0.f;
-#pragma unroll
-            for (int mt = 0; mt < MT; mt++) {
-                const int64_t row = m + 16 * mt;
-                T* out = (T*)e.out + row * 2 * N;
-#pragma unroll
-                for (int t = 0; t < 2; t++) {
-                    const int64_t at = n + 64 * half + 32 * t;
-                    if (row < M && at < N) {
-                        float gate[8], value[8];
-                        ld_codes<8>(e.codes_in + row * N, at, N, e.scales_in[row * G + group], gate);
-                        ld_codes<8>(e.codes_in + (M + row) * N, at, N, e.scales_in[(M + row) * G + group], value);
-#pragma unroll
-                        for (int i = 0; i < 8; i++) {
-                            const float d = acc[mt][4 * half + 2 * t + (i >> 2)][i & 3];
-                            float u, du;
-                            act_both<ACT, kFast<T>>(gate[i], u, du);
-                            gate[i] = d * value[i] * du;
-                            value[i] = d * u;
-                            s[t][i] += gate[i], s[t][8 + i] += value[i];
-                        }
-                        st_entries<T, 8>(out, at, N, gate);
-                        st_entries<T, 8>(out + N, at, N, value);
-                    }
-                    __builtin_amdgcn_sched_barrier(0);
-                }
-            }
-            if (sums) {
-#pragma unroll
-                for (int t = 0; t < 2; t++) {
-                    const float total = sums_by_lane(s[t], r);
-                    const int64_t c = n + 64 * half + 32 * t + (r & 7);
-                    if (c < N) sums[(r >> 3) * N + c] = total;
-                }
-            }
-            __builtin_amdgcn_sched_barrier(0);
-        }
-    });
-}
-
-// The same for rows of whole groups of eight columns, a row's codes under way while the one before it is worked on.  Nothing is stored
-// before the last codes have come: loads and stores complete in the order of their issue, and a load behind stores would be waited for
-// as long as those (us, 65536 x 1024 over 256 bfloat16 without sums: 163, now 136; without loads 102, without stores 93).  What is
-// stored waits in the sums' registers, both gradients of an entry in one where they are bfloat16.
-template <typename T, int ACT, int MT>
-__device__ __forceinline__ void finish_gate_grad8(const Epilogue& e, f32x4 (&acc)[MT][8], int64_t m, int64_t M, int64_t n, int64_t N, int r, float* sums) {
     const int64_t G = (N + kPackGroup - 1) / kPackGroup, group = n / kPackGroup;
     float steps[MT][2];
 #pragma unroll
@@ -545,13 +497,20 @@ __device__ __forceinline__ void finish_gate_grad8(const Epilogue& e, f32x4 (&acc
     }
     f32x4 second[sizeof(T) == 4 ? MT : 1][8];  // float: the value's gradients
     uint2 held[2][2][2];
-    const auto request = [&](int at, uint2(&to)[2][2]) {  // at: half * MT + row; columns behind the last: those of the row's first group
+    // from where a lane's eight codes come (columns behind the last: from any eight of the row)
+    const auto from = [&](int64_t c) { return c + 8 <= N ? c : ALIGNED ? 0 : N - 8; };
+    const auto request = [&](int at, uint2(&to)[2][2]) {  // at: half * MT + row
         const int64_t row = m + 16 * (at % MT) < M ? m + 16 * (at % MT) : M - 1;
         const int8_t *gate = e.codes_in + row * N, *value = gate + M * N;
 #pragma unroll
         for (int t = 0; t < 2; t++) {
-            const int64_t c = n + 64 * (at / MT) + 32 * t, from = c < N ? c : 0;
-            to[t][0] = *(const uint2*)(gate + from), to[t][1] = *(const uint2*)(value + from);
+            const int64_t c = from(n + 64 * (at / MT) + 32 * t);
+            if constexpr (ALIGNED) {
+                to[t][0] = *(const uint2*)(gate + c), to[t][1] = *(const uint2*)(value + c);
+            } else {
+                const Codes8 a = *(const Codes8*)(gate + c), b = *(const Codes8*)(value + c);
+                to[t][0] = make_uint2(a.w[0], a.w[1]), to[t][1] = make_uint2(b.w[0], b.w[1]);
+            }
         }
     };
     request(0, held[0]);
@@ -567,7 +526,13 @@ __device__ __forceinline__ void finish_gate_grad8(const Epilogue& e, f32x4 (&acc
 #pragma unroll
             for (int t = 0; t < 2; t++) {
                 if (m + 16 * mt < M) {
-                    const uint2 a = held[step & 1][t][0], b = held[step & 1][t][1];
+                    uint2 a = held[step & 1][t][0], b = held[step & 1][t][1];
+                    if constexpr (!ALIGNED) {
+                        const int64_t c = n + 64 * half + 32 * t;
+                        const int by = (int)(c - from(c)) * 8 & 63;
+                        const uint64_t x = (((uint64_t)a.y << 32) | a.x) >> by, y = (((uint64_t)b.y << 32) | b.x) >> by;
+                        a = make_uint2((uint32_t)x, (uint32_t)(x >> 32)), b = make_uint2((uint32_t)y, (uint32_t)(y >> 32));
+                    }
 #pragma unroll
                     for (int i = 0; i < 8; i++) {
                         const int nt = 4 * half + 2 * t + (i >> 2);
@@ -595,8 +560,8 @@ __device__ __forceinline__ void finish_gate_grad8(const Epilogue& e, f32x4 (&acc
 #pragma unroll
             for (int t = 0; t < 2; t++) {
                 const float total = sums_by_lane(s[t], r);
-                const int64_t c = n + 64 * half + 32 * t;
-                if (c < N) sums[(r >> 3) * N + c + (r & 7)] = total;
+                const int64_t c = n + 64 * half + 32 * t + (r & 7);
+                if (c < N) sums[(r >> 3) * N + c] = total;
             }
         }
         __builtin_amdgcn_sched_barrier(0);
@@ -608,22 +573,36 @@ __device__ __forceinline__ void finish_gate_grad8(const Epilogue& e, f32x4 (&acc
         T* out = (T*)e.out + row * 2 * N + n;
 #pragma unroll
         for (int t = 0; t < 4; t++) {
-            if (n + 32 * t >= N) continue;
+            const int64_t left = N - (n + 32 * t);  // columns from this lane's first on
+            if (left <= 0) continue;
             if constexpr (sizeof(T) == 2) {
-                uint32_t gate[4], value[4];
+                Group16<T> gate, value;
 #pragma unroll
                 for (int i = 0; i < 4; i++) {
                     const uint32_t lo = __float_as_uint(acc[mt][2 * t + (i >> 1)][2 * (i & 1)]), hi = __float_as_uint(acc[mt][2 * t + (i >> 1)][2 * (i & 1) + 1]);
-                    gate[i] = __builtin_amdgcn_perm(hi, lo, 0x05040100u), value[i] = __builtin_amdgcn_perm(hi, lo, 0x07060302u);
+                    gate.w[i] = __builtin_amdgcn_perm(hi, lo, 0x05040100u), value.w[i] = __builtin_amdgcn_perm(hi, lo, 0x07060302u);
                 }
-                *(uint4*)(out + 32 * t) = make_uint4(gate[0], gate[1], gate[2], gate[3]);
-                *(uint4*)(out + N + 32 * t) = make_uint4(value[0], value[1], value[2], value[3]);
-            } else {
+                if (ALIGNED) {
+                    *(uint4*)(out + 32 * t) = make_uint4(gate.w[0], gate.w[1], gate.w[2], gate.w[3]);
+                    *(uint4*)(out + N + 32 * t) = make_uint4(value.w[0], value.w[1], value.w[2], value.w[3]);
+                } else if (left >= 8) {
+                    *(Group16<T>*)(out + 32 * t) = gate, *(Group16<T>*)(out + N + 32 * t) = value;
+                } else {
 #pragma unroll
-                for (int i = 0; i < 2; i++) {
-                    *(f32x4*)(out + 32 * t + 4 * i) = acc[mt][2 * t + i];
-                    *(f32x4*)(out + N + 32 * t + 4 * i) = second[mt][2 * t + i];
+                    for (int i = 0; i < 7; i++)
+                        if (i < left) out[32 * t + i] = (T)(gate.w[i / 2] >> 16 * (i % 2)), out[N + 32 * t + i] = (T)(value.w[i / 2] >> 16 * (i % 2));
                 }
+            } else {
+                const auto store = [&](T* to, const f32x4& lo, const f32x4& hi) {
+                    if (ALIGNED) {
+                        *(f32x4*)to = lo, *(f32x4*)(to + 4) = hi;
+                    } else {
+                        const float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+                        st_entries<T, 8>(to, 0, left, v);
+                    }
+                };
+                store(out + 32 * t, acc[mt][2 * t], acc[mt][2 * t + 1]);
+                store(out + N + 32 * t, second[mt][2 * t], second[mt][2 * t + 1]);
             }
         }
         __builtin_amdgcn_sched_barrier(0);
@@ -631,9 +610,9 @@ __device__ __forceinline__ void finish_gate_grad8(const Epilogue& e, f32x4 (&acc
 }
 
 // Workgroups stay for all of their tiles: a tile's first loads are under way while the one before it is finished and stored.
-// ACT >= 0: the gate's gradients of that activation, in rows of whole groups of eight columns (one kernel for all of them leaves the
-// compiler no registers).
-template <typename E, typename T, int KIND, int TM, int TN, int WM, int ACT = -1>
+// ACT, ALIGNED: of the gate's gradients (one kernel for all activations leaves the compiler no registers); ACT < 0, for those: the joining
+// kernel works them out.
+template <typename E, typename T, int KIND, int TM, int TN, int WM, int ACT = -1, bool ALIGNED = true>
 __global__ __launch_bounds__((TM / WM) * (TN / 128) * 64, 2) void k_gemm(const GemmArgs a) {
 #ifdef __HIP_DEVICE_COMPILE__  // (the host's pass does not know all of the builtins, and would leave out the kernel's stub)
     constexpr bool GATED = KIND == kGated, FORWARD = KIND == kForward || GATED, PT = !FORWARD, QT = KIND == kWeightGrad;
@@ -867,9 +846,7 @@ __global__ __launch_bounds__((TM / WM) * (TN / 128) * 64, 2) void k_gemm(const G
             } else if constexpr (KIND == kGatedGrad) {
                 float* col_sums = a.e.col_sums ? a.e.col_sums + ((int64_t)tile_m * (TM / WM) + wm) * 2 * a.n : nullptr;
                 if constexpr (ACT >= 0) {
-                    if (nw < a.n) finish_gate_grad8<T, ACT, MT>(a.e, acc, m, a.m, nl, a.n, r, col_sums);
-                } else {
-                    if (nw < a.n) finish_gate_grad<T, MT>(a.e, acc, m, a.m, nl, a.n, r, col_sums);
+                    if (nw < a.n) finish_gate_grad<T, ACT, MT, ALIGNED>(a.e, acc, m, a.m, nl, a.n, r, col_sums);
                 }
             } else {
                 constexpr bool kI8 = sizeof(E) == 1;
@@ -888,30 +865,33 @@ __global__ __launch_bounds__((TM / WM) * (TN / 128) * 64, 2) void k_gemm(const G
 #endif
 }
 
-template <typename E, typename T, int KIND, int TM, int TN, int WM, int ACT = -1>
+template <typename E, typename T, int KIND, int TM, int TN, int WM, int ACT = -1, bool ALIGNED = true>
 cat_status launch_gemm_tiles(const GemmArgs& a, hipStream_t st) {
     constexpr int TO = KIND == kGated ? TN / 2 : TN;
     const int64_t tiles = ((a.m + TM - 1) / TM) * ((a.n + TO - 1) / TO);
     if (tiles * a.splits >= (1ll << 31)) return set_error(CAT_ERR_UNSUPPORTED, "product of %lld x %lld entries has too many tiles", (long long)a.m, (long long)a.n);
     // as many workgroups as the card holds at a time (256 CUs, by LDS one large tile's or two small ones' each)
     const int64_t most = 256 * (TM == 256 ? 1 : 2);
-    hipLaunchKernelGGL((k_gemm<E, T, KIND, TM, TN, WM, ACT>), dim3((unsigned)(a.splits > 1 ? tiles * a.splits : tiles < most ? tiles : most)), dim3((TM / WM) * (TN / 128) * 64), 0, st, a);
+    hipLaunchKernelGGL((k_gemm<E, T, KIND, TM, TN, WM, ACT, ALIGNED>), dim3((unsigned)(a.splits > 1 ? tiles * a.splits : tiles < most ? tiles : most)), dim3((TM / WM) * (TN / 128) * 64), 0, st, a);
     CAT_LAUNCH_CHECK("k_gemm");
     return CAT_OK;
 }
 
-// the gate's gradients: a kernel for each activation where rows are whole groups of eight columns, one for all where they are not (or
-// where the joining kernel works them out)
+// the gate's gradients: a kernel for each activation and for either alignment of rows, or the sums alone
+template <typename T, int EDGE, int WM, bool ALIGNED>
+cat_status launch_gate_grad(const GemmArgs& a, hipStream_t st) {
+    switch (a.e.act) {
+        case CAT_ACT_NONE: return launch_gemm_tiles<T, T, kGatedGrad, EDGE, EDGE, WM, CAT_ACT_NONE, ALIGNED>(a, st);
+        case CAT_ACT_RELU: return launch_gemm_tiles<T, T, kGatedGrad, EDGE, EDGE, WM, CAT_ACT_RELU, ALIGNED>(a, st);
+        case CAT_ACT_GELU: return launch_gemm_tiles<T, T, kGatedGrad, EDGE, EDGE, WM, CAT_ACT_GELU, ALIGNED>(a, st);
+        case CAT_ACT_GELU_TANH: return launch_gemm_tiles<T, T, kGatedGrad, EDGE, EDGE, WM, CAT_ACT_GELU_TANH, ALIGNED>(a, st);
+        default: return launch_gemm_tiles<T, T, kGatedGrad, EDGE, EDGE, WM, CAT_ACT_SILU, ALIGNED>(a, st);
+    }
+}
 template <typename T, int EDGE, int WM>
 cat_status launch_gate_grad(const GemmArgs& a, hipStream_t st) {
-    if (a.n % 8 != 0 || a.parts) return launch_gemm_tiles<T, T, kGatedGrad, EDGE, EDGE, WM>(a, st);
-    switch (a.e.act) {
-        case CAT_ACT_NONE: return launch_gemm_tiles<T, T, kGatedGrad, EDGE, EDGE, WM, CAT_ACT_NONE>(a, st);
-        case CAT_ACT_RELU: return launch_gemm_tiles<T, T, kGatedGrad, EDGE, EDGE, WM, CAT_ACT_RELU>(a, st);
-        case CAT_ACT_GELU: return launch_gemm_tiles<T, T, kGatedGrad, EDGE, EDGE, WM, CAT_ACT_GELU>(a, st);
-        case CAT_ACT_GELU_TANH: return launch_gemm_tiles<T, T, kGatedGrad, EDGE, EDGE, WM, CAT_ACT_GELU_TANH>(a, st);
-        default: return launch_gemm_tiles<T, T, kGatedGrad, EDGE, EDGE, WM, CAT_ACT_SILU>(a, st);
-    }
+    if (a.parts) return launch_gemm_tiles<T, T, kGatedGrad, EDGE, EDGE, WM>(a, st);
+    return a.n % 8 ? launch_gate_grad<T, EDGE, WM, false>(a, st) : launch_gate_grad<T, EDGE, WM, true>(a, st);
 }
 
 }  // namespace cat

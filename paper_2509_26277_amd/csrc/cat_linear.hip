@@ -123,7 +123,7 @@ Plan plan(GemmKind kind, int64_t m, int64_t n, int64_t k, int64_t rows_q, int64_
         if (pl.k_split < step) pl.k_split = step;
         pl.splits = (int)((k + pl.k_split - 1) / pl.k_split);
         if (pl.splits < 1) pl.splits = 1;
-        pl.joined = pl.splits > 1 || (kind == kGated && pack && !pl.large);
+        pl.joined = pl.splits > 1 || (kind == kGated && pack && !pl.large) || (kind == kGatedGrad && n < 8);
     }
     size_t at = 0;
     pl.at_q = at;
@@ -151,7 +151,7 @@ Plan plan(GemmKind kind, int64_t m, int64_t n, int64_t k, int64_t rows_q, int64_
             int64_t P = 1024 / G;
             P = P < most ? P : most;
             P = P < 1 ? 1 : P;
-            pl.sum_rows = (m + P - 1) / P;
+            pl.sum_rows = m > P ? (m + P - 1) / P : 1;
             pl.sum_parts = (int)((m + pl.sum_rows - 1) / pl.sum_rows);
         } else {
             const int64_t edge = pl.large ? 256 : 128;

@@ -12,7 +12,7 @@ pytestmark = pytest.mark.gpu
 # (M, F, K): single rows and few rows, tiles with ragged ends in every direction, odd lengths (the value's rows, bias and gradients
 # then start on any boundary), shares of k, one entry; large tiles (bfloat16) whole and ragged, with shares, and more than workgroups
 SHAPES = [(1, 1, 1), (1, 16, 8), (1, 1001, 2048), (3, 17, 33), (16, 100, 512), (17, 65, 300), (33, 64, 136), (64, 257, 1030), (48, 40, 4096),
-          (65, 64, 64), (66, 1, 7), (100, 129, 100), (128, 128, 128), (129, 255, 136), (300, 513, 1030), (200, 150, 4096), (777, 12, 63),
+          (65, 64, 64), (66, 1, 7), (100, 129, 100), (128, 128, 128), (129, 255, 136), (300, 513, 1030), (200, 150, 4096), (777, 12, 63), (300, 9, 40), (2100, 7, 64), (513, 15, 128),
           (1025, 320, 72), (3600, 1795, 72), (3584, 1920, 200), (2000, 1001, 6000), (6144, 2560, 256), (6001, 2503, 130), (4864, 2048, 64)]
 # a few rows behind the last whole tile, for which the tiles would need a round of workgroups more
 TAILS = [("f32", 923, 2051, 130), ("f32", 4099, 1001, 513), ("bf16", 8200, 1001, 130), ("bf16", 8193, 1000, 128)]
