@@ -225,10 +225,11 @@ __device__ __forceinline__ Sums<T> multiply(f32x4 a, f32x4 b, Sums<T> c) {
 // acc[mt][2 t] and acc[mt][2 t + 1].  WHOLE: all columns lie inside out, whose rows are whole 16-byte groups.  Otherwise the
 // eight columns are read and written where they lie (16-byte accesses on an element's boundary), entry by entry where they
 // cross the row's end.
-template <typename T, bool WHOLE>
+// Not ALIGNED, WHOLE: all columns lie inside out, whose rows start anywhere.
+template <typename T, bool WHOLE, bool ALIGNED = true>
 __device__ __forceinline__ void ld8(const T* row, int64_t n, int64_t N, float (&v)[8]) {
-    if constexpr (!WHOLE) {
-        ld_entries<T, 8>(row, n, N, v);
+    if constexpr (!WHOLE || !ALIGNED) {
+        ld_entries<T, 8>(row, n, WHOLE ? n + 8 : N, v);
     } else if constexpr (sizeof(T) == 2) {
         const uint4 q = *(const uint4*)(row + n);
         const uint32_t w[4] = {q.x, q.y, q.z, q.w};
@@ -240,10 +241,10 @@ __device__ __forceinline__ void ld8(const T* row, int64_t n, int64_t N, float (&
         for (int e = 0; e < 4; e++) v[e] = lo[e], v[4 + e] = hi[e];
     }
 }
-template <typename T, bool WHOLE>
+template <typename T, bool WHOLE, bool ALIGNED = true>
 __device__ __forceinline__ void st8(T* row, int64_t n, int64_t N, const float (&v)[8]) {
-    if constexpr (!WHOLE) {
-        st_entries<T, 8>(row, n, N, v);
+    if constexpr (!WHOLE || !ALIGNED) {
+        st_entries<T, 8>(row, n, WHOLE ? n + 8 : N, v);
     } else if constexpr (sizeof(T) == 2) {
         *(uint4*)(row + n) = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
     } else {
@@ -252,8 +253,9 @@ __device__ __forceinline__ void st8(T* row, int64_t n, int64_t N, const float (&
     }
 }
 // I8: of 8-bit integers, whose products leave no checkpoint.  CUT (with WHOLE): rows are whole groups of eight columns, of which some
-// lie behind the row's end.
-template <typename T, int KIND, bool I8, int MT, bool WHOLE, bool CUT = false>
+// lie behind the row's end.  Not ALIGNED (with WHOLE): all columns inside, rows that start anywhere (us, 16384 x 8198 over 1024 to fp32: 325
+// with every group compared with the row's end, 269; bfloat16 with a residual 253 and 241.  The gated product gains nothing so).
+template <typename T, int KIND, bool I8, int MT, bool WHOLE, bool CUT = false, bool ALIGNED = true>
 __device__ __forceinline__ void finish_rows(const Epilogue& e, f32x4 (&acc)[MT][8], int64_t m, int64_t M, int64_t n, int64_t N, int g) {
     const int64_t G = (N + kPackGroup - 1) / kPackGroup, group = n / kPackGroup;
     constexpr int FAST = I8 ? kFast<T> : sizeof(T) == 2;
@@ -292,7 +294,7 @@ __device__ __forceinline__ void finish_rows(const Epilogue& e, f32x4 (&acc)[MT][
     }
     // What the tile reads besides its sums (the residual; the argument of the derivative), as it lies, for all of its rows at
     // once: they come from memory, and row by row each of them would be waited for.
-    constexpr bool kAhead = WHOLE && (KIND == kInputGrad || (KIND == kForward && MT * sizeof(T) <= 8));  // (what the registers hold)
+    constexpr bool kAhead = WHOLE && ALIGNED && (KIND == kInputGrad || (KIND == kForward && MT * sizeof(T) <= 8));  // (what the registers hold)
     constexpr int kWords = !kAhead ? 1 : KIND == kInputGrad ? 2 : 2 * (int)sizeof(T);
     uint32_t raw[kAhead ? MT : 1][4][kWords];
     float steps[MT];
@@ -337,7 +339,7 @@ __device__ __forceinline__ void finish_rows(const Epilogue& e, f32x4 (&acc)[MT][
             } else if constexpr (res) {
 #pragma unroll
                 for (int t = 0; t < 4; t++)
-                    if (!CUT || n + 32 * t < N) ld8<T, WHOLE>((const T*)e.residual + row * N, n + 32 * t, N, more[t]);
+                    if (!CUT || n + 32 * t < N) ld8<T, WHOLE, ALIGNED>((const T*)e.residual + row * N, n + 32 * t, N, more[t]);
             }
             if constexpr (KIND == kInputGrad && ACT != CAT_ACT_NONE) {
 #pragma unroll
@@ -360,7 +362,7 @@ __device__ __forceinline__ void finish_rows(const Epilogue& e, f32x4 (&acc)[MT][
                     if constexpr (KIND == kInputGrad) v[i] *= act_grad<ACT, FAST>(more[t][i]);
                     if constexpr (res) v[i] += more[t][i];
                 }
-                if (!CUT || n + 32 * t < N) st8<T, WHOLE>((T*)e.out + row * N, n + 32 * t, N, v);
+                if (!CUT || n + 32 * t < N) st8<T, WHOLE, ALIGNED>((T*)e.out + row * N, n + 32 * t, N, v);
             }
             __builtin_amdgcn_sched_barrier(0);
         }
@@ -854,6 +856,8 @@ __global__ __launch_bounds__((TM / WM) * (TN / 128) * 64, 2) void k_gemm(const G
                     finish_rows<T, KIND, kI8, MT, true>(a.e, acc, m, a.m, nl, a.n, g);
                 else if (kI8 && nw < a.n && a.n % 8 == 0)
                     finish_rows<T, KIND, kI8, MT, true, kI8>(a.e, acc, m, a.m, nl, a.n, g);
+                else if (kI8 && nw + WN <= a.n)
+                    finish_rows<T, KIND, kI8, MT, true, false, !kI8>(a.e, acc, m, a.m, nl, a.n, g);
                 else if (nw < a.n)
                     finish_rows<T, KIND, kI8, MT, false>(a.e, acc, m, a.m, nl, a.n, g);
             }
