@@ -51,10 +51,16 @@ struct GemmArgs {
     int64_t m, n, k;
     int64_t k_split;  // entries of k a share takes (a multiple of the kernel's step)
     int splits;
-    void* parts;  // instead of an epilogue: sums as they are, splits x m x n (gated: x 2 n), float or 32-bit integers
+    void* parts;  // instead of an epilogue: sums as they are, splits x m x n (gated: x 2 n), float or 32-bit integers; of weight
+                  // gradients tile by tile, as the registers hold them (splits x tiles x TM x TN)
     Epilogue e;
 };
 
+// Tiles in the order in which the XCDs take them: eight columns at a time.
+__host__ __device__ inline void tile_place(uint32_t tile, uint32_t tm, uint32_t tn, uint32_t& row, uint32_t& column) {
+    const uint32_t band = tile / (8 * tm), in = tile - band * 8 * tm, width = tn - band * 8 < 8 ? tn - band * 8 : 8;
+    row = in / width, column = band * 8 + in % width;
+}
 constexpr int64_t kGemmMaxRowBytes = 1 << 23;  // offsets inside a tile of 256 rows stay below 2^31
 
 // E (4 or 8) neighbouring entries of a row of out, from column n on (a multiple of E), through the epilogue.  PACK: the 16 lanes of

@@ -640,10 +640,7 @@ __global__ __launch_bounds__((TM / WM) * (TN / 128) * 64, 2) void k_gemm(const G
     uint32_t t = xcd * share + (xcd < more ? xcd : more) + blockIdx.x / 8, share_of_k = 0;
     if (t >= end) return;
     if (a.splits > 1) share_of_k = t / tiles, t -= share_of_k * tiles, end = t + 1, stride = 1;  // (a tile each)
-    const auto place = [&](uint32_t tile, uint32_t& m0, uint32_t& n0) {
-        const uint32_t band = tile / (8 * tm), in = tile - band * 8 * tm, width = tn - band * 8 < 8 ? tn - band * 8 : 8;
-        m0 = in / width, n0 = band * 8 + in % width;
-    };
+    const auto place = [&](uint32_t tile, uint32_t& m0, uint32_t& n0) { tile_place(tile, tm, tn, m0, n0); };
 
     const int64_t k0 = (int64_t)share_of_k * a.k_split, k_all = a.k - k0 < a.k_split ? a.k - k0 : a.k_split;
     Stage<E, PT, true, TN, W> sp;
@@ -794,7 +791,11 @@ __global__ __launch_bounds__((TM / WM) * (TN / 128) * 64, 2) void k_gemm(const G
         asm volatile("" : "+v"(lane_end));
         const int r = lane_end & 15, g = lane_end >> 4;
         const int64_t nw = n0 + wn * WO, nl = nw + 8 * g;  // the wave's first column; this lane's of pair t: nl + 32 t (gated: t & 1)
-        if (a.parts) {  // the sums as they are (of a share of k, say): a kernel of its own goes on with them
+        if (KIND == kWeightGrad && a.parts) {  // 1 KB a store of a wave (us, 1024 x 4096 over 16384 rows: 158 with pieces of 16 bytes of rows, 140 so)
+            float* part = (float*)a.parts + (((int64_t)share_of_k * tiles + t) * (TM * TN) + wave * (WM * WN)) + lane_end * 4;
+#pragma unroll
+            for (int i = 0; i < MT * NT; i++) *(Sums<E>*)(part + i * 256) = sums[i / NT][i % NT];
+        } else if (a.parts) {  // the sums as they are (of a share of k, say): a kernel of its own goes on with them
             const int64_t width = GATED ? 2 * a.n : a.n;
 #pragma unroll
             for (int mt = 0; mt < MT; mt++) {

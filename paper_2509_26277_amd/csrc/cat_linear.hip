@@ -132,7 +132,10 @@ Plan plan(GemmKind kind, int64_t m, int64_t n, int64_t k, int64_t rows_q, int64_
     if (pl.lay_p) at += up256((size_t)rows_p * pl.ldp * entry);
     pl.at_parts = at;
     // (few rows: the checkpoint's groups of 128 columns are found by the joining kernel, whatever the number of shares)
-    if (pl.joined || (pl.few && (own || pack || pl.splits > 1))) at += up256((size_t)pl.splits * m * (kind == kGated ? 2 * n : n) * 4);
+    if (pl.joined && kind == kWeightGrad) {
+        const int64_t edge = pl.large ? 256 : 128;
+        at += up256((size_t)pl.splits * ((m + edge - 1) / edge) * ((n + edge - 1) / edge) * edge * edge * 4);
+    } else if (pl.joined || (pl.few && (own || pack || pl.splits > 1))) at += up256((size_t)pl.splits * m * (kind == kGated ? 2 * n : n) * 4);
     pl.at_sums = at;
     if (kind == kWeightGrad) {  // sums over the rows of dy (k rows, m columns)
         const int64_t v = 16 / entry, gx = (m + 64 * v - 1) / (64 * v);
@@ -164,6 +167,32 @@ Plan plan(GemmKind kind, int64_t m, int64_t n, int64_t k, int64_t rows_q, int64_
 }
 
 namespace {
+
+// The shares of k of a weight's gradient, as the tile kernel left them: a thread eight neighbouring columns of a row, which are a lane's
+// of two of its tiles of 16 x 16.
+template <typename T>
+__global__ __launch_bounds__(256) void k_join_tiles(const float* __restrict__ parts, int splits, int64_t m, int64_t n, int edge, uint32_t tm, uint32_t tn, T* __restrict__ out) {
+    const int rows = edge / 64;  // tiles of 16 rows a wave
+    const int64_t tiles = (int64_t)tm * tn, each = (int64_t)edge * edge, pieces = tiles * each / 8;
+    for (int64_t p = (int64_t)blockIdx.x * 256 + threadIdx.x; p < pieces; p += (int64_t)gridDim.x * 256) {
+        const int64_t tile = p / (each / 8);
+        const int in = (int)(p - tile * (each / 8)), lane = in & 63, pair = in / 64 % 4, row16 = in / 256 % rows, wave = in / 256 / rows;
+        uint32_t tile_m, tile_n;
+        tile_place((uint32_t)tile, tm, tn, tile_m, tile_n);
+        const int across = edge / 128, wm = wave / across, wn = wave % across;
+        const int64_t row = (int64_t)tile_m * edge + wm * (edge / 4) + row16 * 16 + (lane & 15), column = (int64_t)tile_n * edge + wn * 128 + pair * 32 + (lane >> 4) * 8;
+        if (row >= m || column >= n) continue;
+        const float* at = parts + tile * each + ((int64_t)(wave * rows + row16) * 8 + 2 * pair) * 256 + lane * 4;
+        float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        for (int s = 0; s < splits; s++) {
+            const f32x4 lo = *(const f32x4*)(at + s * tiles * each), hi = *(const f32x4*)(at + s * tiles * each + 256);
+#pragma unroll
+            for (int i = 0; i < 4; i++) v[i] += lo[i], v[4 + i] += hi[i];
+        }
+        st_entries<T, 8>(out + row * n, column, n, v);
+    }
+}
+
 template <typename T>
 cat_status join(GemmKind kind, const void* parts, int splits, int64_t M, int64_t N, const Epilogue& e, hipStream_t st) {
     if (kind == kForward) return join<T, T, kForward>(parts, splits, M, N, e, st);
@@ -176,6 +205,17 @@ cat_status multiply_tiles(GemmKind kind, const Plan& pl, cat_dtype dt, const voi
     const GemmArgs a = gemm_args(pl, entry_bytes(dt), q, rows_q, p, rows_p, m, n, k, e, ws);
     CAT_TRY(dt == CAT_F32 ? launch_gemm_f32(kind, a, st) : launch_gemm_bf16(kind, pl.large, a, st));
     if (!pl.joined) return CAT_OK;
+    if (kind == kWeightGrad) {
+        const int edge = pl.large ? 256 : 128;
+        const uint32_t tm = (uint32_t)((m + edge - 1) / edge), tn = (uint32_t)((n + edge - 1) / edge);
+        const dim3 grid(blocks_of((int64_t)tm * tn * edge * edge / 8));
+        if (dt == CAT_F32)
+            hipLaunchKernelGGL(k_join_tiles<float>, grid, dim3(256), 0, st, (const float*)a.parts, pl.splits, m, n, edge, tm, tn, (float*)e.out);
+        else
+            hipLaunchKernelGGL(k_join_tiles<bf16_t>, grid, dim3(256), 0, st, (const float*)a.parts, pl.splits, m, n, edge, tm, tn, (bf16_t*)e.out);
+        CAT_LAUNCH_CHECK("k_join_tiles");
+        return CAT_OK;
+    }
     return dt == CAT_F32 ? join<float>(kind, a.parts, pl.splits, m, n, e, st) : join<bf16_t>(kind, a.parts, pl.splits, m, n, e, st);
 }
 
