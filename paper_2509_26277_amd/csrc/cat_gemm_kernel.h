@@ -252,6 +252,25 @@ __device__ __forceinline__ void st8(T* row, int64_t n, int64_t N, const float (&
         *(f32x4*)(row + n + 4) = f32x4{v[4], v[5], v[6], v[7]};
     }
 }
+// Float results: eight columns a lane are two stores of 16 bytes, each of which would leave gaps as wide.  Lanes r and r + 8 exchange
+// halves, so that one store has the whole 128 bytes of rows 0..7 of 16 and the other those of rows 8..15.  to: columns n .. n + 7 of
+// the lane's own row, r of 16; `left` rows from the first of the 16 on are there.  All lanes of a row of 16 take part.
+// (us: gate's gradients 8192 x 1000 over 256 60 -> 57, 65536 x 1000 over 512 8-bit integers 90 -> 83; of long rows it is the slower one, 16384 x
+// 8192 over 1024 8-bit integers 236 -> 243, and of the gated float product, bound by its products, neither.)
+constexpr int64_t kExchangeMost = 1024;  // columns of out, of 8-bit integers
+__device__ __forceinline__ void st_float_rows(float* to, int64_t pitch, int64_t left, int r, f32x4 lo, f32x4 hi) {
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+        const int a = (int)__float_as_uint(lo[i]), b = (int)__float_as_uint(hi[i]);
+        lo[i] = __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(a, b, 0x128, 0xF, 0xC, false));  // row_ror 8, lanes 8..15
+        hi[i] = __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(b, a, 0x128, 0xF, 0x3, false));  // lanes 0..7
+    }
+    const int row = r & 7;
+    float* at = to + (row - r) * pitch + 4 * (r >> 3);
+    if (row < left) *(Group16<float>*)at = __builtin_bit_cast(Group16<float>, lo);
+    if (row + 8 < left) *(Group16<float>*)(at + 8 * pitch) = __builtin_bit_cast(Group16<float>, hi);
+}
+
 // I8: of 8-bit integers, whose products leave no checkpoint.  CUT (with WHOLE): rows are whole groups of eight columns, of which some
 // lie behind the row's end.  Not ALIGNED (with WHOLE): all columns inside, rows that start anywhere (us, 16384 x 8198 over 1024 to fp32: 325
 // with every group compared with the row's end, 269; bfloat16 with a residual 253 and 241.  The gated product gains nothing so).
@@ -326,8 +345,9 @@ __device__ __forceinline__ void finish_rows(const Epilogue& e, f32x4 (&acc)[MT][
         if constexpr (KIND == kInputGrad ? ACT != CAT_ACT_NONE : res) request();
 #pragma unroll
         for (int mt = 0; mt < MT; mt++) {
-            const int64_t row = m + 16 * mt;
-            if (row >= M) continue;
+            constexpr bool kExchange = I8 && sizeof(T) == 4 && WHOLE;
+            const int64_t row = kExchange && m + 16 * mt >= M ? M - 1 : m + 16 * mt;
+            if (!kExchange && row >= M) continue;
             float more[4][8];
             if constexpr (kAhead && res) {
 #pragma unroll
@@ -362,7 +382,16 @@ __device__ __forceinline__ void finish_rows(const Epilogue& e, f32x4 (&acc)[MT][
                     if constexpr (KIND == kInputGrad) v[i] *= act_grad<ACT, FAST>(more[t][i]);
                     if constexpr (res) v[i] += more[t][i];
                 }
-                if (!CUT || n + 32 * t < N) st8<T, WHOLE, ALIGNED>((T*)e.out + row * N, n + 32 * t, N, v);
+                if constexpr (kExchange) {
+                    const int r = threadIdx.x & 15;
+                    if (CUT && n + 32 * t >= N) continue;
+                    if (N > kExchangeMost) {
+                        if (m + 16 * mt < M) st8<T, WHOLE, ALIGNED>((T*)e.out + row * N, n + 32 * t, N, v);
+                    } else
+                        st_float_rows((float*)e.out + (m + 16 * mt) * N + n + 32 * t, N, M - (m + 16 * mt - r), r, f32x4{v[0], v[1], v[2], v[3]}, f32x4{v[4], v[5], v[6], v[7]});
+                } else {
+                    if (!CUT || n + 32 * t < N) st8<T, WHOLE, ALIGNED>((T*)e.out + row * N, n + 32 * t, N, v);
+                }
             }
             __builtin_amdgcn_sched_barrier(0);
         }
@@ -571,7 +600,7 @@ __device__ __forceinline__ void finish_gate_grad(const Epilogue& e, f32x4 (&acc)
 #pragma unroll
     for (int mt = 0; mt < MT; mt++) {
         const int64_t row = m + 16 * mt;
-        if (row >= M) continue;
+        if (sizeof(T) == 2 && row >= M) continue;
         T* out = (T*)e.out + row * 2 * N + n;
 #pragma unroll
         for (int t = 0; t < 4; t++) {
@@ -596,9 +625,9 @@ __device__ __forceinline__ void finish_gate_grad(const Epilogue& e, f32x4 (&acc)
                 }
             } else {
                 const auto store = [&](T* to, const f32x4& lo, const f32x4& hi) {
-                    if (ALIGNED) {
-                        *(f32x4*)to = lo, *(f32x4*)(to + 4) = hi;
-                    } else {
+                    if (ALIGNED || left >= 8) {
+                        st_float_rows((float*)to, 2 * N, M - (row - r), r, lo, hi);
+                    } else if (row < M) {
                         const float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
                         st_entries<T, 8>(to, 0, left, v);
                     }
