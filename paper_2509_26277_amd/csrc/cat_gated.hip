@@ -8,6 +8,10 @@
 //
 // A wave of the tile kernel works on 64 columns of the gate and the same 64 of the value, so that both meet in a lane's registers:
 // neither projection, nor dh, goes to memory.
+//
+// The products bound them and, on top, what a tile's end reads and writes (us, bfloat16: 16384 x 2 x 4096 over 1024 212, with checkpoints 270;
+// both gradients of 16384 x 4096 over 1024 203, where the products alone take 117; dW2 of the same 122, its shares' join 13, act(g) * v laid
+// out 54; float, 8192 x 1000 over 256: 52, and 38, 7, 12).
 #include "cat_product.h"
 
 namespace cat {

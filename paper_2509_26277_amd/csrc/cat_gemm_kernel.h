@@ -1,8 +1,8 @@
 // The tile kernel of the block's matrix products on the matrix cores (v_mfma_f32_16x16x32_bf16, v_mfma_f32_16x16x4_f32:
-// exact products, fp32 sums).
+// exact products, fp32 sums; v_mfma_i32_16x16x64_i8: exact sums).
 //
-// A workgroup computes TM x TN entries of out, each of its waves WM x 128.  A step takes 128 bytes of k (64 bfloat16 or 32
-// float entries) of both operands into LDS by loads that go there directly (no registers, no stores; what lies outside an
+// A workgroup computes TM x TN entries of out, each of its waves WM x 128.  A step takes 128 bytes of k (64 bfloat16, 32
+// float or 128 8-bit entries) of both operands into LDS by loads that go there directly (no registers, no stores; what lies outside an
 // operand arrives as zeros by the bounds of its buffer), two steps' worth of LDS in turn.
 //   k contiguous: 128 bytes of a row, its eight 16-byte chunks c at position c ^ key(row), so that the 16 rows of a
 //                 fragment are read without bank conflicts; the load's lane order does the exchange.
@@ -19,6 +19,8 @@
 // 16384 x 8192 over 2048 with GELU, at 2.0 GHz; what comes on top of the steps is the epilogue, whose instructions they wait for:
 // GELU 21 us of 16384 x 4096 over 1024 (126 without), codes 14, a derivative 40 (121 without).  (Through LDS, 16 rows at a time, a tile's epilogue took 11 to
 // 27 us, as long as 8 to 16 steps of k.)
+// 8-bit integers (TOP/s; the library 2050 at 8192^3): 8192^3 2270 to 2510, gated 2730; 16384 x 8192 over 2048 2300, with GELU 2140.  Gated bfloat16
+// 8192 x 2 x 4096 over 8192 1450 to 1490, checkpoints 4 % more time; 16384 x 2 x 4096 over 1024 212 us, with checkpoints 255 to 270.
 #pragma once
 #include "cat_gemm.h"
 

@@ -6,6 +6,9 @@
 // One pass over memory and bound by it, 3 bytes an entry of bfloat16 rows, 5 of float ones: a row is read once and stays in
 // registers for its statistics, its largest magnitude and its codes, the next one requested ahead, as in layer norm.  Rows of more
 // than 8192 entries have a workgroup each that reads the row again for every use.
+//
+// Measured (us, inputs from memory): 65536 x 1024 bfloat16 33 (6.1 TB/s), fp32 63 (5.3); through the norm 49 and 66: the bfloat16 norm is bound
+// by its instructions.  One row of 2048: 2.7.
 #include "cat_rows.h"
 
 namespace cat {
