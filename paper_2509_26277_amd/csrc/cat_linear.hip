@@ -99,7 +99,7 @@ Plan plan(GemmKind kind, int64_t m, int64_t n, int64_t k, int64_t rows_q, int64_
           bool pack) {
     Plan pl = {};
     const int64_t step = 128 / entry;
-    const int64_t bytes_w = rows_p * cols_p * entry;
+    const int64_t bytes_w = rows_p * k * entry;  // (however far apart its rows lie: the sizes of workspace know nothing of that)
     const bool own = kind == kForward && entry > 1;  // (the products of the block's training step: as they were)
     pl.few = (kind == kForward || kind == kGated) && m <= kFewRows && (own || m <= 16 || bytes_w < kFewMostBytes);
     pl.ldq = cols_q, pl.ldp = cols_p;

@@ -158,6 +158,20 @@ def test_rows_that_lie_apart(M, N, K):
     assert torch.equal(cat_linear8(wide, xs, w, ws), cat_linear8(x, xs, w, ws))
 
 
+@pytest.mark.parametrize("M,N,K", [(17, 1030, 8208), (40, 4100, 8208), (64, 4100, 8208), (64, 8200, 8208)])
+def test_few_rows_by_a_large_weight_whose_rows_lie_apart(M, N, K):
+    """What lies between the rows of w counts for nothing: the same bits, in a workspace of the stated size."""
+    x, xs, w, ws = _operands(M, N, K)
+    z, z_err = _product(x, xs, w, ws, None)
+    want = z.clamp(min=0)
+    y = cat_linear8(x, xs, w, ws, act="relu", dtype=torch.float32)
+    _close(y, want, z_err + U32 * want, "y")
+    room = torch.empty(binding.load_library().cat_linear8_workspace_bytes(M, N, K), dtype=torch.uint8, device="cuda")
+    assert torch.equal(cat_linear8(x, xs, _apart(w, 3 * K), ws, act="relu", dtype=torch.float32, workspace=room), y)
+    far = cat_gated_linear8(x, xs, _apart(w, 3 * K), ws, act="silu")
+    assert torch.equal(far, cat_gated_linear8(x, xs, w, ws, act="silu"))
+
+
 def test_a_view_whose_last_row_ends_with_its_memory_is_refused():
     view = torch.zeros(63 * 48 + 45, dtype=torch.int8, device="cuda").as_strided((64, 45), (48, 1))  # 48 entries of its last row are not there
     with pytest.raises(ValueError):
