@@ -82,7 +82,7 @@ extern "C" {
 
 size_t cat_gated_linear_workspace_bytes(int64_t M, int64_t F, int64_t K, cat_dtype dt) {
     if (check_linear("cat_gated_linear_workspace_bytes", M, F, K, dt) != CAT_OK) return 0;
-    const size_t a = plan_gated(M - tail_rows(kGated, M, F, K, entry_bytes(dt)), F, K, dt, false).total, b = plan_gated(M, F, K, dt, true).total;
+    const size_t a = stated(plan_gated(M - tail_rows(kGated, M, F, K, entry_bytes(dt)), F, K, dt, false)), b = stated(plan_gated(M, F, K, dt, true));
     return a > b ? a : b;
 }
 
@@ -118,7 +118,7 @@ cat_status cat_gated_linear(const void* x, const void* w, const float* bias, int
 
 size_t cat_gated_backward_workspace_bytes(int64_t M, int64_t N, int64_t F, cat_dtype dt) {
     if (check_linear("cat_gated_backward_workspace_bytes", M, N, F, dt) != CAT_OK) return 0;
-    const size_t a = plan_gate_grad(M, N, F, dt).total, b = plan_gate_weight(M, N, F, dt).total;
+    const size_t a = stated(plan_gate_grad(M, N, F, dt)), b = stated(plan_gate_weight(M, N, F, dt));
     return a > b ? a : b;
 }
 

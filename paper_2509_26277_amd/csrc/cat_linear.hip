@@ -163,6 +163,7 @@ Plan plan(GemmKind kind, int64_t m, int64_t n, int64_t k, int64_t rows_q, int64_
         at += up256((size_t)pl.sum_parts * 2 * n * 4);
     }
     pl.total = at > 256 ? at : 256;
+    pl.writes = at > 0;
     return pl;
 }
 

@@ -48,7 +48,7 @@ int64_t tail8(bool gated, int64_t M, int64_t N, int64_t K) { return tail_rows(ga
 Plan plan8(bool gated, int64_t M, int64_t N, int64_t K, int64_t ldx, int64_t ldw) {
     return plan(gated ? kGated : kForward, M, N, K, M, ldx, gated ? 2 * N : N, K % 16 ? K : ldw, 1, false);
 }
-size_t workspace8(bool gated, int64_t M, int64_t N, int64_t K) { return plan8(gated, M - tail8(gated, M, N, K), N, K, K, K).total; }
+size_t workspace8(bool gated, int64_t M, int64_t N, int64_t K) { return stated(plan8(gated, M - tail8(gated, M, N, K), N, K, K, K)); }
 
 template <typename T, bool GATED>
 cat_status product8(const Plan& pl, const int8_t* x, int64_t ldx, const int8_t* w, int64_t ldw, int64_t M, int64_t N, int64_t K, const Epilogue& e, char* ws,

@@ -15,9 +15,13 @@ struct Plan {
     int64_t ldq, ldp;          // row lengths of the operands as the kernel reads them
     bool lay_q, lay_p;         // laid out anew in the workspace
     size_t at_q, at_p, at_parts, at_sums, total;
+    bool writes;               // to the workspace at all
     int sum_parts;
     int64_t sum_rows;
 };
+// The size that a call states.  256 bytes mean that nothing is written there, so that all calls, on whatever streams, may be given the
+// same 256: one that does write, be it less, states more.
+inline size_t stated(const Plan& pl) { return pl.writes && pl.total <= 256 ? 512 : pl.total; }
 // q: rows_q x cols_q, p: rows_p x cols_p as they lie in memory, entries of so many bytes; out is m x n, contracted over k.
 // pack: out's checkpoint is written (of a gated product: small tiles leave that to the joining kernel)
 Plan plan(GemmKind kind, int64_t m, int64_t n, int64_t k, int64_t rows_q, int64_t cols_q, int64_t rows_p, int64_t cols_p, int entry, bool from_codes,

@@ -163,6 +163,14 @@ def test_sizes_of_workspace(lib):
     for M, N, K in [(0, 1, 1), (1, 8192, 2048), (4096, 1000, 512), (16384, 4096, 2048)]:
         for n in [i(M, N, K), g(M, N, K)] + [h(M, N, K, dt) for h in (f, b) for dt in (0, 1)]:
             assert n > 0 and n % 256 == 0
+    # 256 bytes are stated where nothing is written (all calls may share them): a call that writes there, be it less, states more
+    assert i(1, 8192, 2048) == 256 and g(1, 4096, 2048) == 256 and i(4096, 1024, 512) == 256
+    for M in (1, 4, 100, 300):
+        for N in (1, 8, 16):
+            assert all(f(M, N, 8, dt) > 256 and b(M, 8, N, dt) > 256 for dt in (0, 1))  # a checkpoint's sums, sums over rows
+            assert i(M, N, 1030) == 256 or i(M, N, 1030) > 256 and M > 64  # (laid out anew)
+    for M, N, K in [(1, 1, 131071), (1, 2, 8192), (4, 16, 8192)]:  # shares of k of few rows: 4 bytes of sums and more
+        assert i(M, N, K) > 256 and g(M, N, K) > 256
     # rows that are no whole number of 16-byte groups are laid out anew
     assert i(4096, 1000, 513) >= (4096 + 1000) * 528 and g(4096, 1000, 513) >= (4096 + 2000) * 528 and f(4096, 1000, 513, 0) >= (4096 + 2000) * 516 * 4
 
