@@ -186,6 +186,45 @@ def test_nan_and_infinity_go_where_the_formula_takes_them(M, dtype):
         assert torch.equal(g[rows][:, 128:], cat_unpack8(held[0][i], held[1][i])[rows][:, 128:])
 
 
+@pytest.mark.parametrize("M,F,K", [((1 << 20) + 300, 2056, 64), ((1 << 20) + 300, 8, 2056), ((1 << 20) + 300, 2051, 24)])
+def test_more_than_two_to_the_31_entries(M, F, K):
+    """Of the result, its checkpoints and gradients, or of x and dy (more than 4 GiB of them): first and last rows against the definitions."""
+    x, w, w2 = _matrix(M, K, "bf16", 1), _matrix(2 * F, K, "bf16", 2, K ** -0.5), _matrix(K, F, "bf16", 3, K ** -0.5)
+    half, ends = half_step(x.dtype), (slice(0, 400), slice(M - 400, M))
+    y, packed = cat_gated_linear(x, w, act="relu", pack=True)
+    alone = cat_gated_linear(x, w, act="relu")
+    for rows in ends:
+        z, z_err = x[rows].double() @ w.double().t(), U32 * (K + 8) * (x[rows].double().abs() @ w.double().abs().t())
+        (g, v), (ge, ve) = z.split(F, 1), z_err.split(F, 1)
+        want = g.clamp(min=0) * v
+        bound = half * want.abs() * (1 + U32) + U32 * want.abs() + (ge * (v.abs() + ve) + g.abs() * ve) * (1 + half)
+        _close(y[rows], want, bound, "y")
+        _close(alone[rows], want, bound, "y without the checkpoint")
+        for i, (t, err) in enumerate(((g, ge), (v, ve))):
+            top, perr = _groups(t.abs(), lambda a: a.amax(2)), _groups(err, lambda a: a.amax(2))
+            step, off = ((a.repeat_interleave(128, 1)[:, :F]) for a in (top / 127, perr))
+            got = cat_unpack8(packed[0][i, rows].contiguous(), packed[1][i, rows].contiguous())
+            _close(got, t, 0.5 * step + 2 * err + 2 * off + 256 * U32 * step, "checkpoint")
+    del y, alone
+    dz, _ = cat_gated_backward_input(x, w2, packed, act="relu")
+    dy = torch.zeros_like(x)
+    for rows in ends:
+        dy[rows] = x[rows]
+    dw, _ = cat_gated_backward_weight(dy, packed, act="relu", want_bias=False)
+    want_w, size_w, err_w = 0, 0, 0
+    for rows in ends:
+        g, v = (cat_unpack8(packed[0][i, rows].contiguous(), packed[1][i, rows].contiguous()).double() for i in range(2))
+        d = x[rows].double()
+        dh, size = d @ w2.double(), d.abs() @ w2.double().abs()
+        want, e = torch.cat((dh * v * (g > 0), dh * g.clamp(min=0)), 1), U32 * (K + 8) * size
+        err = torch.cat((v.abs() * e, g.abs() * e), 1) + 3 * U32 * want.abs()
+        _close(dz[rows], want, half * want.abs() + err * (1 + half), "dz")
+        h = g.clamp(min=0) * v
+        want_w, size_w = want_w + d.t() @ h, size_w + d.abs().t() @ h.abs()
+        err_w = err_w + d.abs().t() @ (half * h.abs() + (1 + half) * U32 * h.abs())
+    _close(dw, want_w, half * want_w.abs() + U32 * (M + 8) * size_w + err_w + 1e-30, "dw")
+
+
 def test_no_rows():
     for dtype in TYPES.values():
         x, w = torch.empty(0, 33, dtype=dtype, device="cuda"), torch.ones(14, 33, dtype=dtype, device="cuda")

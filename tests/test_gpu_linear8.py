@@ -220,6 +220,24 @@ def test_activations_over_their_whole_range(M):
                 assert far[1] == 0.0 and far[3] == 0.0 and far[5] == 0.0 and far[4] == 200.0
 
 
+@pytest.mark.parametrize("M,N,K", [((1 << 22) + 300, 8, 1040), ((1 << 21) + 300, 1032, 16), ((1 << 21) + 300, 1031, 24)])
+def test_more_than_two_to_the_31_entries(M, N, K):
+    """Of x (more than 4 GiB of it), or of the result: first and last rows against the definition."""
+    g = torch.Generator(device="cuda").manual_seed(1)
+    x = torch.randint(-128, 128, (M, K), generator=g, device="cuda", dtype=torch.int8)
+    w = torch.randint(-128, 128, (2 * N, K), generator=g, device="cuda", dtype=torch.int8)
+    xs, ws = torch.rand(M, generator=g, device="cuda") / 74, torch.rand(2 * N, generator=g, device="cuda") / (74 * K ** 0.5)
+    y, h = cat_linear8(x, xs, w[:N], ws[:N], act="relu"), cat_gated_linear8(x, xs, w, ws, act="relu")
+    half = half_step(y.dtype)
+    for rows in (slice(0, 400), slice(M - 400, M)):
+        z, z_err = _product(x[rows], xs[rows], w, ws, None)
+        want, err = z[:, :N].clamp(min=0), z_err[:, :N]
+        _close(y[rows], want, half * want + err + U32 * want, "y")
+        (a, v), (ae, ve) = z.split(N, 1), z_err.split(N, 1)
+        u = a.clamp(min=0)
+        _close(h[rows], u * v, half * (u * v).abs() * (1 + U32) + U32 * (u * v).abs() + ae * (v.abs() + ve) + u * ve, "gated")
+
+
 def test_no_rows():
     x, w = torch.empty(0, 33, dtype=torch.int8, device="cuda"), torch.ones(8, 33, dtype=torch.int8, device="cuda")
     none, ws = torch.empty(0, device="cuda"), torch.ones(8, device="cuda")

@@ -120,6 +120,20 @@ def test_norm_to_8_bits(D, dtype):
         assert bool((codes.cpu().int().abs().amax(1) == 127).all() if D > 1 else True)
 
 
+@pytest.mark.parametrize("D", [2056, 2051])
+def test_more_than_two_to_the_31_entries(D):
+    """First and last rows against the definition; a row's codes through the norm do not hang on the number of rows."""
+    N = (1 << 20) + 300
+    x = torch.randn(N, D, generator=torch.Generator(device="cuda").manual_seed(1), device="cuda", dtype=torch.bfloat16)
+    codes, scales = cat_quantize_rows(x)
+    norm_codes, norm_scales = cat_layer_norm_quantize(x)
+    for rows in (slice(0, 100), slice(N - 100, N)):
+        want_c, want_s = _reference(x[rows])
+        assert torch.equal(scales[rows].cpu(), want_s) and torch.equal(codes[rows].cpu(), want_c)
+        c, s = cat_layer_norm_quantize(x[rows].contiguous())
+        assert torch.equal(norm_codes[rows], c) and torch.equal(norm_scales[rows], s)
+
+
 def test_no_rows():
     for call in (cat_quantize_rows, cat_layer_norm_quantize):
         codes, scales = call(torch.empty(0, 33, device="cuda"))
