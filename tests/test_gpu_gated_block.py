@@ -124,11 +124,10 @@ def _step(x, dy, p, q):
     return [y, dx, *grads.values(), block_forward8(x, q, act="silu")]
 
 
-@pytest.mark.parametrize("M", [40, 300])
-def test_on_a_stream_and_in_graphs(M):
+@pytest.mark.parametrize("M,D,F", [(40, 96, 200), (300, 96, 200), (1, 33, 7), (131, 131, 1027), (2100, 131, 1027)])
+def test_on_a_stream_and_in_graphs(M, D, F):
     """On a stream of its own, and in two graphs captured one after the other, replayed in turn with eager work between: every replay,
     on new inputs, gives the eager calls' bits."""
-    D, F = 96, 200
     p, g = _params(D, F, torch.bfloat16, 3, True)
     q = quantize_block(p)
     inputs = [[torch.randn(M, D, generator=g).bfloat16().cuda() for _ in range(2)] for _ in range(2)]
