@@ -683,7 +683,8 @@ cat_status cat_activation_backward(const void *dy, const int8_t *codes, const fl
  *               dh * act(g), g and v from the checkpoints; dbias (2F floats, nullable): the sums over rows of dz, before its
  *               rounding to dt.
  * cat_gated_backward_weight  dw = dy^T (act(g) * v) (N x F of dt), dbias = sum over rows of dy (N floats, nullable).  With bfloat16
- *               rows act(g) * v is rounded to bfloat16, as cat_linear_backward_weight has it.
+ *               rows the product takes act(g) * v in two bfloat16 terms (16 bits of it and more), unlike the act(c) of
+ *               cat_linear_backward_weight: the result's rounding is the only one to 8 bits.
  * One size of workspace covers both gradients, and cat_gated_linear with and without checkpoints; F is below 2^23 bytes of dt.
  * CAT_ERR_UNSUPPORTED also for K of more than 131071 8-bit integers. */
 cat_status cat_quantize_rows(const void *x, int64_t N, int64_t D, cat_dtype dt, int8_t *codes, int64_t ld, float *scales,

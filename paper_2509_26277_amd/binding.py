@@ -1079,8 +1079,8 @@ def cat_gated_backward_input(dy, w, packed, act="silu", want_bias=True, out=None
 
 def cat_gated_backward_weight(dy, packed, act="silu", want_bias=True, out=None, workspace=None):
     """Gradients of the weight and bias of the product that takes act(g) * v (cat_gated_backward_weight), from the checkpoints of g
-    and v.  Returns (dw, dbias): dw (N x F) of dy's type, dbias float32, None without ``want_bias``.  Rounding of act(g) * v as in
-    cat_linear_backward_weight."""
+    and v.  Returns (dw, dbias): dw (N x F) of dy's type, dbias float32, None without ``want_bias``.  Of bfloat16 rows, too, act(g) * v is
+    not rounded to bfloat16 on the way (two products of bfloat16 terms)."""
     lib = load_library()
     M, N, dt = _rows(dy, "dy")
     here = _here(dy, "dy")

@@ -4,7 +4,7 @@
 //   g = x Wg^T + bg, v = x Wv^T + bv, h = act(g) * v      w = [Wg; Wv]; 4 M F K operations; reads x, w, writes h (and codes of g, v)
 //   dh = dy W2, dz = [dh v act'(g) | dh act(g)]           W2: N x F; 2 M N F; reads dy, W2, the codes, writes dz
 //   db = sum over rows of dz                              from the fp32 values on their way out
-//   dW2 = dy^T (act(g) * v), db2 = sum over rows of dy    2 M N F
+//   dW2 = dy^T (act(g) * v), db2 = sum over rows of dy    2 M N F (bfloat16: twice, act(g) * v being two terms)
 //
 // A wave of the tile kernel works on 64 columns of the gate and the same 64 of the value, so that both meet in a lane's registers:
 // neither projection, nor dh, goes to memory.
@@ -66,7 +66,7 @@ __global__ __launch_bounds__(256) void k_join_gate_grad(const float* __restrict_
 
 Plan plan_gated(int64_t M, int64_t F, int64_t K, cat_dtype dt, bool pack) { return plan(kGated, M, F, K, M, K, 2 * F, K, entry_bytes(dt), false, pack); }
 Plan plan_gate_grad(int64_t M, int64_t N, int64_t F, cat_dtype dt) { return plan(kGatedGrad, M, F, N, M, N, N, F, entry_bytes(dt), false); }
-Plan plan_gate_weight(int64_t M, int64_t N, int64_t F, cat_dtype dt) { return plan(kWeightGrad, N, F, M, M, N, M, F, entry_bytes(dt), true); }
+Plan plan_gate_weight(int64_t M, int64_t N, int64_t F, cat_dtype dt) { return plan(kWeightGrad, N, F, M, M, N, M, F, entry_bytes(dt), true, false, true); }
 
 cat_status check_gate(const char* who, int64_t M, const int8_t* codes, const float* scales) {
     CAT_TRY(check_ptr(who, "codes", codes, M > 0));

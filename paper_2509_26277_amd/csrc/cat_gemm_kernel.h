@@ -673,7 +673,10 @@ __global__ __launch_bounds__((TM / WM) * (TN / 128) * 64, 2) void k_gemm(const G
     if (a.splits > 1) share_of_k = t / tiles, t -= share_of_k * tiles, end = t + 1, stride = 1;  // (a tile each)
     const auto place = [&](uint32_t tile, uint32_t& m0, uint32_t& n0) { tile_place(tile, tm, tn, m0, n0); };
 
-    const int64_t k0 = (int64_t)share_of_k * a.k_split, k_all = a.k - k0 < a.k_split ? a.k - k0 : a.k_split;
+    // (a weight gradient's p in two terms: the shares of the second one stand behind the first's)
+    const uint32_t term = KIND == kWeightGrad && a.splits > a.k_shares ? share_of_k / (uint32_t)a.k_shares : 0;
+    const void* const p = KIND == kWeightGrad ? (const char*)a.p + term * a.p_bytes : a.p;
+    const int64_t k0 = (int64_t)(share_of_k - term * (uint32_t)a.k_shares) * a.k_split, k_all = a.k - k0 < a.k_split ? a.k - k0 : a.k_split;
     Stage<E, PT, true, TN, W> sp;
     Stage<E, QT, false, TM, W> sq;
     Fragments<E, PT, true, TN> fp;
@@ -699,14 +702,14 @@ __global__ __launch_bounds__((TM / WM) * (TN / 128) * 64, 2) void k_gemm(const G
     uint32_t tile_m, tile_n;
     place(t, tile_m, tile_n);
     int ahead = steps;
-    sp.tile(a.p, a.p_bytes, first_p(tile_n), k0, sp.base, sp.left);
+    sp.tile(p, a.p_bytes, first_p(tile_n), k0, sp.base, sp.left);
     sq.tile(a.q, a.q_bytes, (int64_t)tile_m * TM, k0, sq.base, sq.left);
     const char *next_p, *next_q;
     int64_t next_p_left, next_q_left;
     const auto look_ahead = [&](uint32_t next) {
         uint32_t next_m, next_n;
         place(next < end ? next : t, next_m, next_n);
-        sp.tile(a.p, a.p_bytes, first_p(next_n), k0, next_p, next_p_left);
+        sp.tile(p, a.p_bytes, first_p(next_n), k0, next_p, next_p_left);
         sq.tile(a.q, a.q_bytes, (int64_t)next_m * TM, k0, next_q, next_q_left);
     };
     const auto begin = [&] {
@@ -775,9 +778,9 @@ __global__ __launch_bounds__((TM / WM) * (TN / 128) * 64, 2) void k_gemm(const G
         // A step's second half is read while the first is multiplied, and the next step's first half while the second half's last
         // rows are: the wait for the next step's loads, and for the waves that still read this one's, stands before those rows, and
         // the loads of the step after it follow, one by one between the products.
-        const auto multiply_rows = [&](const f32x4(&p)[NT], const f32x4(&q)[MT], int from, int to) {  // products from .. to - 1
+        const auto multiply_rows = [&](const f32x4(&pf)[NT], const f32x4(&qf)[MT], int from, int to) {  // products from .. to - 1
 #pragma unroll
-            for (int i = from; i < to; i++) sums[i / NT][i % NT] = multiply<E>(p[i % NT], q[i / NT], sums[i / NT][i % NT]);
+            for (int i = from; i < to; i++) sums[i / NT][i % NT] = multiply<E>(pf[i % NT], qf[i / NT], sums[i / NT][i % NT]);
         };
         f32x4 p0[NT], q0[MT], p1[NT], q1[MT];
         fp.template read<0>(lds + cur, p0);

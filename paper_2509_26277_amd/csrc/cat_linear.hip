@@ -96,8 +96,9 @@ int64_t tail_rows(GemmKind kind, int64_t m, int64_t n, int64_t k, int entry) {
 // 8192 x 2048 bfloat16, gated, not: 17.8 and 21.1).
 constexpr int64_t kFewWideBytes = 1 << 24, kFewMostBytes = 1 << 26;
 Plan plan(GemmKind kind, int64_t m, int64_t n, int64_t k, int64_t rows_q, int64_t cols_q, int64_t rows_p, int64_t cols_p, int entry, bool from_codes,
-          bool pack) {
+          bool pack, bool gated) {
     Plan pl = {};
+    pl.terms = gated && entry == 2 ? 2 : 1;
     const int64_t step = 128 / entry;
     const int64_t bytes_w = rows_p * k * entry;  // (however far apart its rows lie: the sizes of workspace know nothing of that)
     const bool own = kind == kForward && entry > 1;  // (the products of the block's training step: as they were)
@@ -118,18 +119,20 @@ Plan plan(GemmKind kind, int64_t m, int64_t n, int64_t k, int64_t rows_q, int64_
         pl.lay_p = from_codes || cols_p != whole(cols_p, entry);
         if (pl.lay_q) pl.ldq = whole_lines(cols_q, entry);
         if (pl.lay_p) pl.ldp = whole_lines(cols_p, entry);
-        choose_tiles(kind, m, n, (k + step - 1) / step, entry, pack, pl.large, pl.splits);
+        choose_tiles(kind, m, n, (k + step - 1) / step * pl.terms, entry, pack, pl.large, pl.splits);
+        pl.splits = (pl.splits + pl.terms - 1) / pl.terms;  // (a term's)
         pl.k_split = ((k + pl.splits - 1) / pl.splits + step - 1) / step * step;
         if (pl.k_split < step) pl.k_split = step;
         pl.splits = (int)((k + pl.k_split - 1) / pl.k_split);
         if (pl.splits < 1) pl.splits = 1;
+        pl.splits *= pl.terms;
         pl.joined = pl.splits > 1 || (kind == kGated && pack && !pl.large) || (kind == kGatedGrad && n < 8);
     }
     size_t at = 0;
     pl.at_q = at;
     if (pl.lay_q) at += up256((size_t)rows_q * pl.ldq * entry);
     pl.at_p = at;
-    if (pl.lay_p) at += up256((size_t)rows_p * pl.ldp * entry);
+    if (pl.lay_p) at += up256((size_t)pl.terms * rows_p * pl.ldp * entry);
     pl.at_parts = at;
     // (few rows: the checkpoint's groups of 128 columns are found by the joining kernel, whatever the number of shares)
     if (pl.joined && kind == kWeightGrad) {

@@ -9,7 +9,7 @@ namespace cat {
 constexpr int64_t kFewRows = 64;
 struct Plan {
     bool few, wide, large;     // wide: few rows of x, 32 rows of w a workgroup
-    int splits;
+    int splits, terms;         // shares, and of how many terms of p (of both, where there are two)
     bool joined;               // the tile kernel writes its sums as they are, and the joining kernel goes on with them
     int64_t k_split;
     int64_t ldq, ldp;          // row lengths of the operands as the kernel reads them
@@ -23,9 +23,10 @@ struct Plan {
 // same 256: one that does write, be it less, states more.
 inline size_t stated(const Plan& pl) { return pl.writes && pl.total <= 256 ? 512 : pl.total; }
 // q: rows_q x cols_q, p: rows_p x cols_p as they lie in memory, entries of so many bytes; out is m x n, contracted over k.
-// pack: out's checkpoint is written (of a gated product: small tiles leave that to the joining kernel)
+// pack: out's checkpoint is written (of a gated product: small tiles leave that to the joining kernel).  gated: a weight's gradient
+// behind a gate, whose p is in two terms where it is bfloat16.
 Plan plan(GemmKind kind, int64_t m, int64_t n, int64_t k, int64_t rows_q, int64_t cols_q, int64_t rows_p, int64_t cols_p, int entry, bool from_codes,
-          bool pack = false);
+          bool pack = false, bool gated = false);
 // How many of m rows, behind the last whole tile, are better off in the kernel for few rows (forward and gated, without a checkpoint):
 // none, unless the tiles then need a round of workgroups less.
 int64_t tail_rows(GemmKind kind, int64_t m, int64_t n, int64_t k, int entry);
@@ -264,6 +265,9 @@ __global__ __launch_bounds__(256) void k_join(const float* __restrict__ parts, i
 // act(c) is rounded to bfloat16 with bfloat16 rows: the matrix cores take no wider operand at their rate (the rest as a second
 // operand is the product over again), and the forward product's rows, whose product is differentiated, were rounded so too.
 // Relative error of dw, 4096 x 1024 over 16384 rows: 2.3e-3, of which its own rounding is 1.7e-3.  Float rows keep all of it.
+// act(g) * v, of a gate's checkpoints, is not: bfloat16 operands hold it in two terms, its upper 16 bits and what is left of it, rounded, one
+// matrix behind the other, and the product is taken with both (2^-15 of a term at most; dw's error is its own rounding's, 1.66e-3, where
+// one term left 2.34e-3).  An infinity has no rest.
 template <typename T>
 struct Layout {
     const T* src;
@@ -295,6 +299,16 @@ __global__ __launch_bounds__(256) void k_lay_out(const Layout<T> first, const La
                 ld_codes<V>(a.codes + (a.rows + row) * a.cols, j, a.cols, a.scales[(a.rows + row) * G + j / kPackGroup], value);
 #pragma unroll
                 for (int e = 0; e < V; e++) v[e] *= value[e];
+                if constexpr (sizeof(T) == 2) {
+                    float rest[V];
+#pragma unroll
+                    for (int e = 0; e < V; e++) {
+                        const float upper = __uint_as_float(__float_as_uint(v[e]) & 0xFFFF0000u);
+                        rest[e] = fabsf(v[e]) < INFINITY ? v[e] - upper : 0.f;
+                        v[e] = upper;
+                    }
+                    st_group(a.dst + (a.rows + row) * a.ld + j, rest);
+                }
             }
         } else {
             ld_group_to(a.src + row * a.from, j, a.cols, v);
@@ -346,6 +360,7 @@ cat_status join(const void* parts, int splits, int64_t M, int64_t N, const Epilo
 inline GemmArgs gemm_args(const Plan& pl, int entry, const void* q, int64_t rows_q, const void* p, int64_t rows_p, int64_t m, int64_t n, int64_t k, const Epilogue& e,
                           char* ws) {
     GemmArgs a = {};
+    a.k_shares = pl.splits / pl.terms;
     a.q = q, a.p = p, a.ldq = pl.ldq, a.ldp = pl.ldp;
     a.q_bytes = rows_q * pl.ldq * entry, a.p_bytes = rows_p * pl.ldp * entry;
     a.m = m, a.n = n, a.k = k, a.k_split = pl.k_split, a.splits = pl.splits, a.parts = pl.joined ? ws + pl.at_parts : nullptr, a.e = e;
@@ -383,7 +398,7 @@ cat_status few_tail(const void* x, int64_t ldx, const void* w, int64_t ldw, int6
     if (e.residual) e.residual = (const T*)e.residual + m0 * N;
     if (e.row_scales) e.row_scales += m0;
     Plan pl = {};
-    pl.splits = 1, pl.k_split = K;
+    pl.splits = pl.terms = 1, pl.k_split = K;
     return few_rows<E, T, GATED>(pl, (const E*)x + m0 * ldx, ldx, w, ldw, tail, N, K, e, nullptr, st);
 }
 
