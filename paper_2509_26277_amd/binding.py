@@ -925,8 +925,10 @@ _unused = {}
 
 def _room(here, workspace, nbytes, device):
     """The caller's workspace, or one of the stated size.  256 bytes are what a call asks for that uses none: those are kept (1.4 us
-    of the 20 of a row through both of a token's calls)."""
+    of the 20 of a row through both of a token's calls).  A size of 0 is that of a call that will be refused: it gets nothing."""
     if workspace is None:
+        if nbytes == 0:
+            return torch.empty(0, dtype=torch.uint8, device=device)
         if nbytes > 256:
             return _workspace(nbytes, device)
         if here not in _unused:

@@ -48,7 +48,11 @@ int64_t tail8(bool gated, int64_t M, int64_t N, int64_t K) { return tail_rows(ga
 Plan plan8(bool gated, int64_t M, int64_t N, int64_t K, int64_t ldx, int64_t ldw) {
     return plan(gated ? kGated : kForward, M, N, K, M, ldx, gated ? 2 * N : N, K % 16 ? K : ldw, 1, false);
 }
-size_t workspace8(bool gated, int64_t M, int64_t N, int64_t K) { return stated(plan8(gated, M - tail8(gated, M, N, K), N, K, K, K)); }
+// (whatever the result's type: of bfloat16, rows of out may be the longest)
+size_t workspace8(const char* who, bool gated, int64_t M, int64_t N, int64_t K) {
+    if (check8(who, M, N, K, CAT_BF16, 0) != CAT_OK) return 0;
+    return stated(plan8(gated, M - tail8(gated, M, N, K), N, K, K, K));
+}
 
 template <typename T, bool GATED>
 cat_status product8(const Plan& pl, const int8_t* x, int64_t ldx, const int8_t* w, int64_t ldw, int64_t M, int64_t N, int64_t K, const Epilogue& e, char* ws,
@@ -104,7 +108,7 @@ using namespace cat;
 extern "C" {
 
 size_t cat_linear8_workspace_bytes(int64_t M, int64_t N, int64_t K) {
-    return check8("cat_linear8_workspace_bytes", M, N, K, CAT_F32, 0) == CAT_OK ? workspace8(false, M, N, K) : 0;
+    return workspace8("cat_linear8_workspace_bytes", false, M, N, K);
 }
 cat_status cat_linear8(const int8_t* x, int64_t ldx, const float* x_scales, const int8_t* w, int64_t ldw, const float* w_scales, const float* bias, const void* residual, int64_t M,
                        int64_t N, int64_t K, cat_dtype dt, cat_activation act, void* y, void* workspace, size_t workspace_bytes, void* hip_stream) {
@@ -112,7 +116,7 @@ cat_status cat_linear8(const int8_t* x, int64_t ldx, const float* x_scales, cons
 }
 
 size_t cat_gated_linear8_workspace_bytes(int64_t M, int64_t F, int64_t K) {
-    return check8("cat_gated_linear8_workspace_bytes", M, F, K, CAT_F32, 0) == CAT_OK ? workspace8(true, M, F, K) : 0;
+    return workspace8("cat_gated_linear8_workspace_bytes", true, M, F, K);
 }
 cat_status cat_gated_linear8(const int8_t* x, int64_t ldx, const float* x_scales, const int8_t* w, int64_t ldw, const float* w_scales, const float* bias, int64_t M, int64_t F,
                              int64_t K, cat_dtype dt, cat_activation act, void* y, void* workspace, size_t workspace_bytes, void* hip_stream) {
