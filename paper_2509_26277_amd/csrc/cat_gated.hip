@@ -66,7 +66,9 @@ __global__ __launch_bounds__(256) void k_join_gate_grad(const float* __restrict_
 
 Plan plan_gated(int64_t M, int64_t F, int64_t K, cat_dtype dt, bool pack) { return plan(kGated, M, F, K, M, K, 2 * F, K, entry_bytes(dt), false, pack); }
 Plan plan_gate_grad(int64_t M, int64_t N, int64_t F, cat_dtype dt) { return plan(kGatedGrad, M, F, N, M, N, N, F, entry_bytes(dt), false); }
-Plan plan_gate_weight(int64_t M, int64_t N, int64_t F, cat_dtype dt) { return plan(kWeightGrad, N, F, M, M, N, M, F, entry_bytes(dt), true, false, true); }
+Plan plan_gate_weight(int64_t M, int64_t N, int64_t F, cat_dtype dt) {
+    return plan(kWeightGrad, N, F, M, M, N, M, F, entry_bytes(dt), true, false, dt == CAT_BF16 ? 2 : 1, true);
+}
 
 cat_status check_gate(const char* who, int64_t M, const int8_t* codes, const float* scales) {
     CAT_TRY(check_ptr(who, "codes", codes, M > 0));

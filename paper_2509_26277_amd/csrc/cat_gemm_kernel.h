@@ -825,7 +825,7 @@ __global__ __launch_bounds__((TM / WM) * (TN / 128) * 64, 2) void k_gemm(const G
         asm volatile("" : "+v"(lane_end));
         const int r = lane_end & 15, g = lane_end >> 4;
         const int64_t nw = n0 + wn * WO, nl = nw + 8 * g;  // the wave's first column; this lane's of pair t: nl + 32 t (gated: t & 1)
-        if (KIND == kWeightGrad && a.parts) {  // 1 KB a store of a wave (us, 1024 x 4096 over 16384 rows: 158 with pieces of 16 bytes of rows, 140 so)
+        if (KIND == kWeightGrad && a.tiled) {  // 1 KB a store of a wave (us, 1024 x 4096 over 16384 rows: 158 with pieces of 16 bytes of rows, 140 so)
             float* part = (float*)a.parts + (((int64_t)share_of_k * tiles + t) * (TM * TN) + wave * (WM * WN)) + lane_end * 4;
 #pragma unroll
             for (int i = 0; i < MT * NT; i++) *(Sums<E>*)(part + i * 256) = sums[i / NT][i % NT];

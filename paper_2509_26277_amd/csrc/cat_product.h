@@ -10,7 +10,7 @@ constexpr int64_t kFewRows = 64;
 struct Plan {
     bool few, wide, large;     // wide: few rows of x, 32 rows of w a workgroup
     int splits, terms;         // shares, and of how many terms of p (of both, where there are two)
-    bool joined;               // the tile kernel writes its sums as they are, and the joining kernel goes on with them
+    bool joined, tiled;        // the tile kernel writes its sums as they are, and the joining kernel goes on with them; tile by tile
     int64_t k_split;
     int64_t ldq, ldp;          // row lengths of the operands as the kernel reads them
     bool lay_q, lay_p;         // laid out anew in the workspace
@@ -23,10 +23,10 @@ struct Plan {
 // same 256: one that does write, be it less, states more.
 inline size_t stated(const Plan& pl) { return pl.writes && pl.total <= 256 ? 512 : pl.total; }
 // q: rows_q x cols_q, p: rows_p x cols_p as they lie in memory, entries of so many bytes; out is m x n, contracted over k.
-// pack: out's checkpoint is written (of a gated product: small tiles leave that to the joining kernel).  gated: a weight's gradient
-// behind a gate, whose p is in two terms where it is bfloat16.
+// pack: out's checkpoint is written (of a gated product: small tiles leave that to the joining kernel).  terms: of p, of a weight's
+// gradient.  tiled: a weight's gradient may take the memory of whole tiles for its shares.
 Plan plan(GemmKind kind, int64_t m, int64_t n, int64_t k, int64_t rows_q, int64_t cols_q, int64_t rows_p, int64_t cols_p, int entry, bool from_codes,
-          bool pack = false, bool gated = false);
+          bool pack = false, int terms = 1, bool tiled = false);
 // How many of m rows, behind the last whole tile, are better off in the kernel for few rows (forward and gated, without a checkpoint):
 // none, unless the tiles then need a round of workgroups less.
 int64_t tail_rows(GemmKind kind, int64_t m, int64_t n, int64_t k, int entry);
@@ -363,7 +363,7 @@ inline GemmArgs gemm_args(const Plan& pl, int entry, const void* q, int64_t rows
     a.k_shares = pl.splits / pl.terms;
     a.q = q, a.p = p, a.ldq = pl.ldq, a.ldp = pl.ldp;
     a.q_bytes = rows_q * pl.ldq * entry, a.p_bytes = rows_p * pl.ldp * entry;
-    a.m = m, a.n = n, a.k = k, a.k_split = pl.k_split, a.splits = pl.splits, a.parts = pl.joined ? ws + pl.at_parts : nullptr, a.e = e;
+    a.m = m, a.n = n, a.k = k, a.k_split = pl.k_split, a.splits = pl.splits, a.parts = pl.joined ? ws + pl.at_parts : nullptr, a.tiled = pl.tiled, a.e = e;
     return a;
 }
 
