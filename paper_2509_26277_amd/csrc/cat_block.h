@@ -248,17 +248,20 @@ __device__ __forceinline__ float tail_factor(float x) {
     return t * g;
 }
 __device__ __forceinline__ float normal_exp(float z) { return __builtin_amdgcn_exp2f(z * z * -0.72134752044448170f); }
-// The tail by itself, Phi(-x) = 2^P(x): P a polynomial of degree 7, fitted so that x 2^P(x) is off by 2.4e-7 at most, and 2^P(x) by 4.4e-5
-// of its value up to x = 7 (behind that Phi is below 2e-12, and P falls on).  14 instructions' time for GELU where exponential, reciprocal
-// and tail_factor take 24 (us, 16384 x 8192 over 2048 8-bit integers: 285 -> 264).
-__device__ __forceinline__ float tail(float x) {
-    float p = fmaf(x, -1.592344006e-6f, 5.686387885e-5f);
-    p = fmaf(x, p, -8.961785352e-4f);
-    p = fmaf(x, p, 8.394782431e-3f);
-    p = fmaf(x, p, -5.379608646e-2f);
-    p = fmaf(x, p, -4.58545059e-1f);
-    p = fmaf(x, p, -1.151258111f);
-    return __builtin_amdgcn_exp2f(fmaf(x, p, -9.999888539e-1f));
+// The tail by itself, 2^32 Phi(-x) = 2^(P(x) + 32): P a polynomial of degree 9 for log2 Phi(-x) over [0, 13.3] (behind that the result is below
+// the smallest float, and P falls on), fitted so that x 2^P(x) is off by 3.0e-7 at most and 2^P(x) by 3.8e-5 of its value; the roundings of its
+// evaluation add 5.2e-5 at most, so that a bfloat16 result is right to 1.03 half steps wherever it is not below the smallest normal number.  (2^32:
+// the hardware's exponential gives 0 below 2^-126, where x Phi(-x) is still above.)
+__device__ __forceinline__ float tail32(float x) {
+    float p = fmaf(x, -2.10506601e-9f, 1.52080861e-7f);
+    p = fmaf(x, p, -4.81919572e-6f);
+    p = fmaf(x, p, 8.87049865e-5f);
+    p = fmaf(x, p, -1.06312655e-3f);
+    p = fmaf(x, p, 8.87474187e-3f);
+    p = fmaf(x, p, -5.45356521e-2f);
+    p = fmaf(x, p, -4.57971281e-1f);
+    p = fmaf(x, p, -1.15145381f);
+    return __builtin_amdgcn_exp2f(fmaf(x, p, 31.000031949f));
 }
 template <int ACT, int FAST>
 __device__ __forceinline__ float act_value(float z) {
@@ -266,7 +269,7 @@ __device__ __forceinline__ float act_value(float z) {
         return z > 0.f ? z : (z != z ? z : 0.f);
     } else if constexpr (ACT == CAT_ACT_GELU && FAST == 2) {  // (as below; minimum and maximum hand a NaN on)
         const float x = fabsf(__builtin_elementwise_minimum(z, 1e30f));
-        return fmaf(-x, tail(x), __builtin_elementwise_maximum(z, 0.f));
+        return fmaf(x * -0x1p-32f, tail32(x), __builtin_elementwise_maximum(z, 0.f));
     } else if constexpr (ACT == CAT_ACT_GELU && kHalf<FAST>) {  // z - z Phi(-z), or z Phi(z)
         const float x = fabsf(fminf(z, 1e30f));           // (no inf * 0 for +inf)
         return fmaf(-x, normal_exp(z) * tail_factor(x), fmaxf(z, 0.f));
