@@ -315,9 +315,18 @@ __device__ __forceinline__ void act_both(float z, float& value, float& grad) {
         value = fmaf(-x, e * g, fmaxf(z, 0.f));
         grad = z > 0.f ? 1.f - s : s;
     } else if constexpr (ACT == CAT_ACT_GELU_TANH) {
-        const float p = logistic<kTanh<FAST>>(tanh_arg2(z)), c = fminf(fmaxf(z, -32.f), 32.f);
+        float p, q;  // q = 1 - p
+        if constexpr (FAST == 3) {  // (as e / (1 + e): 1 - p itself loses the places that p near 1 has not)
+            const float e = __expf(-tanh_arg2(z));
+            p = __builtin_amdgcn_rcpf(1.f + e);
+            q = e < 0x1p100f ? e * p : 1.f;
+        } else {
+            p = logistic<kTanh<FAST>>(tanh_arg2(z));
+            q = 1.f - p;
+        }
+        const float c = fminf(fmaxf(z, -32.f), 32.f);
         value = z * p;
-        grad = fmaf(c * p * (1.f - p), 2.f * kTanhIn * fmaf(3.f * kTanhCube * c, c, 1.f), p);
+        grad = fmaf(c * p * q, 2.f * kTanhIn * fmaf(3.f * kTanhCube * c, c, 1.f), p);
     } else {
         value = act_value<ACT, FAST>(z);
         grad = act_grad<ACT, FAST>(z);
