@@ -670,8 +670,10 @@ cat_status cat_activation_backward(const void *dy, const int8_t *codes, const fl
  *               through it once, its rows being output channels.
  *               ld >= D: entries from a row of codes to the next; what lies between is left as it was.
  * cat_layer_norm_quantize  the same of cat_layer_norm's y, before its rounding to dt.
- * cat_linear8   z = (sum over k of x w) * x_scales * w_scales + bias, y = act(z) + residual (M x N of dt, nullable).  x: M x K, w:
- *               N x K, any 8-bit integers (-128 too); the sums are exact, K at most 131071; x_scales: M floats, w_scales: N.
+ * cat_linear8   z = (sum over k of x w) * (x_scales * w_scales) + bias, y = act(z) + residual (M x N of dt, nullable).  x: M x K, w:
+ *               N x K, any 8-bit integers (-128 too); the sums are exact, K at most 131071; x_scales: M floats, w_scales: N,
+ *               whose products are rounded to float first: one that is neither 0 nor from 2^-126 to below 2^128 leaves z without
+ *               a float's precision (an infinity times a sum of 0 is a NaN).
  *               ldx, ldw: entries from a row of x, of w, to the next: K, or a larger multiple of 16, in which case the last row may be
  *               read up to the next multiple of 16 too.  What lies behind K does not count.  Where K is no multiple of 16, w is laid
  *               out anew in the workspace, and x unless ldx is one: rows that cat_quantize_rows left 16 bytes' multiples apart are not.

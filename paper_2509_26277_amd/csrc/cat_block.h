@@ -251,7 +251,9 @@ __device__ __forceinline__ float normal_exp(float z) { return __builtin_amdgcn_e
 // The tail by itself, 2^32 Phi(-x) = 2^(P(x) + 32): P a polynomial of degree 9 for log2 Phi(-x) over [0, 13.3] (behind that the result is below
 // the smallest float, and P falls on), fitted so that x 2^P(x) is off by 3.0e-7 at most and 2^P(x) by 3.8e-5 of its value; the roundings of its
 // evaluation add 5.2e-5 at most, so that a bfloat16 result is right to 1.03 half steps wherever it is not below the smallest normal number.  (2^32:
-// the hardware's exponential gives 0 below 2^-126, where x Phi(-x) is still above.)
+// the hardware's exponential gives 0 below 2^-126, where x Phi(-x) is still above.)  (us,
+// 8-bit integers with GELU: 65536 x 2048 over 512 135, 127 with a fit of degree 7 that holds to 8 alone; 16384 x 8192 over 2048 266 and 253, 285 with
+// exponential, reciprocal and tail_factor.)
 __device__ __forceinline__ float tail32(float x) {
     float p = fmaf(x, -2.10506601e-9f, 1.52080861e-7f);
     p = fmaf(x, p, -4.81919572e-6f);

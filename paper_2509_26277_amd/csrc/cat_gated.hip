@@ -10,8 +10,8 @@
 // neither projection, nor dh, goes to memory.
 //
 // The products bound them and, on top, what a tile's end reads and writes (us, bfloat16: 16384 x 2 x 4096 over 1024 212, with checkpoints 270;
-// both gradients of 16384 x 4096 over 1024 203, where the products alone take 117; dW2 of the same 122, its shares' join 13, act(g) * v laid
-// out 54; float, 8192 x 1000 over 256: 52, and 38, 7, 12).
+// both gradients of 16384 x 4096 over 1024 203, where the products alone take 117; dW2 of the same, both terms, 233, its shares' join 13, act(g) * v
+// laid out 70; float, 8192 x 1000 over 256: 52, and 38, 7, 12).
 #include "cat_product.h"
 
 namespace cat {

@@ -19,7 +19,7 @@
 // 16384 x 8192 over 2048 with GELU, at 2.0 GHz; what comes on top of the steps is the epilogue, whose instructions they wait for:
 // GELU 21 us of 16384 x 4096 over 1024 (126 without), codes 14, a derivative 40 (121 without).  (Through LDS, 16 rows at a time, a tile's epilogue took 11 to
 // 27 us, as long as 8 to 16 steps of k.)
-// 8-bit integers (TOP/s; the library 2050 at 8192^3): 8192^3 2270 to 2510, gated 2730; 16384 x 8192 over 2048 2300, with GELU 2140.  Gated bfloat16
+// 8-bit integers (TOP/s; the library 2050 at 8192^3): 8192^3 2270 to 2510, gated 2730; 16384 x 8192 over 2048 2300, with GELU 2060.  Gated bfloat16
 // 8192 x 2 x 4096 over 8192 1450 to 1490, checkpoints 4 % more time; 16384 x 2 x 4096 over 1024 212 us, with checkpoints 255 to 270.
 #pragma once
 #include "cat_gemm.h"

@@ -7,8 +7,8 @@
 // The tile kernel and the one for few rows are those of the other products: 16 integers fill the registers of 8 bfloat16 entries and
 // a matrix instruction takes the same time over twice as many, so a step of 128 bytes is 128 entries of k.
 //
-// With many rows the matrix cores bound it and, where k is short, the tiles' ends (us: 16384 x 8192 over 2048 to bfloat16 235, with GELU 257;
-// 65536 x 2048 over 512 with GELU 120; 65536 x 1000 over 512 to float 68; gated 16384 x 2 x 4096 over 2048 224); with few the bytes of w
+// With many rows the matrix cores bound it and, where k is short, the tiles' ends (us: 16384 x 8192 over 2048 to bfloat16 235, with GELU 267;
+// 65536 x 2048 over 512 with GELU 135; 65536 x 1000 over 512 to float 68; gated 16384 x 2 x 4096 over 2048 224); with few the bytes of w
 // (8192 x 2048, one row 5.8; gated 2 x 8192 x 2048 8.5).
 #include "cat_product.h"
 
