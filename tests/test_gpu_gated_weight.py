@@ -54,3 +54,13 @@ def test_infinities_and_the_largest_values(M):
     assert bool((got[:, 128] - want).abs().max() <= 2.0 ** -8 * want)
     got[:, 0] = got[:, 128] = 0.0
     assert not bool(got.any())
+
+
+def test_a_nan_stays_in_the_columns_of_its_group():
+    packed, _ = _held(300, 384, "bf16", 7)
+    dy = _matrix(300, 40, "bf16", 5)
+    clean, _ = cat_gated_backward_weight(dy, packed, act="silu")
+    packed[1][0, 17, 1] = float("nan")  # the scale of a row's channels 128 .. 255
+    dw, db = cat_gated_backward_weight(dy, packed, act="silu")
+    assert bool(torch.isnan(dw[:, 128:256]).all()) and bool(torch.isfinite(db).all())
+    assert torch.equal(dw[:, :128], clean[:, :128]) and torch.equal(dw[:, 256:], clean[:, 256:])
