@@ -61,7 +61,7 @@ cat_status product8(const Plan& pl, const int8_t* x, int64_t ldx, const int8_t* 
     if (pl.few) return few_rows<int8_t, T, GATED>(pl, x, ldx, w, ldw, M, N, K, e, ws, st);
     const int64_t rows_w = GATED ? 2 * N : N;
     Layout<int8_t> lq = layout_of<int8_t>(x, nullptr, nullptr, M, K, pl.ldq, ws + pl.at_q), lp = layout_of<int8_t>(w, nullptr, nullptr, rows_w, K, pl.ldp, ws + pl.at_p);
-    lq.from = ldx, lp.from = ldw;
+    lq.from = (int)ldx, lp.from = (int)ldw;
     if (pl.lay_p) {  // (and x with it, or not)
         const Layout<int8_t> none = {};
         hipLaunchKernelGGL(k_lay_out8, dim3(lp.blocks + (pl.lay_q ? lq.blocks : 0)), dim3(256), 0, st, lp, pl.lay_q ? lq : none);

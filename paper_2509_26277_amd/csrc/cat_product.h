@@ -273,7 +273,8 @@ struct Layout {
     const T* src;
     const int8_t* codes;  // instead of src: a checkpoint, through act; gated: times the one behind it
     const float* scales;
-    int64_t rows, cols, from, ld;  // from, ld: from a row of src, of dst, to the next
+    int64_t rows, cols;
+    int from, ld;  // from a row of src, of dst, to the next (rows are below kGemmMaxRowBytes; 64 bytes in all, a line of the arguments each)
     T* dst;
     unsigned blocks;
 };
@@ -318,7 +319,8 @@ __global__ __launch_bounds__(256) void k_lay_out(const Layout<T> first, const La
 }
 template <typename T>
 Layout<T> layout_of(const void* src, const int8_t* codes, const float* scales, int64_t rows, int64_t cols, int64_t ld, void* dst) {
-    return {(const T*)src, codes, scales, rows, cols, cols, ld, (T*)dst, blocks_of(rows * (ld / kVec<T>))};
+    static_assert(sizeof(Layout<T>) == 64, "");
+    return {(const T*)src, codes, scales, rows, cols, (int)cols, (int)ld, (T*)dst, blocks_of(rows * (ld / kVec<T>))};
 }
 // q and p as the plan has them, those that lie otherwise; p from a checkpoint if codes are given
 template <typename T>
