@@ -50,7 +50,7 @@ struct GemmArgs {
     int64_t p_bytes, q_bytes;  // what may be read from p (of a term), q on
     int64_t m, n, k;
     int64_t k_split;  // entries of k a share takes (a multiple of the kernel's step)
-    int splits, k_shares;  // all shares, and those of k: where p has two terms, rounded and rest, one behind the other, each has its own
+    int splits, k_shares;  // all shares, and those of k: where p has two terms, upper bits and rest, one behind the other, each has its own
     void* parts;  // instead of an epilogue: sums as they are, splits x m x n (gated: x 2 n), float or 32-bit integers
     bool tiled;   // those of weight gradients tile by tile, as the registers hold them (splits x tiles x TM x TN)
     Epilogue e;
